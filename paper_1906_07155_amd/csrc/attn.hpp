@@ -1,0 +1,235 @@
+// attn.hpp -- device-side parts shared by the attention kernels of the relation head.
+//
+// Every product runs on 16x16 matrix instructions.  Operand layouts (lane l, n = l % 16,
+// g = l / 16): A holds row n, B holds column n, both the k-slots 8g .. 8g + 7 of a step of
+// 32; the result has column n and rows 4g + i, i = 0..3.  Binary32 has steps of 4, k-slot g:
+// eight of them, the j-th taking element j of the same registers, make the same step of 32.
+//
+// Two things follow from the freedom to order rows and k-slots as one likes:
+//   - A lane's results of two 16-row tiles (rows 4g + i of either) are, as they stand, its B
+//     operand of a step of 32 in which slot 8g + j is row 4g + j of the first tile (j < 4)
+//     or row 4g + j - 4 of the second: the softmax weights never leave their lane.
+//   - The transposed operand (channels as rows) is read straight from row-major memory: lane
+//     n takes channels 2n and 2n + 1 of its eight rows, and the low and the high halves
+//     are the A operands of two 16-channel tiles, channel 2r + t in row r of tile t.  Of the
+//     two results a lane then holds channels 8g .. 8g + 7 of its column: one 16-byte store.
+#pragma once
+
+#include "relation.hpp"
+
+namespace rex {
+
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using f32x2 = float __attribute__((ext_vector_type(2)));
+using f32x8 = float __attribute__((ext_vector_type(8)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using i32x4 = int __attribute__((ext_vector_type(4)));
+
+constexpr float kInf = __builtin_inff();
+
+template <typename T> struct Num;     // the operands of one type
+
+template <> struct Num<uint16_t> {    // bf16
+    using Frag = bf16x8;
+    using Pair = uint32_t;            // two adjacent channels
+    static constexpr int kSize = 2;
+    static __device__ __forceinline__ Frag zero() { return Frag{}; }
+    static __device__ __forceinline__ Frag load(const char *p) {
+        return *(const REX_GLOBAL Frag *)(p);
+    }
+    static __device__ __forceinline__ Frag load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+        return __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+    }
+    static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+        return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+    }
+    static __device__ __forceinline__ Pair no_pair() { return 0u; }
+    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    // the two 16-channel operands of eight pairs
+    static __device__ __forceinline__ void split(const Pair (&x)[8], Frag &lo, Frag &hi) {
+        u32x4 a, b;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            a[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
+            b[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x07060302u);
+        }
+        lo = __builtin_bit_cast(Frag, a);
+        hi = __builtin_bit_cast(Frag, b);
+    }
+    static __device__ __forceinline__ Frag round(const float (&x)[8]) {
+        Frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = static_cast<__bf16>(x[j]);
+        return f;
+    }
+    static constexpr bool kExact = false;     // round() cuts off
+    // x rounded, and x left with what that cut off
+    static __device__ __forceinline__ Frag round_off(float (&x)[8]) {
+        const Frag f = round(x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] -= static_cast<float>(f[j]);
+        return f;
+    }
+    // eight channels to memory
+    static __device__ __forceinline__ void store(char *p, const float (&x)[8]) {
+        *(REX_GLOBAL Frag *)(p) = round(x);
+    }
+    // four codes of the memory -> four numbers
+    static __device__ __forceinline__ void widen(Frag &f, int at, uint32_t c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            f[at + j] = static_cast<__bf16>(static_cast<float>(static_cast<int8_t>(c >> (8 * j))));
+    }
+};
+
+template <> struct Num<float> {
+    using Frag = f32x8;
+    using Pair = f32x2;
+    static constexpr int kSize = 4;
+    static __device__ __forceinline__ Frag zero() { return Frag{}; }
+    static __device__ __forceinline__ Frag load(const char *p) {
+        const f32x4 a = *(const REX_GLOBAL f32x4 *)(p);
+        const f32x4 b = *(const REX_GLOBAL f32x4 *)(p + 16);
+        return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
+    static __device__ __forceinline__ Frag load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+        const f32x4 a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+        const f32x4 b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16, 0, 0));
+        return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
+    static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+        return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+    }
+    static __device__ __forceinline__ Pair no_pair() { return Pair{}; }
+    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ void split(const Pair (&x)[8], Frag &lo, Frag &hi) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            lo[j] = x[j][0];
+            hi[j] = x[j][1];
+        }
+    }
+    static __device__ __forceinline__ Frag round(const float (&x)[8]) {
+        return Frag{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+    }
+    static constexpr bool kExact = true;
+    static __device__ __forceinline__ Frag round_off(float (&x)[8]) { return round(x); }
+    static __device__ __forceinline__ void store(char *p, const float (&x)[8]) {
+        *(REX_GLOBAL f32x4 *)(p) = f32x4{x[0], x[1], x[2], x[3]};
+        *(REX_GLOBAL f32x4 *)(p + 16) = f32x4{x[4], x[5], x[6], x[7]};
+    }
+    static __device__ __forceinline__ void widen(Frag &f, int at, uint32_t c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[at + j] = static_cast<float>(static_cast<int8_t>(c >> (8 * j)));
+    }
+};
+
+// acc += A x for weights x of which bf16 keeps the first TERMS rounded parts: 1 rounds them
+// once, 2 leaves up to 2^-16 of them out, 3 nothing that binary32 sums would keep.
+template <typename T, int TERMS, int NT>
+__device__ __forceinline__ void add_weighted(const typename Num<T>::Frag (&rows)[NT], float (&x)[8],
+                                             f32x4 (&acc)[NT]) {
+    using N = Num<T>;
+#pragma unroll
+    for (int i = 0; i < (N::kExact ? 1 : TERMS); ++i) {
+        const typename N::Frag f = i + 1 < TERMS ? N::round_off(x) : N::round(x);
+#pragma unroll
+        for (int k = 0; k < NT; ++k) acc[k] = N::mma(rows[k], f, acc[k]);
+    }
+}
+
+// The first `rows` rows of one head of one image, read through a buffer resource: a lane's
+// 32-bit offset past the last of them (or marked kBufOOB: channels past D) reads 0 without
+// an access, so tiles may run over the end and padding is never read.  The host checks that (rows + 32) * stride stays
+// below kBufMaxBytes, so no offset wraps.
+struct HeadRows {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t sr;              // bytes from row to row
+};
+template <typename T>
+__device__ __forceinline__ HeadRows head_rows(const Rows &x, int b, int head, int rows, int D) {
+    const char *base = static_cast<const char *>(x.p) + b * x.sb + static_cast<int64_t>(head) * x.sh;
+    const uint32_t bytes = rows > 0 ? static_cast<uint32_t>(rows - 1) * x.sr + D * Num<T>::kSize : 0u;
+    return HeadRows{make_rsrc(base, bytes), x.sr};
+}
+// Lane offsets inside a row: of the operand whose rows are rows (channels 32k + 8g ..), and
+// of the one whose rows are channels (32k + 2n and the next), marked where past D.
+template <typename T>
+__device__ __forceinline__ uint32_t frag_col(int k, int g, int D) {
+    const int ch = 32 * k + 8 * g;
+    return ch < D ? static_cast<uint32_t>(ch * Num<T>::kSize) : kBufOOB;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pair_col(int k, int n, int D) {
+    const int ch = 32 * k + 2 * n;
+    return ch < D ? static_cast<uint32_t>(ch * Num<T>::kSize) : kBufOOB;
+}
+// The transposed operand of 32 rows from row `first` on: 2 * DB tiles of 16 channels.
+template <typename T, int DB>
+__device__ __forceinline__ void load_pairs(const HeadRows &h, uint32_t off0, const uint32_t (&col)[DB],
+                                           typename Num<T>::Pair (&x)[DB][8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t off = off0 + (j < 4 ? j : 12 + j) * h.sr;      // + 4g rows, in off0
+#pragma unroll
+        for (int k = 0; k < DB; ++k) x[k][j] = Num<T>::load_pair(h.r, off + col[k]);
+    }
+}
+
+// Largest / sum over the four lanes that share a column (l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float max_over_rows(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float sum_over_rows(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// Row of the streamed 32 that element j of a lane's operand is (see above).
+__device__ __forceinline__ int slot_row(int g, int j) { return j < 4 ? 4 * g + j : 12 + 4 * g + j; }
+
+// A box as the bucket rule sees it: centre and, for a query, 1 / side.
+struct BoxGeo {
+    float cx, cy, ix, iy;
+};
+__device__ __forceinline__ void box_centre(const REX_GLOBAL float *b, float &cx, float &cy) {
+    cx = (b[0] + b[2]) * 0.5f;
+    cy = (b[1] + b[3]) * 0.5f;
+}
+__device__ __forceinline__ BoxGeo box_geo(const REX_GLOBAL float *b) {
+    BoxGeo o;
+    box_centre(b, o.cx, o.cy);
+    o.ix = 1.0f / fmaxf(b[2] - b[0], 1.0f);
+    o.iy = 1.0f / fmaxf(b[3] - b[1], 1.0f);
+    return o;
+}
+// Signed bucket of one axis in [-half, half].  The magnitude's edges are binary32 numbers
+// whose low bits are 0, so counting those reached is a shift of the bits of |r|.
+__device__ __forceinline__ int axis_bucket(float r, const BucketRule &b) {
+    const int e = static_cast<int>((__float_as_uint(r) & 0x7fffffffu) >> b.shift) - b.base + 1;
+    const int m = min(max(e, 0), b.half);
+    return r < 0.0f ? -m : m;
+}
+// Byte offset of a pair's entry in one head's table.
+__device__ __forceinline__ uint32_t pair_bucket(const BoxGeo &q, float kx, float ky,
+                                                const BucketRule &b) {
+    const int bx = axis_bucket((kx - q.cx) * q.ix, b);
+    const int by = axis_bucket((ky - q.cy) * q.iy, b);
+    return static_cast<uint32_t>(((by + b.half) * b.nb + bx + b.half) * 4);
+}
+
+constexpr int kBuckStride = 36;   // 16-bit entries of one column's 32 rows in LDS (8-byte reads
+                                  // of 16 columns then start in 16 different bank pairs)
+
+// Workgroup ids in runs per XCD: ids go to the eight XCDs in turn, so handing each of them
+// one run of neighbouring tiles keeps an image's keys in one L2.  n is a multiple of 8.
+__device__ __forceinline__ int xcd_run(int id, int n) { return (id & 7) * (n >> 3) + (id >> 3); }
+
+}  // namespace rex

@@ -1,0 +1,573 @@
+// attn_bwd.hip -- the backward of the attention among boxes (box_attn_bwd).
+//
+//   rowstat   per (row, head): the row's log sum in units of log 2 (+inf where the row has no
+//             part), and delta = sum_c grad_out * out
+//   dq        query columns, keys streamed: grad_q and the bias gradient
+//   dkv       key columns, queries streamed, over the heads that share the key head: grad_k,
+//             grad_v
+//   hist      the bias gradient's partial tables added up
+//
+// Both passes compute the weights again from q, k and the row's log sum (seven products of
+// the pair matrix instead of five), which costs less than adding one side's gradient with
+// atomics, and every element is written once and in a fixed order.
+//
+// The bias gradient is a histogram of ds by bucket.  Each wave adds into a table of its own
+// in LDS: LDS serves a wave's additions in order, so the sums repeat bit for bit.
+#include "attn.hpp"
+
+namespace rex {
+
+namespace {
+
+
+template <typename T>
+__global__ __launch_bounds__(256) void attn_rowstat_kernel(AttnArgs a) {
+    using N = Num<T>;
+    using Frag = typename N::Frag;
+    const int lanes = a.D <= 32 ? 4 : a.D <= 64 ? 8 : 16, c = threadIdx.x & (lanes - 1);
+    const int64_t e = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / lanes;
+    // e = (b * Nqp + row) * H + h
+    const int h = static_cast<int>(e % a.H);
+    const int row = static_cast<int>(e / a.H % a.Nqp);
+    const int64_t b = e / (static_cast<int64_t>(a.H) * a.Nqp);
+    if (b >= a.B) return;
+    const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
+    const int64_t bh = b * a.H + h;
+    float lse = -kInf, delta = 0.0f;
+    if (row < qlen) {
+        lse = as_global<float>(a.flse)[bh * a.Nq + row];
+        if (8 * c < a.D) {
+            const int64_t at = (((b * a.Nq + row) * a.H + h) * a.D + 8 * c) * N::kSize;
+            const Frag g = N::load(static_cast<const char *>(a.gout.p) + at);
+            f32x8 o;
+            if (a.fout_f32) {
+                o = Num<float>::load(reinterpret_cast<const char *>(a.fout_f32) + at * (4 / N::kSize));
+            } else {
+                const Frag f = N::load(static_cast<const char *>(a.fout) + at);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = static_cast<float>(f[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) delta = fmaf(static_cast<float>(g[i]), o[i], delta);
+        }
+    }
+    for (int d = 1; d < lanes; d <<= 1) delta += __shfl_xor(delta, d);
+    if (c == 0) {
+        const bool none = lse == -kInf;
+        *(REX_GLOBAL f32x2 *)(a.rowstat + (bh * a.Nqp + row) * 2) =
+            none ? f32x2{kInf, 0.0f} : f32x2{lse * kLog2e, delta};
+    }
+}
+
+// Steps whose buckets are computed between two barriers.
+inline __host__ __device__ int bwd_ahead(int parts) { return parts >= 4 ? 1 : 4 / parts; }
+
+// LDS of the two passes, bytes.
+struct BwdLds {
+    int bias, hist, geo, buck, acc, total;
+};
+inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, int tables, int nb,
+                                          bool bias, bool hist) {
+    BwdLds l{};
+    int at = 0;
+    const int table = (nb * nb * 4 + 15) & ~15;
+    l.hist = at;
+    if (bias && hist) at += kAttnWaves * table;
+    l.bias = at;
+    if (bias) at += tables * table;
+    l.geo = at;
+    if (bias) at += cols * 16;
+    l.buck = at;
+    if (bias) at += 2 * bwd_ahead(parts) * parts * cols * kBuckStride * 2;
+    l.acc = l.bias;               // the end: only the histograms are still needed
+    const int end = l.acc + (parts > 1 ? hp * parts * cols * (dp + 4) * 4 : 0);
+    l.total = at > end ? at : end;
+    return l;
+}
+
+template <typename T, int DB, int NS, bool BIAS, int TERMS>
+__global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a) {
+    using N = Num<T>;
+    using Frag = typename N::Frag;
+    using Pair = typename N::Pair;
+    constexpr int kCols = 16 * NS, kDP = 32 * DB;
+    extern __shared__ char smem[];
+    const int id = xcd_run(blockIdx.x, gridDim.x);
+    if (id >= a.nwg) return;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hp = a.hp, parts = a.parts, hw = wave & (hp - 1), kw = wave / hp;
+    int rest = id;
+    const int sp = rest % a.spans;
+    rest /= a.spans;
+    const int hgroups = a.H / hp;
+    const int h0 = (rest % hgroups) * hp, b = rest / hgroups;
+    const int h = h0 + hw, kh = h / a.group;
+    const int nb2 = a.rule.nb * a.rule.nb, table = (nb2 * 4 + 15) & ~15;
+    const int ahead = bwd_ahead(parts);
+    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, hp, a.rule.nb, BIAS, true);
+
+    const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
+    const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
+    const int all = (klen + kTile - 1) / kTile;
+    BoxGeo *geo = reinterpret_cast<BoxGeo *>(smem + lds.geo);
+    uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
+    char *hist = smem + lds.hist + wave * table;
+    const float sl2 = a.scale * kLog2e;
+    const char *tab = smem + lds.bias + hw * table;
+    uint32_t fcol[DB], pcol[DB];
+#pragma unroll
+    for (int k = 0; k < DB; ++k) {
+        fcol[k] = frag_col<T>(k, g, a.D);
+        pcol[k] = pair_col<T>(k, n, a.D);
+    }
+    const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
+    const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
+    if (BIAS) {
+        for (int i = lane; i < nb2; i += 64) reinterpret_cast<float *>(hist)[i] = 0.0f;
+    }
+
+    auto fill_buckets = [&](int chunk, int t1) {
+        const int r = lane & 31;
+        for (int i = 0; i < ahead; ++i) {
+            const int tile = (chunk * ahead + i) * parts + kw;
+            if (tile >= t1) return;
+            float kx, ky;
+            box_centre(as_global<float>(a.kbox + b * a.kbox_sb + min(tile * kTile + r, a.Nk - 1) * a.kbox_sr),
+                       kx, ky);
+            uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
+            for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
+                dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(geo[c], kx, ky, a.rule));
+        }
+    };
+
+    const int last = min((sp + 1) * a.span, a.tiles);
+    for (int tile_q = sp * a.span; tile_q < last; ++tile_q) {
+        const int q0 = tile_q * kCols;
+        const int t1 = q0 < qlen ? all : 0;
+        Frag q[NS][DB], go[NS][DB];
+        float lse[NS], delta[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int row = q0 + 16 * s + n;
+#pragma unroll
+            for (int k = 0; k < DB; ++k) {
+                q[s][k] = N::load(qr.r, row * qr.sr + fcol[k]);
+                go[s][k] = N::load(gr.r, row * gr.sr + fcol[k]);
+            }
+            const f32x2 st = *(const REX_GLOBAL f32x2 *)(
+                a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + min(row, a.Nqp - 1)) * 2);
+            lse[s] = st[0];
+            delta[s] = st[1];
+        }
+        if (BIAS) {
+            __syncthreads();          // the last tile's end has been read
+            for (int i = lane; i < nb2; i += 64)
+                if (kw == 0)
+                    reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] =
+                        as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i] * kLog2e;
+            if (tid < kCols)
+                geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
+                                                    min(q0 + tid, a.Nq - 1) * a.qbox_sr));
+            __syncthreads();
+            fill_buckets(0, t1);
+        }
+        f32x4 dq[NS][2 * DB] = {};
+        const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            if (BIAS) {
+                __syncthreads();
+                if (chunk + 1 < chunks) fill_buckets(chunk + 1, t1);
+            }
+            for (int it = 0; it < ahead; ++it) {
+                const int tile = (chunk * ahead + it) * parts + kw;
+                if (tile >= t1) break;
+                Pair kp[DB][8];
+                load_pairs<T, DB>(kr, (tile * kTile + 4 * g) * kr.sr, pcol, kp);
+                const int key = tile * kTile + (lane & 31);
+                bool on = key < klen;
+                if (a.kmask)
+                    on = on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
+                const uint32_t vis = static_cast<uint32_t>(__ballot(on));
+                const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+                float x[NS][8];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    Frag kf[DB], vf[DB];
+#pragma unroll
+                    for (int k = 0; k < DB; ++k) {
+                        kf[k] = N::load(kr.r, (tile * kTile + 16 * t + n) * kr.sr + fcol[k]);
+                        vf[k] = N::load(vr.r, (tile * kTile + 16 * t + n) * vr.sr + fcol[k]);
+                    }
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        f32x4 sc = {}, dp = {};
+#pragma unroll
+                        for (int k = 0; k < DB; ++k) {
+                            sc = N::mma(kf[k], q[s][k], sc);
+                            dp = N::mma(vf[k], go[s][k], dp);
+                        }
+                        u32x2 at = {};
+                        if (BIAS) at = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t off = i & 1 ? at[i >> 1] >> 16 : at[i >> 1] & 0xffffu;
+                            float v = sc[i] * sl2;
+                            if (BIAS) v = fmaf(sc[i], sl2, *reinterpret_cast<const float *>(tab + off));
+                            float ds = __builtin_amdgcn_exp2f(v - lse[s]) * (dp[i] - delta[s]);
+                            if (vis != 0xffffffffu) ds = (vis >> (16 * t + 4 * g + i)) & 1u ? ds : 0.0f;
+                            x[s][4 * t + i] = ds;
+                            if (BIAS) atomicAdd(reinterpret_cast<float *>(hist + off), ds);
+                        }
+                    }
+                }
+                if (vis != 0xffffffffu) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int k = 0; k < DB; ++k)
+                            kp[k][j] = (vis >> slot_row(g, j)) & 1u ? kp[k][j] : N::no_pair();
+                }
+                Frag kt[2 * DB];
+#pragma unroll
+                for (int k = 0; k < DB; ++k) N::split(kp[k], kt[2 * k], kt[2 * k + 1]);
+#pragma unroll
+                for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(kt, x[s], dq[s]);
+            }
+        }
+        auto finish = [&](int col, int head, int ch, const float (&x)[8]) {
+            const int row = q0 + col;
+            if (row >= a.Nq || ch >= a.D) return;
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = row < qlen ? x[i] * a.scale : 0.0f;
+            N::store(static_cast<char *>(a.gq) +
+                         (((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch) * N::kSize, y);
+        };
+        if (parts == 1) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int k = 0; k < DB; ++k) {
+                    float y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = dq[s][2 * k + (i & 1)][i >> 1];
+                    finish(16 * s + n, h, 32 * k + 8 * g, y);
+                }
+            continue;
+        }
+        float *acc = reinterpret_cast<float *>(smem + lds.acc);
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int k = 0; k < DB; ++k) {
+                float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4) + 32 * k + 8 * g;
+#pragma unroll
+                for (int i = 0; i < 8; i += 4)
+                    *reinterpret_cast<f32x4 *>(dst + i) =
+                        f32x4{dq[s][2 * k][i >> 1], dq[s][2 * k + 1][i >> 1], dq[s][2 * k][(i >> 1) + 1],
+                              dq[s][2 * k + 1][(i >> 1) + 1]};
+            }
+        __syncthreads();
+        for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
+            const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
+            float y[8] = {};
+            for (int p = 0; p < parts; ++p) {
+                const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] += src[i];
+            }
+            finish(col, h0 + w, ch, y);
+        }
+        __syncthreads();
+    }
+    if (BIAS) {
+        __syncthreads();
+        for (int e = tid; e < hp * nb2; e += kAttnWaves * 64) {
+            const int w = e / nb2, i = e - w * nb2;
+            float sum = 0.0f;
+            for (int p = 0; p < parts; ++p)
+                sum += reinterpret_cast<const float *>(smem + lds.hist + (p * hp + w) * table)[i];
+            as_global_mut<float>(a.hist)[((static_cast<int64_t>(b) * a.spans + sp) * a.H + h0 + w) * nb2 + i] = sum;
+        }
+    }
+}
+
+template <typename T, int DB, int NS, bool BIAS, int TERMS>
+__global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a) {
+    using N = Num<T>;
+    using Frag = typename N::Frag;
+    using Pair = typename N::Pair;
+    constexpr int kCols = 16 * NS, kDP = 32 * DB;
+    extern __shared__ char smem[];
+    const int id = xcd_run(blockIdx.x, gridDim.x);
+    if (id >= a.nwg) return;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hp = a.hp, parts = a.parts, hw = wave & (hp - 1), kw = wave / hp;
+    int rest = id;
+    const int tile_k = rest % a.tiles;
+    rest /= a.tiles;
+    const int hgroups = a.Hkv / hp;
+    const int kh0 = (rest % hgroups) * hp, b = rest / hgroups;
+    const int kh = kh0 + hw;
+    const int nb2 = a.rule.nb * a.rule.nb, table = (nb2 * 4 + 15) & ~15;
+    const int ahead = bwd_ahead(parts);
+    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, hp * a.head_step, a.rule.nb, BIAS, false);
+
+    const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
+    const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
+    const int k0 = tile_k * kCols;
+    const int t1 = k0 < klen ? (qlen + kTile - 1) / kTile : 0;
+    f32x2 *ctr = reinterpret_cast<f32x2 *>(smem + lds.geo);
+    uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
+    const float sl2 = a.scale * kLog2e;
+    uint32_t fcol[DB], pcol[DB];
+#pragma unroll
+    for (int k = 0; k < DB; ++k) {
+        fcol[k] = frag_col<T>(k, g, a.D);
+        pcol[k] = pair_col<T>(k, n, a.D);
+    }
+
+    // The key columns.  A masked key's column is whatever its row makes of it: no other column
+    // sees it, and zeros are written for it at the end.
+    Frag kf[NS][DB], vf[NS][DB];
+    {
+        const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int k = 0; k < DB; ++k) {
+                kf[s][k] = N::load(kr.r, (k0 + 16 * s + n) * kr.sr + fcol[k]);
+                vf[s][k] = N::load(vr.r, (k0 + 16 * s + n) * vr.sr + fcol[k]);
+            }
+    }
+    if (BIAS && tid < kCols) {
+        float cx, cy;
+        box_centre(as_global<float>(a.kbox + b * a.kbox_sb + min(k0 + tid, a.Nk - 1) * a.kbox_sr), cx, cy);
+        ctr[tid] = f32x2{cx, cy};
+    }
+    // here the streamed side is the queries: row r of the tile is query 32 * tile + r
+    auto fill_buckets = [&](int chunk) {
+        const int r = lane & 31;
+        for (int i = 0; i < ahead; ++i) {
+            const int tile = (chunk * ahead + i) * parts + kw;
+            if (tile >= t1) return;
+            const BoxGeo q = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
+                                                      min(tile * kTile + r, a.Nq - 1) * a.qbox_sr));
+            uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
+            for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
+                dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(q, ctr[c][0], ctr[c][1], a.rule));
+        }
+    };
+
+    f32x4 dk[NS][2 * DB] = {}, dv[NS][2 * DB] = {};
+    const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
+    for (int first = 0; first < a.group; first += a.head_step) {
+        const int many = min(a.head_step, a.group - first);
+        if (BIAS) {
+            __syncthreads();              // the tables of the last heads have been read
+            for (int c = 0; c < many; ++c)
+                for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
+                    reinterpret_cast<float *>(smem + lds.bias + (hw * a.head_step + c) * table)[i] =
+                        as_global<float>(a.bias)[static_cast<int64_t>(kh * a.group + first + c) * nb2 + i] * kLog2e;
+            fill_buckets(0);
+        }
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            if (BIAS) {
+                __syncthreads();
+                if (chunk + 1 < chunks) fill_buckets(chunk + 1);
+            }
+            for (int it = 0; it < ahead; ++it) {
+                const int tile = (chunk * ahead + it) * parts + kw;
+                if (tile >= t1) break;
+                const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+                for (int c = 0; c < many; ++c) {
+                    const int h = kh * a.group + first + c;
+                    const char *tab = smem + lds.bias + (hw * a.head_step + c) * table;
+                    const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
+                    const float *stat = a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + tile * kTile) * 2;
+                    float pr[NS][8], ds[NS][8];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        Frag qf[DB], gf[DB];
+#pragma unroll
+                        for (int k = 0; k < DB; ++k) {
+                            qf[k] = N::load(qr.r, (tile * kTile + 16 * t + n) * qr.sr + fcol[k]);
+                            gf[k] = N::load(gr.r, (tile * kTile + 16 * t + n) * gr.sr + fcol[k]);
+                        }
+                        const f32x4 st0 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2);
+                        const f32x4 st1 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2 + 4);
+                        const float lse[4] = {st0[0], st0[2], st1[0], st1[2]};
+                        const float delta[4] = {st0[1], st0[3], st1[1], st1[3]};
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) {
+                            f32x4 sc = {}, dp = {};
+#pragma unroll
+                            for (int k = 0; k < DB; ++k) {
+                                sc = N::mma(qf[k], kf[s][k], sc);
+                                dp = N::mma(gf[k], vf[s][k], dp);
+                            }
+                            u32x2 at = {};
+                            if (BIAS) at = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t off = i & 1 ? at[i >> 1] >> 16 : at[i >> 1] & 0xffffu;
+                                float v = sc[i] * sl2;
+                                if (BIAS) v = fmaf(sc[i], sl2, *reinterpret_cast<const float *>(tab + off));
+                                const float p = __builtin_amdgcn_exp2f(v - lse[i]);
+                                pr[s][4 * t + i] = p;
+                                ds[s][4 * t + i] = p * (dp[i] - delta[i]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int which = 0; which < 2; ++which) {
+                        const HeadRows &r = which ? qr : gr;
+                        Pair p[DB][8];
+                        load_pairs<T, DB>(r, (tile * kTile + 4 * g) * r.sr, pcol, p);
+                        Frag rows[2 * DB];
+#pragma unroll
+                        for (int k = 0; k < DB; ++k) N::split(p[k], rows[2 * k], rows[2 * k + 1]);
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) {
+                            if (which) add_weighted<T, TERMS, 2 * DB>(rows, ds[s], dk[s]);
+                            else add_weighted<T, TERMS, 2 * DB>(rows, pr[s], dv[s]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    auto finish = [&](char *out, float f, int col, int head, int ch, const float (&x)[8]) {
+        const int key = k0 + col;
+        if (key >= a.Nk || ch >= a.D) return;
+        bool on = key < klen;
+        if (a.kmask && on) on = as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + key] != 0;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = on ? x[i] * f : 0.0f;
+        N::store(out + (((static_cast<int64_t>(b) * a.Nk + key) * a.Hkv + head) * a.D + ch) * N::kSize, y);
+    };
+    auto write = [&](const f32x4 (&d)[NS][2 * DB], char *out, float f) {
+        if (parts == 1) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int k = 0; k < DB; ++k) {
+                    float y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = d[s][2 * k + (i & 1)][i >> 1];
+                    finish(out, f, 16 * s + n, kh, 32 * k + 8 * g, y);
+                }
+            return;
+        }
+        float *acc = reinterpret_cast<float *>(smem + lds.acc);
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int k = 0; k < DB; ++k) {
+                float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4) + 32 * k + 8 * g;
+#pragma unroll
+                for (int i = 0; i < 8; i += 4)
+                    *reinterpret_cast<f32x4 *>(dst + i) =
+                        f32x4{d[s][2 * k][i >> 1], d[s][2 * k + 1][i >> 1], d[s][2 * k][(i >> 1) + 1],
+                              d[s][2 * k + 1][(i >> 1) + 1]};
+            }
+        __syncthreads();
+        for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
+            const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
+            float y[8] = {};
+            for (int p = 0; p < parts; ++p) {
+                const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] += src[i];
+            }
+            finish(out, f, col, kh0 + w, ch, y);
+        }
+    };
+    write(dk, static_cast<char *>(a.gk), a.scale);
+    write(dv, static_cast<char *>(a.gv), 1.0f);
+}
+
+// gbias[h][i] = sum over the partial tables, 16 slices of them side by side, in order.
+__global__ __launch_bounds__(1024) void attn_hist_kernel(AttnArgs a) {
+    __shared__ float part[16][64];
+    const int64_t n = static_cast<int64_t>(a.H) * a.rule.nb * a.rule.nb;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63);
+    const int slice = threadIdx.x >> 6;
+    float sum = 0.0f;
+    if (i < n) {
+        gcptr<float> src = as_global<float>(a.hist);
+        const int chunks = a.B * a.spans;
+        for (int c = slice; c < chunks; c += 16) sum += src[c * n + i];
+    }
+    part[slice][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (slice == 0 && i < n) {
+        for (int s = 1; s < 16; ++s) sum += part[s][threadIdx.x];
+        as_global_mut<float>(a.gbias)[i] = sum;
+    }
+}
+
+template <typename T, int DB, int NS, int TERMS>
+void run_pass(const AttnArgs &a, bool keys, hipStream_t s) {
+    if (a.nwg == 0) return;
+    const dim3 grid((a.nwg + 7) & ~7), block(kAttnWaves * 64);
+    const bool bias = a.bias != nullptr;
+    const BwdLds lds = bwd_lds(16 * NS, 32 * DB, a.hp, a.parts, keys ? a.hp * a.head_step : a.hp,
+                               a.rule.nb, bias, !keys);
+    if (keys && bias)
+        hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, true, TERMS>), grid, block, lds.total, s, a);
+    else if (keys)
+        hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, false, TERMS>), grid, block, lds.total, s, a);
+    else if (bias)
+        hipLaunchKernelGGL((attn_dq_kernel<T, DB, NS, true, TERMS>), grid, block, lds.total, s, a);
+    else
+        hipLaunchKernelGGL((attn_dq_kernel<T, DB, NS, false, TERMS>), grid, block, lds.total, s, a);
+}
+
+template <typename T, int TERMS>
+void run_sized(const AttnArgs &a, bool keys, int cols, hipStream_t s) {
+    if (a.D <= 32) {
+        if (cols == 16) run_pass<T, 1, 1, TERMS>(a, keys, s);
+        else run_pass<T, 1, 2, TERMS>(a, keys, s);
+    } else if (a.D <= 64) {
+        if (cols == 16) run_pass<T, 2, 1, TERMS>(a, keys, s);
+        else run_pass<T, 2, 2, TERMS>(a, keys, s);
+    } else {
+        run_pass<T, 4, 1, TERMS>(a, keys, s);
+    }
+}
+
+void run_typed(const AttnArgs &a, int dtype, bool keys, int cols, hipStream_t s) {
+    if (dtype == kF32) run_sized<float, 1>(a, keys, cols, s);
+    else if (a.terms > 1) run_sized<uint16_t, 2>(a, keys, cols, s);
+    else run_sized<uint16_t, 1>(a, keys, cols, s);
+}
+
+}  // namespace
+
+hipError_t launch_attn_bwd(const AttnArgs &dq, const AttnArgs &dkv, int dtype, int dq_cols,
+                           int dkv_cols, hipStream_t s) {
+    const int lanes = dq.D <= 32 ? 4 : dq.D <= 64 ? 8 : 16;
+    const int64_t n = static_cast<int64_t>(dq.B) * dq.H * dq.Nqp * lanes;
+    const dim3 grid(static_cast<uint32_t>((n + 255) / 256));
+    if (n > 0 && dtype == kBF16)
+        hipLaunchKernelGGL((attn_rowstat_kernel<uint16_t>), grid, dim3(256), 0, s, dq);
+    else if (n > 0)
+        hipLaunchKernelGGL((attn_rowstat_kernel<float>), grid, dim3(256), 0, s, dq);
+    run_typed(dq, dtype, false, dq_cols, s);
+    run_typed(dkv, dtype, true, dkv_cols, s);
+    if (dq.bias) {
+        const int64_t t = static_cast<int64_t>(dq.H) * dq.rule.nb * dq.rule.nb;
+        hipLaunchKernelGGL(attn_hist_kernel, dim3(static_cast<uint32_t>((t + 63) / 64)), dim3(1024), 0,
+                           s, dq);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace rex

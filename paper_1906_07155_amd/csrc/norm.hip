@@ -1,0 +1,450 @@
+// norm.hip -- the norms around a block with its gate and residual sum (gated_norm_fwd,
+// gated_norm_bwd):  y = x + alpha * gate * N1(branch),  u = N2(y).
+//
+// A row stays in the registers of TPR threads, V chunks of 16 bytes each, from its one read
+// to its one write: mean and variance are two sums over what is already there (the variance
+// of the deviations, not of the squares).  Both directions are bound by the bytes of
+// the rows.  The column sums of the backward are kept in registers over all the rows of a
+// workgroup and added up in a fixed order by a second kernel.
+#include "attn.hpp"
+
+namespace rex {
+
+namespace {
+
+// A workgroup: several rows side by side, or one row of up to 1024 threads.
+constexpr int threads_of(int tpr) { return tpr > 256 ? tpr : 256; }
+
+template <typename T> struct Chunk;    // the elements of 16 bytes
+template <> struct Chunk<uint16_t> { static constexpr int kN = 8; };
+template <> struct Chunk<float> { static constexpr int kN = 4; };
+
+// E elements from column `col` on of a row; columns past C read as 0.
+template <typename T, int E>
+__device__ __forceinline__ void load_row(const void *row, int col, int C, bool vec, float *x) {
+    if (vec) {
+        if (col < C) {
+            if constexpr (E == 8) {
+                const bf16x8 f = *(const REX_GLOBAL bf16x8 *)(static_cast<const char *>(row) + col * 2);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(f[i]);
+            } else {
+                const f32x4 f = *(const REX_GLOBAL f32x4 *)(static_cast<const char *>(row) + col * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = f[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) x[i] = 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = col + i < C ? load_f32<T>(as_global<T>(row) + col + i) : 0.0f;
+    }
+}
+
+template <typename T, int E>
+__device__ __forceinline__ void store_row(void *row, int col, int C, bool vec, const float *x) {
+    if (vec) {
+        if (col >= C) return;
+        if constexpr (E == 8) {
+            bf16x8 f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = static_cast<__bf16>(x[i]);
+            *(REX_GLOBAL bf16x8 *)(static_cast<char *>(row) + col * 2) = f;
+        } else {
+            *(REX_GLOBAL f32x4 *)(static_cast<char *>(row) + col * 4) = f32x4{x[0], x[1], x[2], x[3]};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (col + i < C) store_f32<T>(as_global_mut<T>(row) + col + i, x[i]);
+    }
+}
+
+// E parameters (binary32, 4-byte aligned) or `none` where there is no such array.
+template <int E>
+__device__ __forceinline__ void load_param(const float *p, int col, int C, float none, float *x) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = p && col + i < C ? as_global<float>(p)[col + i] : none;
+}
+
+// Sums of two values over the TPR threads of a row; every one of them gets both.
+template <int TPR>
+__device__ __forceinline__ void row_sum(float &a, float &b, f32x2 (&mem)[2][16], int &turn) {
+#pragma unroll
+    for (int d = 1; d < (TPR < 64 ? TPR : 64); d <<= 1) {
+        a += __shfl_xor(a, d);
+        b += __shfl_xor(b, d);
+    }
+    if constexpr (TPR > 64) {
+        constexpr int kWaves = TPR / 64;
+        const int wave = threadIdx.x >> 6, first = wave / kWaves * kWaves;
+        if ((threadIdx.x & 63) == 0) mem[turn][wave] = f32x2{a, b};
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            a += mem[turn][first + w][0];
+            b += mem[turn][first + w][1];
+        }
+        turn ^= 1;        // the next sum writes elsewhere, so one barrier is enough
+    }
+}
+
+template <typename T, int TPR, int V>
+__global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(NormArgs a) {
+    constexpr int E = Chunk<T>::kN;
+    constexpr int kThreads = threads_of(TPR);
+    __shared__ f32x2 mem[2][16];
+    int turn = 0;
+    const int t = threadIdx.x % TPR;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / TPR) + threadIdx.x / TPR;
+    const bool on = row < a.rows;                 // (one row per workgroup: always)
+    const int64_t r = on ? row : a.rows - 1;
+    const float inv = 1.0f / static_cast<float>(a.C);
+    float y[V][E];
+    float stat[4] = {};
+
+    // deviations from the mean in place, their 1 / sqrt in rstd
+    auto norm = [&](float (&v)[V][E], float &mean, float &rstd) {
+        float s = 0.0f, none = 0.0f;
+        mean = 0.0f;
+        if (a.layer) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) s += v[k][i];
+            row_sum<TPR>(s, none, mem, turn);
+            mean = s * inv;
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[k][i] = (k * TPR + t) * E + i < a.C ? v[k][i] - mean : 0.0f;
+        }
+        s = none = 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int i = 0; i < E; ++i) s = fmaf(v[k][i], v[k][i], s);
+        row_sum<TPR>(s, none, mem, turn);
+        rstd = 1.0f / sqrtf(s * inv + a.eps);
+    };
+
+    const char *px = static_cast<const char *>(a.x) + r * a.x_stride * static_cast<int>(sizeof(T));
+#pragma unroll
+    for (int k = 0; k < V; ++k) load_row<T, E>(px, (k * TPR + t) * E, a.C, a.vec, y[k]);
+    if (a.branch) {
+        float z[V][E];
+        const char *pb = static_cast<const char *>(a.branch) + r * a.b_stride * static_cast<int>(sizeof(T));
+#pragma unroll
+        for (int k = 0; k < V; ++k) load_row<T, E>(pb, (k * TPR + t) * E, a.C, a.vec, z[k]);
+        norm(z, stat[0], stat[1]);
+        const float *gate = a.gate ? a.gate + r / a.rows_per_gate * a.C : nullptr;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int col = (k * TPR + t) * E;
+            float w[E], c[E], g[E];
+            load_param<E>(a.w1, col, a.C, 1.0f, w);
+            load_param<E>(a.c1, col, a.C, 0.0f, c);
+            load_param<E>(gate, col, a.C, 1.0f, g);
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                y[k][i] = fmaf(a.alpha * g[i], fmaf(z[k][i] * stat[1], w[i], c[i]), y[k][i]);
+            if (on && a.y)
+                store_row<T, E>(static_cast<T *>(a.y) + r * a.C, col, a.C, a.vec, y[k]);
+        }
+    } else if (a.y && on) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            store_row<T, E>(static_cast<T *>(a.y) + r * a.C, (k * TPR + t) * E, a.C, a.vec, y[k]);
+    }
+    if (a.second) {
+        if (a.branch) {               // columns past C hold what an empty gate made of them
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if ((k * TPR + t) * E + i >= a.C) y[k][i] = 0.0f;
+        }
+        norm(y, stat[2], stat[3]);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int col = (k * TPR + t) * E;
+            float w[E], c[E];
+            load_param<E>(a.w2, col, a.C, 1.0f, w);
+            load_param<E>(a.c2, col, a.C, 0.0f, c);
+#pragma unroll
+            for (int i = 0; i < E; ++i) y[k][i] = fmaf(y[k][i] * stat[3], w[i], c[i]);
+            if (on && a.u) store_row<T, E>(static_cast<T *>(a.u) + r * a.C, col, a.C, a.vec, y[k]);
+        }
+    }
+    if (a.stats && t == 0 && on)
+        *(REX_GLOBAL f32x4 *)(a.stats + r * 4) = f32x4{stat[0], stat[1], stat[2], stat[3]};
+}
+
+template <typename T, int TPR, int V>
+__global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(NormArgs a) {
+    constexpr int kThreads = threads_of(TPR);
+    constexpr int E = Chunk<T>::kN, kSlots = kThreads / TPR, kSize = sizeof(T);
+    extern __shared__ float cols[];               // [kSlots][C]
+    __shared__ f32x2 mem[2][16];
+    int turn = 0;
+    const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const float inv = 1.0f / static_cast<float>(a.C);
+    float sw1[V][E] = {}, sc1[V][E] = {}, sw2[V][E] = {}, sc2[V][E] = {}, sg[V][E] = {};
+    const bool each = a.gate && a.rows_per_gate == 1;
+
+    // sums over the row slots, in order, to dst[C]
+    auto flush = [&](const float (&s)[V][E], float *dst) {
+        if constexpr (kSlots == 1) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const int col = (k * TPR + t) * E + i;
+                    if (col < a.C) as_global_mut<float>(dst)[col] = s[k][i];
+                }
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const int col = (k * TPR + t) * E + i;
+                    if (col < a.C) cols[slot * a.C + col] = s[k][i];
+                }
+            __syncthreads();
+            for (int col = threadIdx.x; col < a.C; col += kThreads) {
+                float x = 0.0f;
+                for (int q = 0; q < kSlots; ++q) x += cols[q * a.C + col];
+                as_global_mut<float>(dst)[col] = x;
+            }
+        }
+    };
+
+    for (int64_t unit = blockIdx.x; unit < a.units; unit += a.blocks) {
+        const int64_t seg = unit / a.gate_parts, in = (unit - seg * a.gate_parts) * a.unit_rows;
+        const int64_t begin = seg * a.span + in;
+        const int64_t end = min(min(begin + a.unit_rows, (seg + 1) * a.span), a.rows);
+        for (int64_t first = begin; first < end; first += kSlots) {
+            const bool on = first + slot < end;
+            const int64_t r = on ? first + slot : end - 1;
+            const f32x4 st = *(const REX_GLOBAL f32x4 *)(a.stats + r * 4);
+            float x[V][E], b[V][E], g[V][E];
+            const char *px = static_cast<const char *>(a.x) + r * a.x_stride * kSize;
+            const char *pb = static_cast<const char *>(a.branch) + r * a.b_stride * kSize;
+            const char *pu = static_cast<const char *>(a.gu) + r * a.C * kSize;
+            const char *py = static_cast<const char *>(a.gy) + r * a.C * kSize;
+            const float *gate = a.gate ? a.gate + r / a.rows_per_gate * a.C : nullptr;
+            // b: N1's normalised row; x: y, then the gradient of y
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int col = (k * TPR + t) * E;
+                load_row<T, E>(px, col, a.C, a.vec, x[k]);
+                if (a.branch) {
+                    load_row<T, E>(pb, col, a.C, a.vec, b[k]);
+                    float w[E], c[E], ga[E];
+                    load_param<E>(a.w1, col, a.C, 1.0f, w);
+                    load_param<E>(a.c1, col, a.C, 0.0f, c);
+                    load_param<E>(gate, col, a.C, 1.0f, ga);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        b[k][i] = (b[k][i] - st[0]) * st[1];
+                        x[k][i] = fmaf(a.alpha * ga[i], fmaf(b[k][i], w[i], c[i]), x[k][i]);
+                    }
+                }
+            }
+            float s1 = 0.0f, s0 = 0.0f;
+            if (a.gu) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const int col = (k * TPR + t) * E;
+                    float u[E], w[E];
+                    load_row<T, E>(pu, col, a.C, a.vec, u);
+                    load_param<E>(a.w2, col, a.C, 1.0f, w);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        x[k][i] = (x[k][i] - st[2]) * st[3];
+                        if (on) {
+                            sw2[k][i] = fmaf(u[i], x[k][i], sw2[k][i]);
+                            sc2[k][i] += u[i];
+                        }
+                        g[k][i] = u[i] * w[i];          // 0 past C, as u
+                        s1 = fmaf(g[k][i], x[k][i], s1);
+                        s0 += g[k][i];
+                    }
+                }
+                row_sum<TPR>(s1, s0, mem, turn);
+                s1 *= inv;
+                s0 = a.layer ? s0 * inv : 0.0f;
+            }
+            float m1 = 0.0f, m0 = 0.0f;
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int col = (k * TPR + t) * E;
+                float d[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) d[i] = 0.0f;
+                if (a.gy) load_row<T, E>(py, col, a.C, a.vec, d);
+                if (a.gu) {
+#pragma unroll
+                    for (int i = 0; i < E; ++i)
+                        d[i] += st[3] * ((g[k][i] - s0) - x[k][i] * s1);
+                }
+                if (on && a.gx) store_row<T, E>(static_cast<T *>(a.gx) + r * a.C, col, a.C, a.vec, d);
+                if (a.branch) {
+                    float w[E], c[E], ga[E], dg[E];
+                    load_param<E>(a.w1, col, a.C, 1.0f, w);
+                    load_param<E>(a.c1, col, a.C, 0.0f, c);
+                    load_param<E>(gate, col, a.C, 1.0f, ga);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        const float ad = col + i < a.C ? a.alpha * d[i] : 0.0f;
+                        const float gz = ga[i] * ad;
+                        dg[i] = ad * fmaf(b[k][i], w[i], c[i]);
+                        if (on) {
+                            sg[k][i] += dg[i];
+                            sw1[k][i] = fmaf(gz, b[k][i], sw1[k][i]);
+                            sc1[k][i] += gz;
+                        }
+                        g[k][i] = gz * w[i];
+                        m1 = fmaf(g[k][i], b[k][i], m1);
+                        m0 += g[k][i];
+                    }
+                    if (each && on && a.ggate) {
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            if (col + i < a.C) as_global_mut<float>(a.ggate)[r * a.C + col + i] = dg[i];
+                    }
+                }
+            }
+            if (a.branch) {
+                row_sum<TPR>(m1, m0, mem, turn);
+                m1 *= inv;
+                m0 = a.layer ? m0 * inv : 0.0f;
+                if (on && a.gb) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        float d[E];
+#pragma unroll
+                        for (int i = 0; i < E; ++i) d[i] = st[1] * ((g[k][i] - m0) - b[k][i] * m1);
+                        store_row<T, E>(static_cast<T *>(a.gb) + r * a.C, (k * TPR + t) * E, a.C, a.vec, d);
+                    }
+                }
+            }
+        }
+        if (a.gate_sum) {
+            flush(sg, a.gate_part + unit * a.C);
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) sg[k][i] = 0.0f;
+        }
+    }
+    float *dst = a.part + static_cast<int64_t>(blockIdx.x) * 4 * a.C;
+    if (a.gw1) flush(sw1, dst);
+    if (a.gc1) flush(sc1, dst + a.C);
+    if (a.gw2) flush(sw2, dst + 2 * a.C);
+    if (a.gc2) flush(sc2, dst + 3 * a.C);
+}
+
+// Column sums of the partial rows: 64 columns, 16 slices of the rows side by side, in order.
+// blockIdx.y: 0..3 the four parameters, 4 + g the gate row g.
+__global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a, int gates_first) {
+    __shared__ float part[16][64];
+    const int col = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    const int64_t which = static_cast<int64_t>(blockIdx.y) + gates_first;
+    const float *src;
+    float *dst;
+    int64_t n, step;
+    if (which < 4) {
+        dst = which == 0 ? a.gw1 : which == 1 ? a.gc1 : which == 2 ? a.gw2 : a.gc2;
+        src = a.part + which * a.C;
+        n = a.blocks;
+        step = 4 * static_cast<int64_t>(a.C);
+    } else {
+        dst = a.ggate + (which - 4) * a.C;
+        src = a.gate_part + (which - 4) * a.gate_parts * a.C;
+        n = a.gate_parts;
+        step = a.C;
+    }
+    if (!dst) return;                             // the whole workgroup
+    float s = 0.0f;
+    if (col < a.C)
+        for (int64_t i = slice; i < n; i += 16) s += as_global<float>(src)[i * step + col];
+    part[slice][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (slice == 0 && col < a.C) {
+        for (int q = 1; q < 16; ++q) s += part[q][threadIdx.x];
+        as_global_mut<float>(dst)[col] = s;
+    }
+}
+
+template <typename T, int TPR, int V>
+void run_fwd(const NormArgs &a, hipStream_t s) {
+    constexpr int kThreads = threads_of(TPR);
+    constexpr int kSlots = kThreads / TPR;
+    hipLaunchKernelGGL((norm_fwd_kernel<T, TPR, V>), dim3(static_cast<uint32_t>((a.rows + kSlots - 1) / kSlots)),
+                       dim3(kThreads), 0, s, a);
+}
+template <typename T, int TPR, int V>
+void run_bwd(const NormArgs &a, hipStream_t s) {
+    constexpr int kThreads = threads_of(TPR);
+    constexpr int kSlots = kThreads / TPR;
+    const size_t lds = kSlots > 1 ? static_cast<size_t>(kSlots) * a.C * 4 : 0;
+    if (a.blocks > 0)
+        hipLaunchKernelGGL((norm_bwd_kernel<T, TPR, V>), dim3(a.blocks), dim3(kThreads), lds, s, a);
+}
+
+// Threads of a row by its chunks of 16 bytes: one chunk a thread, so that the backward's five
+// column sums fit the registers, and two for rows that 1024 threads do not cover.
+template <typename T, bool BWD>
+void run_sized(const NormArgs &a, hipStream_t s) {
+    const int chunks = (a.C + Chunk<T>::kN - 1) / Chunk<T>::kN;
+#define REX_NORM(TPR, V)                      \
+    do {                                      \
+        if (BWD) run_bwd<T, TPR, V>(a, s);    \
+        else run_fwd<T, TPR, V>(a, s);        \
+        return;                               \
+    } while (0)
+    if (chunks <= 16) REX_NORM(16, 1);
+    if (chunks <= 32) REX_NORM(32, 1);
+    if (chunks <= 64) REX_NORM(64, 1);
+    if (chunks <= 128) REX_NORM(128, 1);
+    if (chunks <= 256) REX_NORM(256, 1);
+    if (chunks <= 512) REX_NORM(512, 1);
+    if (chunks <= 1024) REX_NORM(1024, 1);
+    if constexpr (sizeof(T) == 4) REX_NORM(1024, 2);
+#undef REX_NORM
+}
+
+}  // namespace
+
+int norm_slots(int dtype, int C) {
+    const int chunks = (C + (dtype == kBF16 ? 7 : 3)) / (dtype == kBF16 ? 8 : 4);
+    return chunks <= 16 ? 16 : chunks <= 32 ? 8 : chunks <= 64 ? 4 : chunks <= 128 ? 2 : 1;
+}
+
+hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s) {
+    if (dtype == kBF16) run_sized<uint16_t, false>(a, s);
+    else run_sized<float, false>(a, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s) {
+    if (dtype == kBF16) run_sized<uint16_t, true>(a, s);
+    else run_sized<float, true>(a, s);
+    const int cols = (a.C + 63) / 64;
+    const bool params = a.gw1 || a.gc1 || a.gw2 || a.gc2;
+    const bool gates = a.gate_sum != 0;
+    // one launch for parameters and gate rows; more gate rows than a grid has go in turns
+    int64_t from = params ? 0 : 4, to = gates ? 4 + a.gates : 4;
+    for (; from < to; from += 65535)
+        hipLaunchKernelGGL(norm_columns_kernel,
+                           dim3(cols, static_cast<uint32_t>(to - from < 65535 ? to - from : 65535)),
+                           dim3(1024), 0, s, a, static_cast<int>(from));
+    return hipGetLastError();
+}
+
+}  // namespace rex

@@ -1,0 +1,120 @@
+// relation.hpp -- argument blocks and launchers of the relation head's kernels, shared by
+// the host API (relation_api.hip) and the kernel translation units.
+#pragma once
+
+#include "common.hpp"
+
+namespace rex {
+
+constexpr int kTile = 32;          // keys of one step of the attention, boxes of one page
+constexpr int kAttnWaves = 8;      // waves of one attention workgroup
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// One side's rows: [batch][row][head][channel], strides in bytes.
+struct Rows {
+    const void *p;
+    int64_t sb;
+    uint32_t sr, sh;
+};
+
+// The bucket rule of box_relation.h on the bits of |r|: m = (bits >> shift) - base + 1,
+// clamped to [0, half].
+struct BucketRule {
+    int32_t nb, half, shift, base;
+};
+
+struct AttnArgs {
+    Rows q, k, v;
+    const float *qbox, *kbox;           // element strides of batch and row below
+    int64_t qbox_sb, qbox_sr, kbox_sb, kbox_sr;
+    const float *bias;                  // [H][nb * nb] or null
+    const int32_t *qlen, *klen;
+    const uint8_t *kmask;
+    BucketRule rule;
+    float scale;                        // of the logits, natural
+    int32_t B, Nq, Nk, H, Hkv, D;
+    int32_t group;                      // H / Hkv
+    // the paged memory (k and v then unused)
+    const int8_t *mk, *mv;
+    const float *mks, *mvs, *mbox;
+    const int32_t *pages;
+    int64_t num_pages;
+    int32_t max_pages;
+    // forward
+    void *out;
+    float *out_f32, *lse;
+    int32_t terms;                      // parts of the weights that multiply bf16 data (add_weighted)
+    float *part, *part_ml;              // nsplit > 1: partial sums [nsplit][B][H][Nq][D], [..][2]
+    int32_t nsplit;
+    // how a workgroup's waves are shared out: heads x parts of the streamed side
+    int32_t hp, parts;
+    int32_t tiles;                      // column tiles of one image
+    int32_t nwg;
+    // backward
+    Rows gout;                          // grad_out, dense
+    const void *fout;                   // what the forward wrote
+    const float *fout_f32, *flse;
+    void *gq, *gk, *gv;
+    float *gbias;
+    float *rowstat;                     // [B][H][Nqp][2]: lse in units of log 2 (+inf: no row), delta
+    float *hist;                        // [B * spans][H][nb * nb]
+    int32_t Nqp;
+    int32_t span, spans;                // query tiles of one workgroup, runs of them per image
+    int32_t head_step;                  // heads of a group whose tables are in LDS together
+};
+
+hipError_t launch_attn_fwd(const AttnArgs &a, int dtype, int cols, hipStream_t s);
+hipError_t launch_attn_recall(const AttnArgs &a, int dtype, int cols, hipStream_t s);
+hipError_t launch_attn_combine(const AttnArgs &a, int dtype, hipStream_t s);
+hipError_t launch_attn_bwd(const AttnArgs &dq, const AttnArgs &dkv, int dtype, int dq_cols,
+                           int dkv_cols, hipStream_t s);
+
+struct MemoryArgs {
+    int8_t *k8, *v8;
+    float *ks, *vs, *mbox;
+    int64_t num_slots;
+    int32_t Hkv, D;
+    const int64_t *slots;
+    int64_t count;
+    const void *k, *v;                  // append: element strides of row and head
+    int64_t k_sr, k_sh, v_sr, v_sh;
+    const float *boxes;
+    int32_t vec;                        // append: rows can be read 16 bytes at a time
+    void *k_out, *v_out;                // read
+    float *boxes_out;
+};
+
+hipError_t launch_memory_append(const MemoryArgs &a, int dtype, hipStream_t s);
+hipError_t launch_memory_read(const MemoryArgs &a, int dtype, hipStream_t s);
+
+struct NormArgs {
+    const void *x, *branch;
+    int64_t x_stride, b_stride;
+    int64_t rows, rows_per_gate;
+    int32_t C;
+    int32_t layer;
+    float alpha, eps;
+    const float *gate, *w1, *c1, *w2, *c2;
+    void *y, *u;
+    float *stats;
+    int32_t second;                     // the second norm takes part
+    int32_t vec;                        // rows can be read and written 16 bytes at a time
+    // backward
+    const void *gy, *gu;
+    void *gx, *gb;
+    float *ggate, *gw1, *gc1, *gw2, *gc2;
+    float *part;                        // [blocks][4][C]: sums for gw1, gc1, gw2, gc2
+    float *gate_part;                   // [gates * gate_parts][C]
+    int32_t gate_sum;                   // ggate is the sum of gate_part's rows
+    // A unit is a run of rows of one gate row: unit i holds rows from
+    // (i / gate_parts) * span + (i % gate_parts) * unit_rows on, span rows per gate row.
+    int64_t units, span, gates;
+    int32_t gate_parts, unit_rows, blocks;
+};
+
+int norm_slots(int dtype, int C);   // rows a workgroup takes side by side
+hipError_t launch_norm_fwd(const NormArgs &a, int dtype, hipStream_t s);
+hipError_t launch_norm_bwd(const NormArgs &a, int dtype, hipStream_t s);
+
+}  // namespace rex
