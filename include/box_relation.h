@@ -40,9 +40,12 @@ extern "C" {
  *   s_ij = scale * q_i.k_j + bias[h][by(i,j)][bx(i,j)],  p_ij = exp(s_ij - lse_i),
  *   lse_i = log sum_j exp(s_ij),  out_i = sum_j p_ij v_j
  * over the visible keys: j < k_len[b] and k_mask[b][j] != 0.  A row without a visible key
- * (or whose every bias is -inf) has out = 0 and lse = -inf.  Rows i >= q_len[b] are padding:
+ * (or whose every bias is -inf, see below) has out = 0 and lse = -inf.  Rows i >= q_len[b] are padding:
  * out = 0, lse = -inf, nothing of them is used.  What masked keys and padding hold (NaN and
  * infinities included) has no effect on any result.
+ *
+ * An entry of bias at or below -1e30 (a type's lowest value, say) counts as -inf: its pairs
+ * are left out.
  *
  * The bucket of a pair says where the key's centre lies as seen from the query, in units of
  * the query's sides and by octaves: along x, every operation rounded to binary32,
@@ -62,7 +65,7 @@ typedef struct {
     /* element strides of batch, row and head, multiples of 16 bytes (channels are
      * adjacent); bases 16-byte aligned; the rows of one image span less than 2^31 bytes */
     int64_t q_stride[3], k_stride[3], v_stride[3];
-    float scale;              /* finite */
+    float scale;              /* finite, at least 1e-20 */
     int32_t buckets;          /* odd, in [1, RE_ATTN_MAX_BUCKETS]; 0 without bias */
     int32_t first_exp;        /* in [-64, 64] */
     int32_t octave_steps;     /* 1, 2 or 4 */

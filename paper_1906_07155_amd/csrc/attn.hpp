@@ -65,12 +65,16 @@ template <> struct Num<uint16_t> {    // bf16
         return f;
     }
     static constexpr bool kExact = false;     // round() cuts off
-    // x rounded, and x left with what that cut off
-    static __device__ __forceinline__ Frag round_off(float (&x)[8]) {
-        const Frag f = round(x);
+    // x cut to bf16 (toward zero: one operation, and the rest is exact), and x left with what
+    // that cut off
+    static __device__ __forceinline__ Frag cut_off(float (&x)[8]) {
+        u32x4 f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] -= static_cast<float>(f[j]);
-        return f;
+        for (int j = 0; j < 4; ++j)
+            f[j] = __builtin_amdgcn_perm(__float_as_uint(x[2 * j + 1]), __float_as_uint(x[2 * j]), 0x07060302u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] -= __uint_as_float(__float_as_uint(x[j]) & 0xffff0000u);
+        return __builtin_bit_cast(Frag, f);
     }
     // eight channels to memory
     static __device__ __forceinline__ void store(char *p, const float (&x)[8]) {
@@ -119,7 +123,7 @@ template <> struct Num<float> {
         return Frag{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
     }
     static constexpr bool kExact = true;
-    static __device__ __forceinline__ Frag round_off(float (&x)[8]) { return round(x); }
+    static __device__ __forceinline__ Frag cut_off(float (&x)[8]) { return round(x); }
     static __device__ __forceinline__ void store(char *p, const float (&x)[8]) {
         *(REX_GLOBAL f32x4 *)(p) = f32x4{x[0], x[1], x[2], x[3]};
         *(REX_GLOBAL f32x4 *)(p + 16) = f32x4{x[4], x[5], x[6], x[7]};
@@ -130,15 +134,15 @@ template <> struct Num<float> {
     }
 };
 
-// acc += A x for weights x of which bf16 keeps the first TERMS rounded parts: 1 rounds them
-// once, 2 leaves up to 2^-16 of them out, 3 nothing that binary32 sums would keep.
+// acc += A x for weights x of which bf16 takes the first TERMS parts of eight bits: 1 rounds
+// them, 2 leaves up to 2^-16 of them out, 3 nothing.
 template <typename T, int TERMS, int NT>
 __device__ __forceinline__ void add_weighted(const typename Num<T>::Frag (&rows)[NT], float (&x)[8],
                                              f32x4 (&acc)[NT]) {
     using N = Num<T>;
 #pragma unroll
     for (int i = 0; i < (N::kExact ? 1 : TERMS); ++i) {
-        const typename N::Frag f = i + 1 < TERMS ? N::round_off(x) : N::round(x);
+        const typename N::Frag f = i + 1 < TERMS ? N::cut_off(x) : N::round(x);
 #pragma unroll
         for (int k = 0; k < NT; ++k) acc[k] = N::mma(rows[k], f, acc[k]);
     }
@@ -225,11 +229,43 @@ __device__ __forceinline__ uint32_t pair_bucket(const BoxGeo &q, float kx, float
     return static_cast<uint32_t>(((by + b.half) * b.nb + bx + b.half) * 4);
 }
 
+// An entry of a head's table in LDS, so that it can be what a logit's sum starts with: in
+// units of the plain products (divided by the scale).  Masks written as a type's lowest
+// value count as -inf: kept as numbers they would drown the logits they are added to.
+__device__ __forceinline__ float table_entry(float bias, float scale) {
+    return bias <= -1e30f ? -kInf : bias / scale;
+}
+
+// The table entries of a lane's four rows: `at` holds four 16-bit byte offsets, `tab` (an LDS
+// address below 2^16) the head's table.
+__device__ __forceinline__ f32x4 table_gather(u32x2 at, const char *tab) {
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t off = i & 1 ? at[i >> 1] >> 16 : at[i >> 1] & 0xffffu;
+        v[i] = *reinterpret_cast<const float *>(tab + off);
+    }
+    return v;
+}
+
 constexpr int kBuckStride = 36;   // 16-bit entries of one column's 32 rows in LDS (8-byte reads
                                   // of 16 columns then start in 16 different bank pairs)
 
-// Workgroup ids in runs per XCD: ids go to the eight XCDs in turn, so handing each of them
-// one run of neighbouring tiles keeps an image's keys in one L2.  n is a multiple of 8.
-__device__ __forceinline__ int xcd_run(int id, int n) { return (id & 7) * (n >> 3) + (id >> 3); }
+// Workgroups go to the eight XCDs in turn.  `per` workgroups that share keys (one image and
+// head group) belong on one XCD, whose L2 then holds those keys: such sets go to the XCDs in
+// turn where there are enough of them to spread the images' different lengths (16 ragged
+// images, 2 head groups: forward 1.25 times faster than runs of neighbouring images), else
+// each XCD gets a run of neighbouring workgroups.  The grid is `xcd_grid(sets * per, per)`.
+inline __host__ __device__ bool xcd_sets(int sets) { return sets >= 64 || (sets >= 8 && sets % 8 == 0); }
+inline __host__ __device__ int xcd_grid(int n, int per) {
+    const int sets = n / per;
+    return xcd_sets(sets) ? (sets + 7) / 8 * 8 * per : (n + 7) & ~7;
+}
+// Workgroup id -> [0, n), or n and more for those that are left over.
+__device__ __forceinline__ int xcd_order(int id, int n, int per) {
+    const int xcd = id & 7, slot = id >> 3;
+    if (xcd_sets(n / per)) return (xcd + 8 * (slot / per)) * per + slot % per;
+    return xcd * ((n + 7) >> 3) + slot;
+}
 
 }  // namespace rex

@@ -11,8 +11,10 @@
 // the pair matrix instead of five), which costs less than adding one side's gradient with
 // atomics, and every element is written once and in a fixed order.
 //
-// The bias gradient is a histogram of ds by bucket.  Each wave adds into a table of its own
-// in LDS: LDS serves a wave's additions in order, so the sums repeat bit for bit.
+// The bias gradient is a histogram of ds by bucket.  Each wave adds into tables of its own
+// in LDS: LDS serves a wave's additions in order, so the sums repeat bit for bit.  The tables
+// are binary64: an addition of 64 lanes to LDS takes 18 to 30 cycles of a CU there, 193 in
+// binary32 (measured, whatever the addresses).
 #include "attn.hpp"
 
 namespace rex {
@@ -64,24 +66,30 @@ inline __host__ __device__ int bwd_ahead(int parts) { return parts >= 4 ? 1 : 4 
 
 // LDS of the two passes, bytes.
 struct BwdLds {
-    int bias, hist, geo, buck, acc, total;
+    int bias, hist, copies, geo, buck, acc, total;
 };
+constexpr int kLdsBytes = 160 << 10;
 inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, int tables, int nb,
                                           bool bias, bool hist) {
     BwdLds l{};
     int at = 0;
     const int table = (nb * nb * 4 + 15) & ~15;
-    l.hist = at;
-    if (bias && hist) at += kAttnWaves * table;
     l.bias = at;
     if (bias) at += tables * table;
     l.geo = at;
     if (bias) at += cols * 16;
     l.buck = at;
     if (bias) at += 2 * bwd_ahead(parts) * parts * cols * kBuckStride * 2;
-    l.acc = l.bias;               // the end: only the histograms are still needed
-    const int end = l.acc + (parts > 1 ? hp * parts * cols * (dp + 4) * 4 : 0);
-    l.total = at > end ? at : end;
+    l.acc = 0;                    // the end: only the histograms are still needed
+    const int end = parts > 1 ? hp * parts * cols * (dp + 4) * 4 : 0;
+    if (end > at) at = end;
+    l.hist = at;
+    l.copies = 1;                 // copies of a wave's table: a power of two that fits
+    if (bias && hist) {
+        while (l.copies < 4 && at + kAttnWaves * nb * nb * 8 * 2 * l.copies <= kLdsBytes) l.copies *= 2;
+        at += (kAttnWaves * nb * nb * 8 * l.copies + 15) & ~15;
+    }
+    l.total = at;
     return l;
 }
 
@@ -92,7 +100,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     using Pair = typename N::Pair;
     constexpr int kCols = 16 * NS, kDP = 32 * DB;
     extern __shared__ char smem[];
-    const int id = xcd_run(blockIdx.x, gridDim.x);
+    const int id = xcd_order(blockIdx.x, a.nwg, a.per);
     if (id >= a.nwg) return;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -112,7 +120,10 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     const int all = (klen + kTile - 1) / kTile;
     BoxGeo *geo = reinterpret_cast<BoxGeo *>(smem + lds.geo);
     uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
-    char *hist = smem + lds.hist + wave * table;
+    // entry off / 4 of the lane's copy is at hist + off * 2 * copies
+    const int copies = lds.copies, log_copies = 32 - __builtin_clz(copies);
+    double *const tables = reinterpret_cast<double *>(smem + lds.hist) + wave * nb2 * copies;
+    char *hist = reinterpret_cast<char *>(tables + (n & (copies - 1)));
     const float sl2 = a.scale * kLog2e;
     const char *tab = smem + lds.bias + hw * table;
     uint32_t fcol[DB], pcol[DB];
@@ -124,7 +135,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
     const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
     if (BIAS) {
-        for (int i = lane; i < nb2; i += 64) reinterpret_cast<float *>(hist)[i] = 0.0f;
+        for (int i = lane; i < nb2 * copies; i += 64) tables[i] = 0.0;
     }
 
     auto fill_buckets = [&](int chunk, int t1) {
@@ -165,7 +176,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
             for (int i = lane; i < nb2; i += 64)
                 if (kw == 0)
                     reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] =
-                        as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i] * kLog2e;
+                        table_entry(as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i], a.scale);
             if (tid < kCols)
                 geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
                                                     min(q0 + tid, a.Nq - 1) * a.qbox_sr));
@@ -190,6 +201,19 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
                     on = on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
                 const uint32_t vis = static_cast<uint32_t>(__ballot(on));
                 const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+                u32x2 at[NS][2];
+                f32x4 sc[NS][2];
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        at[s][t] = u32x2{};
+                        sc[s][t] = f32x4{};
+                        if (BIAS) {
+                            at[s][t] = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
+                            sc[s][t] = table_gather(at[s][t], tab);
+                        }
+                    }
                 float x[NS][8];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -201,25 +225,33 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
                     }
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
-                        f32x4 sc = {}, dp = {};
+                        f32x4 dp = {};
 #pragma unroll
                         for (int k = 0; k < DB; ++k) {
-                            sc = N::mma(kf[k], q[s][k], sc);
+                            sc[s][t] = N::mma(kf[k], q[s][k], sc[s][t]);
                             dp = N::mma(vf[k], go[s][k], dp);
                         }
-                        u32x2 at = {};
-                        if (BIAS) at = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t off = i & 1 ? at[i >> 1] >> 16 : at[i >> 1] & 0xffffu;
-                            float v = sc[i] * sl2;
-                            if (BIAS) v = fmaf(sc[i], sl2, *reinterpret_cast<const float *>(tab + off));
-                            float ds = __builtin_amdgcn_exp2f(v - lse[s]) * (dp[i] - delta[s]);
-                            if (vis != 0xffffffffu) ds = (vis >> (16 * t + 4 * g + i)) & 1u ? ds : 0.0f;
-                            x[s][4 * t + i] = ds;
-                            if (BIAS) atomicAdd(reinterpret_cast<float *>(hist + off), ds);
-                        }
+                        for (int i = 0; i < 4; ++i)
+                            x[s][4 * t + i] = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -lse[s])) * (dp[i] - delta[s]);
                     }
+                }
+                if (vis != 0xffffffffu) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) x[s][j] = (vis >> slot_row(g, j)) & 1u ? x[s][j] : 0.0f;
+                }
+                // all additions of a tile in a row: reads of LDS would wait for those before them
+                if (BIAS) {
+#pragma unroll
+                    for (int s = 0; s < NS; ++s)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint32_t two = at[s][j >> 2][(j & 3) >> 1];
+                            const uint32_t off = j & 1 ? two >> 16 : two & 0xffffu;
+                            unsafeAtomicAdd(reinterpret_cast<double *>(hist + (off << log_copies)), static_cast<double>(x[s][j]));
+                        }
                 }
                 if (vis != 0xffffffffu) {
 #pragma unroll
@@ -286,10 +318,12 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
         __syncthreads();
         for (int e = tid; e < hp * nb2; e += kAttnWaves * 64) {
             const int w = e / nb2, i = e - w * nb2;
-            float sum = 0.0f;
-            for (int p = 0; p < parts; ++p)
-                sum += reinterpret_cast<const float *>(smem + lds.hist + (p * hp + w) * table)[i];
-            as_global_mut<float>(a.hist)[((static_cast<int64_t>(b) * a.spans + sp) * a.H + h0 + w) * nb2 + i] = sum;
+            double sum = 0.0;
+            for (int p = 0; p < parts; ++p) {
+                const double *t = reinterpret_cast<const double *>(smem + lds.hist) + ((p * hp + w) * nb2 + i) * copies;
+                for (int c = 0; c < copies; ++c) sum += t[c];
+            }
+            as_global_mut<float>(a.hist)[((static_cast<int64_t>(b) * a.spans + sp) * a.H + h0 + w) * nb2 + i] = static_cast<float>(sum);
         }
     }
 }
@@ -301,7 +335,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
     using Pair = typename N::Pair;
     constexpr int kCols = 16 * NS, kDP = 32 * DB;
     extern __shared__ char smem[];
-    const int id = xcd_run(blockIdx.x, gridDim.x);
+    const int id = xcd_order(blockIdx.x, a.nwg, a.per);
     if (id >= a.nwg) return;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -371,7 +405,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
             for (int c = 0; c < many; ++c)
                 for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
                     reinterpret_cast<float *>(smem + lds.bias + (hw * a.head_step + c) * table)[i] =
-                        as_global<float>(a.bias)[static_cast<int64_t>(kh * a.group + first + c) * nb2 + i] * kLog2e;
+                        table_entry(as_global<float>(a.bias)[static_cast<int64_t>(kh * a.group + first + c) * nb2 + i], a.scale);
             fill_buckets(0);
         }
         for (int chunk = 0; chunk < chunks; ++chunk) {
@@ -388,6 +422,13 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                     const char *tab = smem + lds.bias + (hw * a.head_step + c) * table;
                     const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
                     const float *stat = a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + tile * kTile) * 2;
+                    f32x4 sc[NS][2];
+#pragma unroll
+                    for (int s = 0; s < NS; ++s)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            sc[s][t] = BIAS ? table_gather(*reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t), tab)
+                                            : f32x4{};
                     float pr[NS][8], ds[NS][8];
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
@@ -403,20 +444,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                         const float delta[4] = {st0[1], st0[3], st1[1], st1[3]};
 #pragma unroll
                         for (int s = 0; s < NS; ++s) {
-                            f32x4 sc = {}, dp = {};
+                            f32x4 dp = {};
 #pragma unroll
                             for (int k = 0; k < DB; ++k) {
-                                sc = N::mma(qf[k], kf[s][k], sc);
+                                sc[s][t] = N::mma(qf[k], kf[s][k], sc[s][t]);
                                 dp = N::mma(gf[k], vf[s][k], dp);
                             }
-                            u32x2 at = {};
-                            if (BIAS) at = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const uint32_t off = i & 1 ? at[i >> 1] >> 16 : at[i >> 1] & 0xffffu;
-                                float v = sc[i] * sl2;
-                                if (BIAS) v = fmaf(sc[i], sl2, *reinterpret_cast<const float *>(tab + off));
-                                const float p = __builtin_amdgcn_exp2f(v - lse[i]);
+                                const float p = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -lse[i]));
                                 pr[s][4 * t + i] = p;
                                 ds[s][4 * t + i] = p * (dp[i] - delta[i]);
                             }
@@ -516,7 +552,7 @@ __global__ __launch_bounds__(1024) void attn_hist_kernel(AttnArgs a) {
 template <typename T, int DB, int NS, int TERMS>
 void run_pass(const AttnArgs &a, bool keys, hipStream_t s) {
     if (a.nwg == 0) return;
-    const dim3 grid((a.nwg + 7) & ~7), block(kAttnWaves * 64);
+    const dim3 grid(xcd_grid(a.nwg, a.per)), block(kAttnWaves * 64);
     const bool bias = a.bias != nullptr;
     const BwdLds lds = bwd_lds(16 * NS, 32 * DB, a.hp, a.parts, keys ? a.hp * a.head_step : a.hp,
                                a.rule.nb, bias, !keys);

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
     using Pair = typename N::Pair;
     constexpr int kCols = 16 * NS, kDP = 32 * DB;
     extern __shared__ char smem[];
-    const int id = xcd_run(blockIdx.x, gridDim.x);
+    const int id = xcd_order(blockIdx.x, a.nwg, a.per);
     if (id >= a.nwg) return;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         const int nb2 = a.rule.nb * a.rule.nb;
         float *t = reinterpret_cast<float *>(smem + lds.bias);
         gcptr<float> src = as_global<float>(a.bias + static_cast<int64_t>(h0) * nb2);
-        for (int i = tid; i < hp * nb2; i += kAttnWaves * 64) t[i] = src[i] * kLog2e;
+        for (int i = tid; i < hp * nb2; i += kAttnWaves * 64) t[i] = table_entry(src[i], a.scale);
         if (tid < kCols)
             geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
                                                 min(q0 + tid, a.Nq - 1) * a.qbox_sr));
@@ -103,8 +103,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         }
     }
 
-    // One tile's keys: the codes or numbers of the S product's operand, its page and the lane's
-    // mask byte, read one step ahead.
+    // One tile's keys and values, its page and the lane's mask byte, read one step ahead.
     const HeadRows kr = head_rows<T>(a.k, b, kh, PAGED ? 0 : klen, a.D);
     const HeadRows vr = head_rows<T>(a.v, b, kh, PAGED ? 0 : klen, a.D);
     const uint32_t koff = n * kr.sr, voff = 4 * g * vr.sr;
@@ -116,37 +115,59 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         for (int t = 0; t < 2; ++t)
             vcode[k][t] = 32 * k + 2 * n + t < a.D ? (32 * k + 2 * n + t) * kTile + 4 * g : kBufOOB;
     }
-    struct Keys {
-        Frag f[PAGED ? 1 : 2][PAGED ? 1 : DB];
-        u32x2 c[PAGED ? 2 : 1][PAGED ? DB : 1];
-        int page;
+    struct {
+        Frag f[PAGED ? 1 : 2][PAGED ? 1 : DB];           // keys
+        Pair p[PAGED ? 1 : DB][8];                       // values
+        u32x2 kc[PAGED ? 2 : 1][PAGED ? DB : 1];         // their codes and scales in the memory
+        uint32_t vc[PAGED ? DB : 1][2][2];
+        f32x4 ks[2], vs[2];
+        int64_t ph;
         bool on;
     } next;
     auto page_of = [&](int tile) -> int {
-        if (!PAGED) return tile;
         const int p = a.pages[static_cast<int64_t>(b) * a.max_pages + tile];
         return p >= 0 && p < a.num_pages ? p : -1;
     };
-    auto load_keys = [&](int tile, Keys &x) {
-        x.page = page_of(tile);
+    auto load_keys = [&](int tile) {
         const int key = tile * kTile + (lane & 31);
-        x.on = key < klen && x.page >= 0;
-        if (!PAGED && a.kmask)
-            x.on = x.on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
+        next.on = key < klen;
         if constexpr (PAGED) {
-            const int64_t ph = static_cast<int64_t>(max(x.page, 0)) * a.Hkv + kh;
-            const auto r = make_rsrc(a.mk + ph * kTile * a.D, kTile * a.D);
+            const int page = page_of(tile);
+            next.on = next.on && page >= 0;
+            next.ph = static_cast<int64_t>(max(page, 0)) * a.Hkv + kh;
+            const auto r = make_rsrc(a.mk + next.ph * kTile * a.D, kTile * a.D);
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
+                next.ks[t] = *(const REX_GLOBAL f32x4 *)(a.mks + next.ph * kTile + 16 * t + 4 * g);
 #pragma unroll
                 for (int k = 0; k < DB; ++k)
-                    x.c[t][k] = __builtin_amdgcn_raw_buffer_load_b64(r, kcode[k] + 16 * t * a.D, 0, 0);
+                    next.kc[t][k] = __builtin_amdgcn_raw_buffer_load_b64(r, kcode[k] + 16 * t * a.D, 0, 0);
+            }
         } else {
+            if (a.kmask)
+                next.on = next.on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
             const uint32_t off = tile * kTile * kr.sr + koff;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int k = 0; k < DB; ++k) x.f[t][k] = N::load(kr.r, off + 16 * t * kr.sr + fcol[k]);
+                for (int k = 0; k < DB; ++k) next.f[t][k] = N::load(kr.r, off + 16 * t * kr.sr + fcol[k]);
+        }
+    };
+    auto load_values = [&](int tile) {                   // after load_keys of the same tile
+        if constexpr (PAGED) {
+            const auto r = make_rsrc(a.mv + next.ph * kTile * a.D, kTile * a.D);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                next.vs[t] = *(const REX_GLOBAL f32x4 *)(a.mvs + next.ph * kTile + 16 * t + 4 * g);
+#pragma unroll
+            for (int k = 0; k < DB; ++k)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        next.vc[k][t][e] = __builtin_amdgcn_raw_buffer_load_b32(r, vcode[k][t] + 16 * e, 0, 0);
+        } else {
+            load_pairs<T, DB>(vr, tile * kTile * vr.sr + voff, pcol, next.p);
         }
     };
     // Buckets of the chunk's tiles against the workgroup's queries, by the waves that read them.
@@ -156,7 +177,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
             const int tile = t0 + (chunk * ahead + i) * parts + kw;
             if (tile >= t1) return;
             const float *box;
-            if (PAGED) box = a.mbox + (static_cast<int64_t>(max(page_of(tile), 0)) * kTile + r) * 4;
+            if constexpr (PAGED) box = a.mbox + (static_cast<int64_t>(max(page_of(tile), 0)) * kTile + r) * 4;
             else box = a.kbox + b * a.kbox_sb + min(tile * kTile + r, a.Nk - 1) * a.kbox_sr;
             float kx, ky;
             box_centre(as_global<float>(box), kx, ky);
@@ -169,14 +190,20 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
     const float sl2 = a.scale * kLog2e;
     const char *tab = smem + lds.bias + hw * a.rule.nb * a.rule.nb * 4;
     f32x4 o[NS][2 * DB] = {};      // 16-channel tiles 2k, 2k + 1: even and odd channels
-    float m[NS], l[NS];
+    // The running maximum, in units of the products; what exponents are taken from (m in units
+    // of log 2, 0 while there is no key); the sum.
+    float m[NS], ref[NS], l[NS];
+    const float slack = 8.0f / sl2;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
         m[s] = -kInf;
-        l[s] = 0.0f;
+        ref[s] = l[s] = 0.0f;
     }
     const int steps = (t1 - t0 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
-    if (t0 + kw < t1) load_keys(t0 + kw, next);
+    if (t0 + kw < t1) {
+        load_keys(t0 + kw);
+        load_values(t0 + kw);
+    }
     if (BIAS) {
         __syncthreads();
         fill_buckets(0);
@@ -191,133 +218,124 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
             const int tile = t0 + (chunk * ahead + i) * parts + kw;
             if (tile >= t1) break;
             const uint32_t vis = static_cast<uint32_t>(__ballot(next.on));   // bit r: key r is visible
-            const int page = next.page;
-            Pair vp[PAGED ? 1 : DB][8];
-            uint32_t vc[PAGED ? DB : 1][2][2];
-            f32x4 ks[2], vs[2];
-            if constexpr (PAGED) {
-                const int64_t ph = static_cast<int64_t>(max(page, 0)) * a.Hkv + kh;
-                const auto r = make_rsrc(a.mv + ph * kTile * a.D, kTile * a.D);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    ks[t] = *(const REX_GLOBAL f32x4 *)(a.mks + ph * kTile + 16 * t + 4 * g);
-                    vs[t] = *(const REX_GLOBAL f32x4 *)(a.mvs + ph * kTile + 16 * t + 4 * g);
-                }
-#pragma unroll
-                for (int k = 0; k < DB; ++k)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            vc[k][t][e] = __builtin_amdgcn_raw_buffer_load_b32(r, vcode[k][t] + 16 * e, 0, 0);
-            } else {
-                load_pairs<T, DB>(vr, tile * kTile * vr.sr + voff, pcol, vp);
-            }
-
-            // logits in units of log 2: column = query n, rows = keys 4g + i of two tiles
-            float x[NS][8];
+            const bool more = tile + parts < t1;
+            // what a logit starts with: its bias, or nothing
+            f32x4 x[NS][2];
             const uint16_t *bk = buck + ((((chunk & 1) * ahead + i) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    x[s][t] = BIAS ? table_gather(*reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t), tab)
+                                   : f32x4{};
+            // column = query n, rows = keys 4g + e of two tiles
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 Frag kf[DB];
 #pragma unroll
                 for (int k = 0; k < DB; ++k) {
                     if constexpr (PAGED) {
-                        N::widen(kf[k], 0, next.c[t][k][0]);
-                        N::widen(kf[k], 4, next.c[t][k][1]);
+                        N::widen(kf[k], 0, next.kc[t][k][0]);
+                        N::widen(kf[k], 4, next.kc[t][k][1]);
                     } else {
                         kf[k] = next.f[t][k];
                     }
                 }
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
-                    f32x4 acc = {};
+                    if constexpr (PAGED) {
+                        f32x4 acc = {};
 #pragma unroll
-                    for (int k = 0; k < DB; ++k) acc = N::mma(kf[k], q[s][k], acc);
-                    u32x2 at = {};
-                    if (BIAS) at = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
+                        for (int k = 0; k < DB; ++k) acc = N::mma(kf[k], q[s][k], acc);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float f = PAGED ? sl2 * ks[t][e] : sl2;
-                        if (BIAS) {
-                            const uint32_t off = e & 1 ? at[e >> 1] >> 16 : at[e >> 1] & 0xffffu;
-                            x[s][4 * t + e] = fmaf(acc[e], f, *reinterpret_cast<const float *>(tab + off));
-                        } else {
-                            x[s][4 * t + e] = acc[e] * f;
-                        }
+                        for (int e = 0; e < 4; ++e) x[s][t][e] = fmaf(acc[e], next.ks[t][e], x[s][t][e]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < DB; ++k) x[s][t] = N::mma(kf[k], q[s][k], x[s][t]);
                     }
                 }
             }
-            if (tile + parts < t1) load_keys(tile + parts, next);
-            if (vis == 0) continue;
+            Frag vf[2 * DB];
+            f32x4 vs[2];
+            if constexpr (PAGED) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) vs[t] = next.vs[t];
+#pragma unroll
+                for (int k = 0; k < DB; ++k)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        N::widen(vf[2 * k + t], 0, next.vc[k][t][0]);
+                        N::widen(vf[2 * k + t], 4, next.vc[k][t][1]);
+                    }
+            }
             if (vis != 0xffffffffu) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const bool on = (vis >> slot_row(g, j)) & 1u;
 #pragma unroll
-                    for (int s = 0; s < NS; ++s) x[s][j] = on ? x[s][j] : -kInf;
+                    for (int s = 0; s < NS; ++s) x[s][j >> 2][j & 3] = on ? x[s][j >> 2][j & 3] : -kInf;
                     if constexpr (PAGED) {
                         vs[j >> 2][j & 3] = on ? vs[j >> 2][j & 3] : 0.0f;
                     } else {
 #pragma unroll
-                        for (int k = 0; k < DB; ++k) vp[k][j] = on ? vp[k][j] : N::no_pair();
+                        for (int k = 0; k < DB; ++k) next.p[k][j] = on ? next.p[k][j] : N::no_pair();
                     }
                 }
             }
+            if constexpr (!PAGED) {
+#pragma unroll
+                for (int k = 0; k < DB; ++k) N::split(next.p[k], vf[2 * k], vf[2 * k + 1]);
+            }
+            if (more) {
+                load_keys(tile + parts);
+                load_values(tile + parts);
+            }
+            if (vis == 0) continue;
             // The reference of the exponentials follows the maximum only when a logit has passed
-            // it by more than 8: sums stay below 2^8 * keys, and most steps neither rescale
-            // nor look for the maximum across lanes.
+            // it by more than 8 (of log 2): sums stay below 2^8 * keys, and most steps neither
+            // rescale nor look for the maximum across lanes.
             bool grew = false;
             float top[NS];
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                top[s] = x[s][0];
+                top[s] = x[s][0][0];
 #pragma unroll
-                for (int j = 1; j < 8; ++j) top[s] = fmaxf(top[s], x[s][j]);
-                grew |= top[s] > m[s] + 8.0f;
+                for (int j = 1; j < 8; ++j) top[s] = fmaxf(top[s], x[s][j >> 2][j & 3]);
+                grew |= top[s] > m[s] + slack;
             }
             if (__any(grew)) {
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const float mn = fmaxf(m[s], max_over_rows(top[s]));
-                    const float f = __builtin_amdgcn_exp2f(m[s] - (mn == -kInf ? 0.0f : mn));
+                    const float f = __builtin_amdgcn_exp2f((m[s] - (mn == -kInf ? 0.0f : mn)) * sl2);
                     m[s] = mn;
+                    ref[s] = mn == -kInf ? 0.0f : mn * sl2;
                     l[s] *= f;
 #pragma unroll
                     for (int k = 0; k < 2 * DB; ++k) o[s][k] *= f;
                 }
             }
+            float p[NS][8];
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                const float ref = m[s] == -kInf ? 0.0f : m[s];
                 float sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    x[s][j] = __builtin_amdgcn_exp2f(x[s][j] - ref);
-                    sum += x[s][j];
-                    if (PAGED) x[s][j] *= vs[j >> 2][j & 3];
+                    p[s][j] = __builtin_amdgcn_exp2f(fmaf(x[s][j >> 2][j & 3], sl2, -ref[s]));
+                    sum += p[s][j];
+                    if constexpr (PAGED) p[s][j] *= vs[j >> 2][j & 3];
                 }
                 l[s] += sum;
             }
-            Frag vf[2 * DB];
 #pragma unroll
-            for (int k = 0; k < DB; ++k) {
-                if constexpr (PAGED) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        N::widen(vf[2 * k + t], 0, vc[k][t][0]);
-                        N::widen(vf[2 * k + t], 4, vc[k][t][1]);
-                    }
-                } else {
-                    N::split(vp[k], vf[2 * k], vf[2 * k + 1]);
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(vf, x[s], o[s]);
+            for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(vf, p[s], o[s]);
         }
     }
 #pragma unroll
-    for (int s = 0; s < NS; ++s) l[s] = sum_over_rows(l[s]);
+    for (int s = 0; s < NS; ++s) {
+        l[s] = sum_over_rows(l[s]);
+        m[s] = m[s] == -kInf ? -kInf : ref[s];       // from here on in units of log 2
+    }
 
     // eight channels of one row, scaled, to where they belong
     auto finish = [&](int col, int head, int ch, float mx, float sum, const float (&x)[8]) {
@@ -401,7 +419,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
 // than 64 channels, whose sums would fill the registers.
 template <typename T, int DB, int NS, bool PAGED, int TERMS>
 void run_fwd(const AttnArgs &a, hipStream_t s) {
-    const dim3 grid((a.nwg + 7) & ~7), block(kAttnWaves * 64);
+    const dim3 grid(xcd_grid(a.nwg, a.per)), block(kAttnWaves * 64);
     const FwdLds lds = fwd_lds(16 * NS, 32 * DB, a.hp, a.parts, a.rule.nb, a.bias != nullptr);
     if (a.bias)
         hipLaunchKernelGGL((attn_fwd_kernel<T, DB, NS, true, PAGED, TERMS>), grid, block, lds.total, s, a);

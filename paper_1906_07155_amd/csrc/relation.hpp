@@ -50,7 +50,7 @@ struct AttnArgs {
     // how a workgroup's waves are shared out: heads x parts of the streamed side
     int32_t hp, parts;
     int32_t tiles;                      // column tiles of one image
-    int32_t nwg;
+    int32_t nwg, per;                   // workgroups, and those of them that share keys
     // backward
     Rows gout;                          // grad_out, dense
     const void *fout;                   // what the forward wrote

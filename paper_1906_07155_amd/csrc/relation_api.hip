@@ -55,7 +55,7 @@ re_status_t check_shape(int64_t batch, int64_t nq, int64_t nk, int32_t heads, in
     if (heads < 1 || kv_heads < 1 || heads > RE_ATTN_MAX_HEADS || heads % kv_heads != 0)
         return RE_ERR_INVALID_ARG;
     if (dim < 8 || dim > RE_ATTN_MAX_DIM || dim % 8 != 0) return RE_ERR_INVALID_ARG;
-    if (!std::isfinite(scale)) return RE_ERR_INVALID_ARG;
+    if (!std::isfinite(scale) || !(scale >= 1e-20f)) return RE_ERR_INVALID_ARG;
     if (nq > kMaxRows || nk > kMaxRows || batch > kMaxRowHeads) return RE_ERR_UNSUPPORTED;
     if (double(batch) * heads * double(std::max(nq, nk) + kTile) > double(kMaxRowHeads))
         return RE_ERR_UNSUPPORTED;
@@ -122,6 +122,7 @@ void plan_fwd(AttnArgs &a, int *cols) {
     n = std::min(n, streamed / (4 * a.parts));
     a.nsplit = static_cast<int32_t>(std::max<int64_t>(1, wgs < kFill ? n : 1));
     a.nwg = static_cast<int32_t>(wgs * a.nsplit);
+    a.per = a.tiles * a.nsplit;
 }
 
 size_t fwd_bytes(const AttnArgs &a) {
@@ -150,12 +151,14 @@ void plan_bwd(const AttnArgs &a, AttnArgs *dq, AttnArgs *dkv, int *dq_cols, int 
     const int64_t dq_blocks = static_cast<int64_t>(a.B) * dq->spans;
     share_waves(*dq, a.H, dq_blocks, (a.Nk + kTile - 1) / kTile);
     dq->nwg = static_cast<int32_t>(dq_blocks * (a.H / dq->hp));
+    dq->per = dq->spans;
 
     *dkv_cols = columns(a.Nk, a.D);
     dkv->tiles = (a.Nk + *dkv_cols - 1) / *dkv_cols;
     const int64_t blocks = static_cast<int64_t>(a.B) * dkv->tiles;
     share_waves(*dkv, a.Hkv, blocks, (a.Nq + kTile - 1) / kTile);
     dkv->nwg = static_cast<int32_t>(blocks * (a.Hkv / dkv->hp));
+    dkv->per = dkv->tiles;
     // the tables of a group's heads that share 24 KiB of LDS
     const int table = std::max(16, a.rule.nb * a.rule.nb * 4);
     dkv->head_step = std::min(a.group, std::max(1, (24 << 10) / (table * dkv->hp)));
