@@ -37,11 +37,11 @@ template <> struct Num<uint16_t> {    // bf16
     static __device__ __forceinline__ Frag load(const char *p) {
         return *(const REX_GLOBAL Frag *)(p);
     }
-    static __device__ __forceinline__ Frag load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-        return __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+    static __device__ __forceinline__ Frag load(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t soff) {
+        return __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(r, off, soff, 0));
     }
-    static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-        return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+    static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t soff) {
+        return __builtin_amdgcn_raw_buffer_load_b32(r, off, soff, 0);
     }
     static __device__ __forceinline__ Pair no_pair() { return 0u; }
     static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
@@ -98,13 +98,13 @@ template <> struct Num<float> {
         const f32x4 b = *(const REX_GLOBAL f32x4 *)(p + 16);
         return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     }
-    static __device__ __forceinline__ Frag load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-        const f32x4 a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
-        const f32x4 b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16, 0, 0));
+    static __device__ __forceinline__ Frag load(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t soff) {
+        const f32x4 a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, soff, 0));
+        const f32x4 b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16, soff, 0));
         return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     }
-    static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-        return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+    static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t soff) {
+        return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, soff, 0));
     }
     static __device__ __forceinline__ Pair no_pair() { return Pair{}; }
     static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
@@ -148,43 +148,69 @@ __device__ __forceinline__ void add_weighted(const typename Num<T>::Frag (&rows)
     }
 }
 
-// The first `rows` rows of one head of one image, read through a buffer resource: a lane's
-// 32-bit offset past the last of them (or marked kBufOOB: channels past D) reads 0 without
-// an access, so tiles may run over the end and padding is never read.  The host checks that (rows + 32) * stride stays
-// below kBufMaxBytes, so no offset wraps.
+// The first `rows` rows of one head of one image, read through a buffer resource that starts
+// at a tile's first row: a lane's 32-bit offset past the last row (or marked kBufOOB:
+// channels past D) reads 0 without an access, so tiles may run over the end and padding is
+// never read, and the lane offsets are the same for every tile.  The host checks that
+// (rows + 32) * stride stays below kBufMaxBytes, so no offset wraps.
 struct HeadRows {
-    __amdgpu_buffer_rsrc_t r;
-    uint32_t sr;              // bytes from row to row
+    const char *base;
+    uint32_t bytes, sr;       // bytes that may be read; from row to row
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(int row) const {   // row < rows, uniform
+        const uint32_t skip = static_cast<uint32_t>(row) * sr;
+        return make_rsrc(base + skip, bytes - skip);
+    }
 };
 template <typename T>
 __device__ __forceinline__ HeadRows head_rows(const Rows &x, int b, int head, int rows, int D) {
     const char *base = static_cast<const char *>(x.p) + b * x.sb + static_cast<int64_t>(head) * x.sh;
     const uint32_t bytes = rows > 0 ? static_cast<uint32_t>(rows - 1) * x.sr + D * Num<T>::kSize : 0u;
-    return HeadRows{make_rsrc(base, bytes), x.sr};
+    return HeadRows{base, bytes, x.sr};
 }
-// Lane offsets inside a row: of the operand whose rows are rows (channels 32k + 8g ..), and
-// of the one whose rows are channels (32k + 2n and the next), marked where past D.
-template <typename T>
-__device__ __forceinline__ uint32_t frag_col(int k, int g, int D) {
-    const int ch = 32 * k + 8 * g;
-    return ch < D ? static_cast<uint32_t>(ch * Num<T>::kSize) : kBufOOB;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t pair_col(int k, int n, int D) {
-    const int ch = 32 * k + 2 * n;
-    return ch < D ? static_cast<uint32_t>(ch * Num<T>::kSize) : kBufOOB;
-}
-// The transposed operand of 32 rows from row `first` on: 2 * DB tiles of 16 channels.
+// Lane offsets in a tile of 32 rows.  f: of the operand whose rows are rows (n and 16 + n,
+// channels 32k + 8g ..); p: of the one whose rows are channels (32k + 2n and the next, of
+// the rows slot_row(g, j)).
 template <typename T, int DB>
-__device__ __forceinline__ void load_pairs(const HeadRows &h, uint32_t off0, const uint32_t (&col)[DB],
-                                           typename Num<T>::Pair (&x)[DB][8]) {
+struct TileOffsets {
+    uint32_t f[DB], p[DB], sr;
+    __device__ __forceinline__ TileOffsets(uint32_t sr_, int n, int g, int D) : sr(sr_) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t off = off0 + (j < 4 ? j : 12 + j) * h.sr;      // + 4g rows, in off0
-#pragma unroll
-        for (int k = 0; k < DB; ++k) x[k][j] = Num<T>::load_pair(h.r, off + col[k]);
+        for (int k = 0; k < DB; ++k) {
+            f[k] = 32 * k + 8 * g < D ? n * sr + (32 * k + 8 * g) * Num<T>::kSize : kBufOOB;
+            p[k] = 32 * k + 2 * n < D ? 4 * g * sr + (32 * k + 2 * n) * Num<T>::kSize : kBufOOB;
+        }
     }
-}
+    // The rows' offsets go through the scalar register of the load where all 32 rows are there:
+    // the range check does not see it, and no lane register is needed for it.
+    __device__ __forceinline__ void frags(__amdgpu_buffer_rsrc_t r, bool inside,
+                                          typename Num<T>::Frag (&x)[2][DB]) const {
+        if (inside) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int k = 0; k < DB; ++k) x[t][k] = Num<T>::load(r, f[k], 16 * t * sr);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int k = 0; k < DB; ++k) x[t][k] = Num<T>::load(r, f[k] + 16 * t * sr, 0);
+        }
+    }
+    __device__ __forceinline__ void pairs(__amdgpu_buffer_rsrc_t r, bool inside,
+                                          typename Num<T>::Pair (&x)[DB][8]) const {
+        if (inside) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < DB; ++k) x[k][j] = Num<T>::load_pair(r, p[k], (j < 4 ? j : 12 + j) * sr);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < DB; ++k) x[k][j] = Num<T>::load_pair(r, p[k] + (j < 4 ? j : 12 + j) * sr, 0);
+        }
+    }
+};
 
 // Largest / sum over the four lanes that share a column (l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float max_over_rows(float x) {
@@ -214,19 +240,19 @@ __device__ __forceinline__ BoxGeo box_geo(const REX_GLOBAL float *b) {
     o.iy = 1.0f / fmaxf(b[3] - b[1], 1.0f);
     return o;
 }
-// Signed bucket of one axis in [-half, half].  The magnitude's edges are binary32 numbers
-// whose low bits are 0, so counting those reached is a shift of the bits of |r|.
+// Bucket of one axis, 0 .. 2 * half.  The magnitude's edges are binary32 numbers whose low
+// bits are 0, so counting those reached is a shift of the bits of |r|.
 __device__ __forceinline__ int axis_bucket(float r, const BucketRule &b) {
-    const int e = static_cast<int>((__float_as_uint(r) & 0x7fffffffu) >> b.shift) - b.base + 1;
-    const int m = min(max(e, 0), b.half);
-    return r < 0.0f ? -m : m;
+    const int e = static_cast<int>(__builtin_amdgcn_ubfe(__float_as_uint(r), b.shift, 31 - b.shift));
+    const int m = min(max(e, b.base - 1), b.base - 1 + b.half);        // edges reached + base - 1
+    return r < 0.0f ? b.half + b.base - 1 - m : m + (b.half - b.base + 1);
 }
 // Byte offset of a pair's entry in one head's table.
 __device__ __forceinline__ uint32_t pair_bucket(const BoxGeo &q, float kx, float ky,
                                                 const BucketRule &b) {
-    const int bx = axis_bucket((kx - q.cx) * q.ix, b);
-    const int by = axis_bucket((ky - q.cy) * q.iy, b);
-    return static_cast<uint32_t>(((by + b.half) * b.nb + bx + b.half) * 4);
+    const uint32_t bx = axis_bucket((kx - q.cx) * q.ix, b);
+    const uint32_t by = axis_bucket((ky - q.cy) * q.iy, b);
+    return __umul24(by, 4 * b.nb) + 4 * bx;
 }
 
 // An entry of a head's table in LDS, so that it can be what a logit's sum starts with: in

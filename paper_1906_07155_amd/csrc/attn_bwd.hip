@@ -2,9 +2,11 @@
 //
 //   rowstat   per (row, head): the row's log sum in units of log 2 (+inf where the row has no
 //             part), and delta = sum_c grad_out * out
-//   dq        query columns, keys streamed: grad_q and the bias gradient
+//   dq        query columns, keys streamed: grad_q, and for bf16 data delta again, as the sum
+//             of p dp in binary32.  `out` carries the rounding of the weights and its own, which
+//             is little in grad_q but would be the bias gradient's largest error (6e-4 of it)
 //   dkv       key columns, queries streamed, over the heads that share the key head: grad_k,
-//             grad_v
+//             grad_v and the bias gradient
 //   hist      the bias gradient's partial tables added up
 //
 // Both passes compute the weights again from q, k and the row's log sum (seven products of
@@ -20,7 +22,6 @@
 namespace rex {
 
 namespace {
-
 
 template <typename T>
 __global__ __launch_bounds__(256) void attn_rowstat_kernel(AttnArgs a) {
@@ -64,32 +65,32 @@ __global__ __launch_bounds__(256) void attn_rowstat_kernel(AttnArgs a) {
 // Steps whose buckets are computed between two barriers.
 inline __host__ __device__ int bwd_ahead(int parts) { return parts >= 4 ? 1 : 4 / parts; }
 
-// LDS of the two passes, bytes.
+// LDS of the two passes, bytes; `heads` tables of biases (and histograms) a wave.
 struct BwdLds {
     int bias, hist, copies, geo, buck, acc, total;
 };
 constexpr int kLdsBytes = 160 << 10;
-inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, int tables, int nb,
+inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, int heads, int nb,
                                           bool bias, bool hist) {
     BwdLds l{};
     int at = 0;
     const int table = (nb * nb * 4 + 15) & ~15;
     l.bias = at;
-    if (bias) at += tables * table;
+    if (bias) at += hp * heads * table;
     l.geo = at;
     if (bias) at += cols * 16;
     l.buck = at;
     if (bias) at += 2 * bwd_ahead(parts) * parts * cols * kBuckStride * 2;
-    l.acc = 0;                    // the end: only the histograms are still needed
-    const int end = parts > 1 ? hp * parts * cols * (dp + 4) * 4 : 0;
-    if (end > at) at = end;
     l.hist = at;
     l.copies = 1;                 // copies of a wave's table: a power of two that fits
     if (bias && hist) {
-        while (l.copies < 4 && at + kAttnWaves * nb * nb * 8 * 2 * l.copies <= kLdsBytes) l.copies *= 2;
-        at += (kAttnWaves * nb * nb * 8 * l.copies + 15) & ~15;
+        const int waves = kAttnWaves * heads * nb * nb * 8;
+        while (l.copies < 4 && at + 2 * l.copies * waves <= kLdsBytes) l.copies *= 2;
+        at += (l.copies * waves + 15) & ~15;
     }
-    l.total = at;
+    l.acc = 0;                    // the end: the tables are no longer needed
+    const int end = parts > 1 ? hp * parts * cols * (dp + 4) * 4 : 0;
+    l.total = at > end ? at : end;
     return l;
 }
 
@@ -106,39 +107,26 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hp = a.hp, parts = a.parts, hw = wave & (hp - 1), kw = wave / hp;
     int rest = id;
-    const int sp = rest % a.spans;
-    rest /= a.spans;
+    const int q0 = rest % a.tiles * kCols;
+    rest /= a.tiles;
     const int hgroups = a.H / hp;
     const int h0 = (rest % hgroups) * hp, b = rest / hgroups;
     const int h = h0 + hw, kh = h / a.group;
     const int nb2 = a.rule.nb * a.rule.nb, table = (nb2 * 4 + 15) & ~15;
     const int ahead = bwd_ahead(parts);
-    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, hp, a.rule.nb, BIAS, true);
+    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, 1, a.rule.nb, BIAS, false);
 
     const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
     const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
-    const int all = (klen + kTile - 1) / kTile;
+    const int t1 = q0 < qlen ? (klen + kTile - 1) / kTile : 0;
     BoxGeo *geo = reinterpret_cast<BoxGeo *>(smem + lds.geo);
     uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
-    // entry off / 4 of the lane's copy is at hist + off * 2 * copies
-    const int copies = lds.copies, log_copies = 32 - __builtin_clz(copies);
-    double *const tables = reinterpret_cast<double *>(smem + lds.hist) + wave * nb2 * copies;
-    char *hist = reinterpret_cast<char *>(tables + (n & (copies - 1)));
     const float sl2 = a.scale * kLog2e;
     const char *tab = smem + lds.bias + hw * table;
-    uint32_t fcol[DB], pcol[DB];
-#pragma unroll
-    for (int k = 0; k < DB; ++k) {
-        fcol[k] = frag_col<T>(k, g, a.D);
-        pcol[k] = pair_col<T>(k, n, a.D);
-    }
-    const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
     const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
-    if (BIAS) {
-        for (int i = lane; i < nb2 * copies; i += 64) tables[i] = 0.0;
-    }
+    const TileOffsets<T, DB> koff(kr.sr, n, g, a.D), voff(vr.sr, n, g, a.D);
 
-    auto fill_buckets = [&](int chunk, int t1) {
+    auto fill_buckets = [&](int chunk) {
         const int r = lane & 31;
         for (int i = 0; i < ahead; ++i) {
             const int tile = (chunk * ahead + i) * parts + kw;
@@ -147,184 +135,172 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
             box_centre(as_global<float>(a.kbox + b * a.kbox_sb + min(tile * kTile + r, a.Nk - 1) * a.kbox_sr),
                        kx, ky);
             uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
+#pragma unroll 2
             for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
                 dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(geo[c], kx, ky, a.rule));
         }
     };
 
-    const int last = min((sp + 1) * a.span, a.tiles);
-    for (int tile_q = sp * a.span; tile_q < last; ++tile_q) {
-        const int q0 = tile_q * kCols;
-        const int t1 = q0 < qlen ? all : 0;
-        Frag q[NS][DB], go[NS][DB];
-        float lse[NS], delta[NS];
+    Frag q[NS][DB], go[NS][DB];
+    float lse[NS], delta[NS], sum[NS];
+    {
+        const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
+        const TileOffsets<T, DB> qoff(qr.sr, n, g, a.D), goff(gr.sr, n, g, a.D);
+        const int first = min(q0, max(qlen - 1, 0));
+        const auto rq = qr.at(first), rg = gr.at(first);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            const int row = q0 + 16 * s + n;
 #pragma unroll
             for (int k = 0; k < DB; ++k) {
-                q[s][k] = N::load(qr.r, row * qr.sr + fcol[k]);
-                go[s][k] = N::load(gr.r, row * gr.sr + fcol[k]);
+                q[s][k] = N::load(rq, qoff.f[k] + 16 * s * qoff.sr, 0);
+                go[s][k] = N::load(rg, goff.f[k] + 16 * s * goff.sr, 0);
             }
             const f32x2 st = *(const REX_GLOBAL f32x2 *)(
-                a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + min(row, a.Nqp - 1)) * 2);
+                a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + min(q0 + 16 * s + n, a.Nqp - 1)) * 2);
             lse[s] = st[0];
             delta[s] = st[1];
+            sum[s] = 0.0f;
         }
+    }
+    if (BIAS) {
+        for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
+            reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] =
+                table_entry(as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i], a.scale);
+        if (tid < kCols)
+            geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb + min(q0 + tid, a.Nq - 1) * a.qbox_sr));
+        __syncthreads();
+        fill_buckets(0);
+    }
+    f32x4 dq[NS][2 * DB] = {};
+    const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
+    for (int chunk = 0; chunk < chunks; ++chunk) {
         if (BIAS) {
-            __syncthreads();          // the last tile's end has been read
-            for (int i = lane; i < nb2; i += 64)
-                if (kw == 0)
-                    reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] =
-                        table_entry(as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i], a.scale);
-            if (tid < kCols)
-                geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
-                                                    min(q0 + tid, a.Nq - 1) * a.qbox_sr));
             __syncthreads();
-            fill_buckets(0, t1);
+            if (chunk + 1 < chunks) fill_buckets(chunk + 1);
         }
-        f32x4 dq[NS][2 * DB] = {};
-        const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            if (BIAS) {
-                __syncthreads();
-                if (chunk + 1 < chunks) fill_buckets(chunk + 1, t1);
-            }
-            for (int it = 0; it < ahead; ++it) {
-                const int tile = (chunk * ahead + it) * parts + kw;
-                if (tile >= t1) break;
-                Pair kp[DB][8];
-                load_pairs<T, DB>(kr, (tile * kTile + 4 * g) * kr.sr, pcol, kp);
-                const int key = tile * kTile + (lane & 31);
-                bool on = key < klen;
-                if (a.kmask)
-                    on = on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
-                const uint32_t vis = static_cast<uint32_t>(__ballot(on));
-                const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
-                u32x2 at[NS][2];
-                f32x4 sc[NS][2];
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        at[s][t] = u32x2{};
-                        sc[s][t] = f32x4{};
-                        if (BIAS) {
-                            at[s][t] = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
-                            sc[s][t] = table_gather(at[s][t], tab);
-                        }
-                    }
-                float x[NS][8];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    Frag kf[DB], vf[DB];
-#pragma unroll
-                    for (int k = 0; k < DB; ++k) {
-                        kf[k] = N::load(kr.r, (tile * kTile + 16 * t + n) * kr.sr + fcol[k]);
-                        vf[k] = N::load(vr.r, (tile * kTile + 16 * t + n) * vr.sr + fcol[k]);
-                    }
-#pragma unroll
-                    for (int s = 0; s < NS; ++s) {
-                        f32x4 dp = {};
-#pragma unroll
-                        for (int k = 0; k < DB; ++k) {
-                            sc[s][t] = N::mma(kf[k], q[s][k], sc[s][t]);
-                            dp = N::mma(vf[k], go[s][k], dp);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            x[s][4 * t + i] = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -lse[s])) * (dp[i] - delta[s]);
-                    }
-                }
-                if (vis != 0xffffffffu) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-#pragma unroll
-                        for (int s = 0; s < NS; ++s) x[s][j] = (vis >> slot_row(g, j)) & 1u ? x[s][j] : 0.0f;
-                }
-                // all additions of a tile in a row: reads of LDS would wait for those before them
-                if (BIAS) {
-#pragma unroll
-                    for (int s = 0; s < NS; ++s)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const uint32_t two = at[s][j >> 2][(j & 3) >> 1];
-                            const uint32_t off = j & 1 ? two >> 16 : two & 0xffffu;
-                            unsafeAtomicAdd(reinterpret_cast<double *>(hist + (off << log_copies)), static_cast<double>(x[s][j]));
-                        }
-                }
-                if (vis != 0xffffffffu) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-#pragma unroll
-                        for (int k = 0; k < DB; ++k)
-                            kp[k][j] = (vis >> slot_row(g, j)) & 1u ? kp[k][j] : N::no_pair();
-                }
-                Frag kt[2 * DB];
-#pragma unroll
-                for (int k = 0; k < DB; ++k) N::split(kp[k], kt[2 * k], kt[2 * k + 1]);
-#pragma unroll
-                for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(kt, x[s], dq[s]);
-            }
-        }
-        auto finish = [&](int col, int head, int ch, const float (&x)[8]) {
-            const int row = q0 + col;
-            if (row >= a.Nq || ch >= a.D) return;
-            float y[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = row < qlen ? x[i] * a.scale : 0.0f;
-            N::store(static_cast<char *>(a.gq) +
-                         (((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch) * N::kSize, y);
-        };
-        if (parts == 1) {
+        for (int it = 0; it < ahead; ++it) {
+            const int tile = (chunk * ahead + it) * parts + kw;
+            if (tile >= t1) break;
+            const auto rk = kr.at(tile * kTile), rv = vr.at(tile * kTile);
+            const bool inside = tile * kTile + kTile <= klen;
+            Frag kf[2][DB], vf[2][DB];
+            koff.frags(rk, inside, kf);
+            voff.frags(rv, inside, vf);
+            Pair kp[DB][8];
+            koff.pairs(rk, inside, kp);
+            const int key = tile * kTile + (lane & 31);
+            bool on = key < klen;
+            if (a.kmask)
+                on = on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
+            const uint32_t vis = static_cast<uint32_t>(__ballot(on));
+            const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+            f32x4 sc[NS][2], dp[NS][2];
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
-                for (int k = 0; k < DB; ++k) {
-                    float y[8];
+                for (int t = 0; t < 2; ++t)
+                    sc[s][t] = BIAS ? table_gather(*reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t), tab)
+                                    : f32x4{};
+            float x[NS][8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = dq[s][2 * k + (i & 1)][i >> 1];
-                    finish(16 * s + n, h, 32 * k + 8 * g, y);
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    dp[s][t] = f32x4{};
+#pragma unroll
+                    for (int k = 0; k < DB; ++k) {
+                        sc[s][t] = N::mma(kf[t][k], q[s][k], sc[s][t]);
+                        dp[s][t] = N::mma(vf[t][k], go[s][k], dp[s][t]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -lse[s]));
+                        x[s][4 * t + i] = p * (dp[s][t][i] - delta[s]);
+                        dp[s][t][i] *= p;
+                    }
                 }
-            continue;
-        }
-        float *acc = reinterpret_cast<float *>(smem + lds.acc);
-        __syncthreads();
+            if (vis != 0xffffffffu) {
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+                for (int j = 0; j < 8; ++j) {
+                    const bool on_j = (vis >> slot_row(g, j)) & 1u;
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        x[s][j] = on_j ? x[s][j] : 0.0f;
+                        dp[s][j >> 2][j & 3] = on_j ? dp[s][j >> 2][j & 3] : 0.0f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < DB; ++k) kp[k][j] = on_j ? kp[k][j] : N::no_pair();
+                }
+            }
+            if (!N::kExact) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[s] += dp[s][j >> 2][j & 3];
+            }
+            Frag kt[2 * DB];
+#pragma unroll
+            for (int k = 0; k < DB; ++k) N::split(kp[k], kt[2 * k], kt[2 * k + 1]);
+#pragma unroll
+            for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(kt, x[s], dq[s]);
+        }
+    }
+    auto finish = [&](int col, int head, int ch, const float (&x)[8]) {
+        const int row = q0 + col;
+        if (row >= a.Nq || ch >= a.D) return;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = row < qlen ? x[i] * a.scale : 0.0f;
+        N::store(static_cast<char *>(a.gq) +
+                     (((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch) * N::kSize, y);
+    };
+    auto keep_delta = [&](int col, int head, float d) {
+        if (!N::kExact && q0 + col < qlen)
+            as_global_mut<float>(a.rowstat)[((static_cast<int64_t>(b) * a.H + head) * a.Nqp + q0 + col) * 2 + 1] = d;
+    };
+#pragma unroll
+    for (int s = 0; s < NS; ++s) sum[s] = sum_over_rows(sum[s]);
+    if (parts == 1) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            if (g == 0) keep_delta(16 * s + n, h, sum[s]);
 #pragma unroll
             for (int k = 0; k < DB; ++k) {
-                float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4) + 32 * k + 8 * g;
+                float y[8];
 #pragma unroll
-                for (int i = 0; i < 8; i += 4)
-                    *reinterpret_cast<f32x4 *>(dst + i) =
-                        f32x4{dq[s][2 * k][i >> 1], dq[s][2 * k + 1][i >> 1], dq[s][2 * k][(i >> 1) + 1],
-                              dq[s][2 * k + 1][(i >> 1) + 1]};
+                for (int i = 0; i < 8; ++i) y[i] = dq[s][2 * k + (i & 1)][i >> 1];
+                finish(16 * s + n, h, 32 * k + 8 * g, y);
             }
-        __syncthreads();
-        for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
-            const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
-            float y[8] = {};
-            for (int p = 0; p < parts; ++p) {
-                const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] += src[i];
-            }
-            finish(col, h0 + w, ch, y);
         }
-        __syncthreads();
+        return;
     }
-    if (BIAS) {
-        __syncthreads();
-        for (int e = tid; e < hp * nb2; e += kAttnWaves * 64) {
-            const int w = e / nb2, i = e - w * nb2;
-            double sum = 0.0;
-            for (int p = 0; p < parts; ++p) {
-                const double *t = reinterpret_cast<const double *>(smem + lds.hist) + ((p * hp + w) * nb2 + i) * copies;
-                for (int c = 0; c < copies; ++c) sum += t[c];
-            }
-            as_global_mut<float>(a.hist)[((static_cast<int64_t>(b) * a.spans + sp) * a.H + h0 + w) * nb2 + i] = static_cast<float>(sum);
+    // the parts' sums; the first of a row's four spare places holds its sum of p dp
+    float *acc = reinterpret_cast<float *>(smem + lds.acc);
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4);
+        if (g == 0) dst[kDP] = sum[s];
+#pragma unroll
+        for (int k = 0; k < DB; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; i += 4)
+                *reinterpret_cast<f32x4 *>(dst + 32 * k + 8 * g + i) =
+                    f32x4{dq[s][2 * k][i >> 1], dq[s][2 * k + 1][i >> 1], dq[s][2 * k][(i >> 1) + 1],
+                          dq[s][2 * k + 1][(i >> 1) + 1]};
+    }
+    __syncthreads();
+    for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
+        const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
+        float y[8] = {}, d = 0.0f;
+        for (int p = 0; p < parts; ++p) {
+            const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] += src[ch + i];
+            d += src[kDP];
         }
+        if (ch == 0) keep_delta(col, h0 + w, d);
+        finish(col, h0 + w, ch, y);
     }
 }
 
@@ -341,192 +317,253 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hp = a.hp, parts = a.parts, hw = wave & (hp - 1), kw = wave / hp;
     int rest = id;
-    const int tile_k = rest % a.tiles;
-    rest /= a.tiles;
+    const int sp = rest % a.spans;
+    rest /= a.spans;
     const int hgroups = a.Hkv / hp;
     const int kh0 = (rest % hgroups) * hp, b = rest / hgroups;
     const int kh = kh0 + hw;
     const int nb2 = a.rule.nb * a.rule.nb, table = (nb2 * 4 + 15) & ~15;
     const int ahead = bwd_ahead(parts);
-    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, hp * a.head_step, a.rule.nb, BIAS, false);
+    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, a.head_step, a.rule.nb, BIAS, true);
 
     const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
     const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
-    const int k0 = tile_k * kCols;
-    const int t1 = k0 < klen ? (qlen + kTile - 1) / kTile : 0;
     f32x2 *ctr = reinterpret_cast<f32x2 *>(smem + lds.geo);
     uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
     const float sl2 = a.scale * kLog2e;
-    uint32_t fcol[DB], pcol[DB];
-#pragma unroll
-    for (int k = 0; k < DB; ++k) {
-        fcol[k] = frag_col<T>(k, g, a.D);
-        pcol[k] = pair_col<T>(k, n, a.D);
-    }
+    // entry off / 4 of the lane's copy of table c is at hist + c * nb2 * 8 * copies + off * 2 * copies
+    const int copies = lds.copies, log_copies = 32 - __builtin_clz(copies);
+    double *const tables = reinterpret_cast<double *>(smem + lds.hist) + wave * a.head_step * nb2 * copies;
+    char *const hist = reinterpret_cast<char *>(tables + (n & (copies - 1)));
+    float *const partial = BIAS ? a.hist + (static_cast<int64_t>(b) * a.spans + sp) * a.H * nb2 : nullptr;
+    const TileOffsets<T, DB> qoff(a.q.sr, n, g, a.D), goff(a.gout.sr, n, g, a.D);
 
-    // The key columns.  A masked key's column is whatever its row makes of it: no other column
-    // sees it, and zeros are written for it at the end.
-    Frag kf[NS][DB], vf[NS][DB];
-    {
-        const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
+    const int first_tile = sp * a.span, last_tile = min(first_tile + a.span, a.tiles);
+    for (int tile_k = first_tile; tile_k < last_tile; ++tile_k) {
+        const int k0 = tile_k * kCols;
+        const int t1 = k0 < klen ? (qlen + kTile - 1) / kTile : 0;
+        // The key columns.  A masked key's column is whatever its row makes of it: its weights
+        // are set to 0 before they reach the histogram, no other column sees them, and zeros
+        // are written for it at the end.
+        Frag kf[NS][DB], vf[NS][DB];
+        bool live[NS];
+        {
+            const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
+            const TileOffsets<T, DB> koff(kr.sr, n, g, a.D), voff(vr.sr, n, g, a.D);
+            const int first = min(k0, max(klen - 1, 0));
+            const auto rk = kr.at(first), rv = vr.at(first);
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+            for (int s = 0; s < NS; ++s) {
+                const int key = k0 + 16 * s + n;
+                live[s] = key < klen;
+                if (a.kmask)
+                    live[s] = live[s] && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
 #pragma unroll
-            for (int k = 0; k < DB; ++k) {
-                kf[s][k] = N::load(kr.r, (k0 + 16 * s + n) * kr.sr + fcol[k]);
-                vf[s][k] = N::load(vr.r, (k0 + 16 * s + n) * vr.sr + fcol[k]);
+                for (int k = 0; k < DB; ++k) {
+                    kf[s][k] = N::load(rk, koff.f[k] + 16 * s * koff.sr, 0);
+                    vf[s][k] = N::load(rv, voff.f[k] + 16 * s * voff.sr, 0);
+                }
             }
-    }
-    if (BIAS && tid < kCols) {
-        float cx, cy;
-        box_centre(as_global<float>(a.kbox + b * a.kbox_sb + min(k0 + tid, a.Nk - 1) * a.kbox_sr), cx, cy);
-        ctr[tid] = f32x2{cx, cy};
-    }
-    // here the streamed side is the queries: row r of the tile is query 32 * tile + r
-    auto fill_buckets = [&](int chunk) {
-        const int r = lane & 31;
-        for (int i = 0; i < ahead; ++i) {
-            const int tile = (chunk * ahead + i) * parts + kw;
-            if (tile >= t1) return;
-            const BoxGeo q = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
-                                                      min(tile * kTile + r, a.Nq - 1) * a.qbox_sr));
-            uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
-            for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
-                dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(q, ctr[c][0], ctr[c][1], a.rule));
         }
-    };
-
-    f32x4 dk[NS][2 * DB] = {}, dv[NS][2 * DB] = {};
-    const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
-    for (int first = 0; first < a.group; first += a.head_step) {
-        const int many = min(a.head_step, a.group - first);
+        bool all_live = true;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) all_live = all_live && live[s];
+        const bool whole = __all(all_live);
         if (BIAS) {
-            __syncthreads();              // the tables of the last heads have been read
-            for (int c = 0; c < many; ++c)
-                for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
-                    reinterpret_cast<float *>(smem + lds.bias + (hw * a.head_step + c) * table)[i] =
-                        table_entry(as_global<float>(a.bias)[static_cast<int64_t>(kh * a.group + first + c) * nb2 + i], a.scale);
-            fill_buckets(0);
-        }
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            if (BIAS) {
-                __syncthreads();
-                if (chunk + 1 < chunks) fill_buckets(chunk + 1);
+            __syncthreads();              // the last tile's tables have been read
+            if (tid < kCols) {
+                float cx, cy;
+                box_centre(as_global<float>(a.kbox + b * a.kbox_sb + min(k0 + tid, a.Nk - 1) * a.kbox_sr), cx, cy);
+                ctr[tid] = f32x2{cx, cy};
             }
-            for (int it = 0; it < ahead; ++it) {
-                const int tile = (chunk * ahead + it) * parts + kw;
-                if (tile >= t1) break;
-                const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
-                for (int c = 0; c < many; ++c) {
-                    const int h = kh * a.group + first + c;
-                    const char *tab = smem + lds.bias + (hw * a.head_step + c) * table;
-                    const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
-                    const float *stat = a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + tile * kTile) * 2;
-                    f32x4 sc[NS][2];
+        }
+        // here the streamed side is the queries: row r of the tile is query 32 * tile + r
+        auto fill_buckets = [&](int chunk) {
+            const int r = lane & 31;
+            for (int i = 0; i < ahead; ++i) {
+                const int tile = (chunk * ahead + i) * parts + kw;
+                if (tile >= t1) return;
+                const BoxGeo q = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
+                                                          min(tile * kTile + r, a.Nq - 1) * a.qbox_sr));
+                uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
+#pragma unroll 2
+                for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
+                    dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(q, ctr[c][0], ctr[c][1], a.rule));
+            }
+        };
+
+        f32x4 dk[NS][2 * DB] = {}, dv[NS][2 * DB] = {};
+        const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
+        for (int first = 0; first < a.group; first += a.head_step) {
+            const int many = min(a.head_step, a.group - first);
+            if (BIAS) {
+                __syncthreads();          // the tables of the last heads have been read
+                for (int c = 0; c < many; ++c)
+                    for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
+                        reinterpret_cast<float *>(smem + lds.bias + (hw * a.head_step + c) * table)[i] =
+                            table_entry(as_global<float>(a.bias)[static_cast<int64_t>(kh * a.group + first + c) * nb2 + i], a.scale);
+                for (int i = lane; i < many * nb2 * copies; i += 64) tables[i] = 0.0;
+                fill_buckets(0);
+            }
+            for (int chunk = 0; chunk < chunks; ++chunk) {
+                if (BIAS) {
+                    __syncthreads();
+                    if (chunk + 1 < chunks) fill_buckets(chunk + 1);
+                }
+                for (int it = 0; it < ahead; ++it) {
+                    const int tile = (chunk * ahead + it) * parts + kw;
+                    if (tile >= t1) break;
+                    const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+                    for (int c = 0; c < many; ++c) {
+                        const int h = kh * a.group + first + c;
+                        const char *tab = smem + lds.bias + (hw * a.head_step + c) * table;
+                        const auto rq = head_rows<T>(a.q, b, h, qlen, a.D).at(tile * kTile);
+                        const auto rg = head_rows<T>(a.gout, b, h, qlen, a.D).at(tile * kTile);
+                        const float *stat = a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + tile * kTile) * 2;
+                        u32x2 at[NS][2];
+                        f32x4 sc[NS][2];
 #pragma unroll
-                    for (int s = 0; s < NS; ++s)
+                        for (int s = 0; s < NS; ++s)
 #pragma unroll
-                        for (int t = 0; t < 2; ++t)
-                            sc[s][t] = BIAS ? table_gather(*reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t), tab)
-                                            : f32x4{};
-                    float pr[NS][8], ds[NS][8];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        Frag qf[DB], gf[DB];
-#pragma unroll
-                        for (int k = 0; k < DB; ++k) {
-                            qf[k] = N::load(qr.r, (tile * kTile + 16 * t + n) * qr.sr + fcol[k]);
-                            gf[k] = N::load(gr.r, (tile * kTile + 16 * t + n) * gr.sr + fcol[k]);
-                        }
-                        const f32x4 st0 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2);
-                        const f32x4 st1 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2 + 4);
-                        const float lse[4] = {st0[0], st0[2], st1[0], st1[2]};
-                        const float delta[4] = {st0[1], st0[3], st1[1], st1[3]};
-#pragma unroll
-                        for (int s = 0; s < NS; ++s) {
-                            f32x4 dp = {};
-#pragma unroll
-                            for (int k = 0; k < DB; ++k) {
-                                sc[s][t] = N::mma(qf[k], kf[s][k], sc[s][t]);
-                                dp = N::mma(gf[k], vf[s][k], dp);
+                            for (int t = 0; t < 2; ++t) {
+                                at[s][t] = u32x2{};
+                                sc[s][t] = f32x4{};
+                                if (BIAS) {
+                                    at[s][t] = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
+                                    sc[s][t] = table_gather(at[s][t], tab);
+                                }
                             }
+                        const bool inside = tile * kTile + kTile <= qlen;
+                        Frag qf[2][DB], gf[2][DB];
+                        qoff.frags(rq, inside, qf);
+                        goff.frags(rg, inside, gf);
+                        float pr[NS][8], ds[NS][8];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float p = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -lse[i]));
-                                pr[s][4 * t + i] = p;
-                                ds[s][4 * t + i] = p * (dp[i] - delta[i]);
+                        for (int t = 0; t < 2; ++t) {
+                            const f32x4 st0 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2);
+                            const f32x4 st1 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2 + 4);
+                            const float lse[4] = {st0[0], st0[2], st1[0], st1[2]};
+                            const float delta[4] = {st0[1], st0[3], st1[1], st1[3]};
+#pragma unroll
+                            for (int s = 0; s < NS; ++s) {
+                                f32x4 dp = {};
+#pragma unroll
+                                for (int k = 0; k < DB; ++k) {
+                                    sc[s][t] = N::mma(qf[t][k], kf[s][k], sc[s][t]);
+                                    dp = N::mma(gf[t][k], vf[s][k], dp);
+                                }
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -lse[i]));
+                                    pr[s][4 * t + i] = p;
+                                    ds[s][4 * t + i] = p * (dp[i] - delta[i]);
+                                }
                             }
                         }
-                    }
+                        // all additions of a tile in a row: reads of LDS would wait for those
+                        // before them
+                        if (BIAS) {
+                            if (!whole) {
 #pragma unroll
-                    for (int which = 0; which < 2; ++which) {
-                        const HeadRows &r = which ? qr : gr;
-                        Pair p[DB][8];
-                        load_pairs<T, DB>(r, (tile * kTile + 4 * g) * r.sr, pcol, p);
-                        Frag rows[2 * DB];
+                                for (int s = 0; s < NS; ++s)
 #pragma unroll
-                        for (int k = 0; k < DB; ++k) N::split(p[k], rows[2 * k], rows[2 * k + 1]);
+                                    for (int j = 0; j < 8; ++j) ds[s][j] = live[s] ? ds[s][j] : 0.0f;
+                            }
+                            char *const to = hist + c * nb2 * 8 * copies;
 #pragma unroll
-                        for (int s = 0; s < NS; ++s) {
-                            if (which) add_weighted<T, TERMS, 2 * DB>(rows, ds[s], dk[s]);
-                            else add_weighted<T, TERMS, 2 * DB>(rows, pr[s], dv[s]);
+                            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    const uint32_t two = at[s][j >> 2][(j & 3) >> 1];
+                                    const uint32_t off = j & 1 ? two >> 16 : two & 0xffffu;
+                                    unsafeAtomicAdd(reinterpret_cast<double *>(to + (off << log_copies)),
+                                                    static_cast<double>(ds[s][j]));
+                                }
+                        }
+#pragma unroll
+                        for (int which = 0; which < 2; ++which) {
+                            Pair p[DB][8];
+                            if (which) qoff.pairs(rq, inside, p);
+                            else goff.pairs(rg, inside, p);
+                            Frag rows[2 * DB];
+#pragma unroll
+                            for (int k = 0; k < DB; ++k) N::split(p[k], rows[2 * k], rows[2 * k + 1]);
+#pragma unroll
+                            for (int s = 0; s < NS; ++s) {
+                                if (which) add_weighted<T, TERMS, 2 * DB>(rows, ds[s], dk[s]);
+                                else add_weighted<T, TERMS, 2 * DB>(rows, pr[s], dv[s]);
+                            }
                         }
                     }
                 }
             }
+            if (BIAS) {                   // this workgroup's own partial tables
+                __syncthreads();
+                for (int e = tid; e < hp * many * nb2; e += kAttnWaves * 64) {
+                    const int i = e % nb2, c = e / nb2 % many, w = e / (nb2 * many);
+                    double sum = 0.0;
+                    for (int p = 0; p < parts; ++p) {
+                        const double *t = reinterpret_cast<const double *>(smem + lds.hist) +
+                                          (((p * hp + w) * a.head_step + c) * nb2 + i) * copies;
+                        for (int x = 0; x < copies; ++x) sum += t[x];
+                    }
+                    gptr<float> dst = as_global_mut<float>(partial) + ((kh0 + w) * a.group + first + c) * nb2 + i;
+                    *dst = static_cast<float>(sum) + (tile_k > first_tile ? *dst : 0.0f);
+                }
+            }
         }
-    }
 
-    auto finish = [&](char *out, float f, int col, int head, int ch, const float (&x)[8]) {
-        const int key = k0 + col;
-        if (key >= a.Nk || ch >= a.D) return;
-        bool on = key < klen;
-        if (a.kmask && on) on = as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + key] != 0;
-        float y[8];
+        auto finish = [&](char *out, float f, int col, int head, int ch, const float (&x)[8]) {
+            const int key = k0 + col;
+            if (key >= a.Nk || ch >= a.D) return;
+            bool on = key < klen;
+            if (a.kmask && on) on = as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + key] != 0;
+            float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = on ? x[i] * f : 0.0f;
-        N::store(out + (((static_cast<int64_t>(b) * a.Nk + key) * a.Hkv + head) * a.D + ch) * N::kSize, y);
-    };
-    auto write = [&](const f32x4 (&d)[NS][2 * DB], char *out, float f) {
-        if (parts == 1) {
+            for (int i = 0; i < 8; ++i) y[i] = on ? x[i] * f : 0.0f;
+            N::store(out + (((static_cast<int64_t>(b) * a.Nk + key) * a.Hkv + head) * a.D + ch) * N::kSize, y);
+        };
+        auto write = [&](const f32x4 (&d)[NS][2 * DB], char *out, float f) {
+            if (parts == 1) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int k = 0; k < DB; ++k) {
+                        float y[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = d[s][2 * k + (i & 1)][i >> 1];
+                        finish(out, f, 16 * s + n, kh, 32 * k + 8 * g, y);
+                    }
+                return;
+            }
+            float *acc = reinterpret_cast<float *>(smem + lds.acc);
+            __syncthreads();
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
                 for (int k = 0; k < DB; ++k) {
-                    float y[8];
+                    float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4) + 32 * k + 8 * g;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = d[s][2 * k + (i & 1)][i >> 1];
-                    finish(out, f, 16 * s + n, kh, 32 * k + 8 * g, y);
+                    for (int i = 0; i < 8; i += 4)
+                        *reinterpret_cast<f32x4 *>(dst + i) =
+                            f32x4{d[s][2 * k][i >> 1], d[s][2 * k + 1][i >> 1], d[s][2 * k][(i >> 1) + 1],
+                                  d[s][2 * k + 1][(i >> 1) + 1]};
                 }
-            return;
-        }
-        float *acc = reinterpret_cast<float *>(smem + lds.acc);
-        __syncthreads();
+            __syncthreads();
+            for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
+                const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
+                float y[8] = {};
+                for (int p = 0; p < parts; ++p) {
+                    const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch;
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int k = 0; k < DB; ++k) {
-                float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4) + 32 * k + 8 * g;
-#pragma unroll
-                for (int i = 0; i < 8; i += 4)
-                    *reinterpret_cast<f32x4 *>(dst + i) =
-                        f32x4{d[s][2 * k][i >> 1], d[s][2 * k + 1][i >> 1], d[s][2 * k][(i >> 1) + 1],
-                              d[s][2 * k + 1][(i >> 1) + 1]};
+                    for (int i = 0; i < 8; ++i) y[i] += src[i];
+                }
+                finish(out, f, col, kh0 + w, ch, y);
             }
-        __syncthreads();
-        for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
-            const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
-            float y[8] = {};
-            for (int p = 0; p < parts; ++p) {
-                const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] += src[i];
-            }
-            finish(out, f, col, kh0 + w, ch, y);
-        }
-    };
-    write(dk, static_cast<char *>(a.gk), a.scale);
-    write(dv, static_cast<char *>(a.gv), 1.0f);
+        };
+        write(dk, static_cast<char *>(a.gk), a.scale);
+        write(dv, static_cast<char *>(a.gv), 1.0f);
+    }
 }
 
 // gbias[h][i] = sum over the partial tables, 16 slices of them side by side, in order.
@@ -554,8 +591,8 @@ void run_pass(const AttnArgs &a, bool keys, hipStream_t s) {
     if (a.nwg == 0) return;
     const dim3 grid(xcd_grid(a.nwg, a.per)), block(kAttnWaves * 64);
     const bool bias = a.bias != nullptr;
-    const BwdLds lds = bwd_lds(16 * NS, 32 * DB, a.hp, a.parts, keys ? a.hp * a.head_step : a.hp,
-                               a.rule.nb, bias, !keys);
+    const BwdLds lds = bwd_lds(16 * NS, 32 * DB, a.hp, a.parts, keys ? a.head_step : 1, a.rule.nb,
+                               bias, keys);
     if (keys && bias)
         hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, true, TERMS>), grid, block, lds.total, s, a);
     else if (keys)
@@ -598,10 +635,10 @@ hipError_t launch_attn_bwd(const AttnArgs &dq, const AttnArgs &dkv, int dtype, i
         hipLaunchKernelGGL((attn_rowstat_kernel<float>), grid, dim3(256), 0, s, dq);
     run_typed(dq, dtype, false, dq_cols, s);
     run_typed(dkv, dtype, true, dkv_cols, s);
-    if (dq.bias) {
-        const int64_t t = static_cast<int64_t>(dq.H) * dq.rule.nb * dq.rule.nb;
+    if (dkv.bias) {
+        const int64_t t = static_cast<int64_t>(dkv.H) * dkv.rule.nb * dkv.rule.nb;
         hipLaunchKernelGGL(attn_hist_kernel, dim3(static_cast<uint32_t>((t + 63) / 64)), dim3(1024), 0,
-                           s, dq);
+                           s, dkv);
     }
     return hipGetLastError();
 }

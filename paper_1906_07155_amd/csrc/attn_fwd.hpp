@@ -15,6 +15,9 @@
 #pragma once
 
 #include "attn.hpp"
+#ifndef REX_FWPE
+#define REX_FWPE 2
+#endif
 
 namespace rex {
 
@@ -44,7 +47,7 @@ inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, i
 }
 
 template <typename T, int DB, int NS, bool BIAS, bool PAGED, int TERMS>
-__global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(AttnArgs a) {
     using N = Num<T>;
     using Frag = typename N::Frag;
     using Pair = typename N::Pair;
@@ -85,39 +88,31 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
                                                 min(q0 + tid, a.Nq - 1) * a.qbox_sr));
     }
 
-    uint32_t fcol[DB], pcol[DB];
-#pragma unroll
-    for (int k = 0; k < DB; ++k) {
-        fcol[k] = frag_col<T>(k, g, a.D);
-        pcol[k] = pair_col<T>(k, n, a.D);
-    }
     // the queries: column n of NS tiles; rows that are padding are zeros
     Frag q[NS][DB];
     {
         const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D);
+        const TileOffsets<T, DB> off(qr.sr, n, g, a.D);
+        const auto r = qr.at(min(q0, max(qlen - 1, 0)));
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const uint32_t off = (q0 + 16 * s + n) * qr.sr;
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int k = 0; k < DB; ++k) q[s][k] = N::load(qr.r, off + fcol[k]);
-        }
+            for (int k = 0; k < DB; ++k) q[s][k] = N::load(r, off.f[k] + 16 * s * off.sr, 0);
     }
 
     // One tile's keys and values, its page and the lane's mask byte, read one step ahead.
     const HeadRows kr = head_rows<T>(a.k, b, kh, PAGED ? 0 : klen, a.D);
     const HeadRows vr = head_rows<T>(a.v, b, kh, PAGED ? 0 : klen, a.D);
-    const uint32_t koff = n * kr.sr, voff = 4 * g * vr.sr;
-    uint32_t kcode[DB], vcode[DB][2];      // the same inside a page of the memory
+    const TileOffsets<T, DB> koff(kr.sr, n, g, a.D), voff(vr.sr, n, g, a.D);
+    uint32_t kcode[DB], vcode[DB];         // the same inside a page of the memory
 #pragma unroll
     for (int k = 0; k < DB; ++k) {
         kcode[k] = 32 * k + 8 * g < a.D ? n * a.D + 32 * k + 8 * g : kBufOOB;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            vcode[k][t] = 32 * k + 2 * n + t < a.D ? (32 * k + 2 * n + t) * kTile + 4 * g : kBufOOB;
+        vcode[k] = 32 * k + 2 * n < a.D ? (32 * k + 2 * n) * kTile + 4 * g : kBufOOB;
     }
     struct {
-        Frag f[PAGED ? 1 : 2][PAGED ? 1 : DB];           // keys
-        Pair p[PAGED ? 1 : DB][8];                       // values
+        Frag f[2][DB];                                   // keys
+        Pair p[DB][8];                                   // values
         u32x2 kc[PAGED ? 2 : 1][PAGED ? DB : 1];         // their codes and scales in the memory
         uint32_t vc[PAGED ? DB : 1][2][2];
         f32x4 ks[2], vs[2];
@@ -141,16 +136,12 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
                 next.ks[t] = *(const REX_GLOBAL f32x4 *)(a.mks + next.ph * kTile + 16 * t + 4 * g);
 #pragma unroll
                 for (int k = 0; k < DB; ++k)
-                    next.kc[t][k] = __builtin_amdgcn_raw_buffer_load_b64(r, kcode[k] + 16 * t * a.D, 0, 0);
+                    next.kc[t][k] = __builtin_amdgcn_raw_buffer_load_b64(r, kcode[k], 16 * t * a.D, 0);
             }
         } else {
             if (a.kmask)
                 next.on = next.on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
-            const uint32_t off = tile * kTile * kr.sr + koff;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int k = 0; k < DB; ++k) next.f[t][k] = N::load(kr.r, off + 16 * t * kr.sr + fcol[k]);
+            koff.frags(kr.at(tile * kTile), tile * kTile + kTile <= klen, next.f);
         }
     };
     auto load_values = [&](int tile) {                   // after load_keys of the same tile
@@ -165,9 +156,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        next.vc[k][t][e] = __builtin_amdgcn_raw_buffer_load_b32(r, vcode[k][t] + 16 * e, 0, 0);
+                        next.vc[k][t][e] = __builtin_amdgcn_raw_buffer_load_b32(r, vcode[k] + kTile * t + 16 * e, 0, 0);
         } else {
-            load_pairs<T, DB>(vr, tile * kTile * vr.sr + voff, pcol, next.p);
+            voff.pairs(vr.at(tile * kTile), tile * kTile + kTile <= klen, next.p);
         }
     };
     // Buckets of the chunk's tiles against the workgroup's queries, by the waves that read them.
@@ -182,6 +173,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
             float kx, ky;
             box_centre(as_global<float>(box), kx, ky);
             uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
+#pragma unroll 2
             for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
                 dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(geo[c], kx, ky, a.rule));
         }

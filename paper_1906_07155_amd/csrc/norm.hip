@@ -19,30 +19,6 @@ template <typename T> struct Chunk;    // the elements of 16 bytes
 template <> struct Chunk<uint16_t> { static constexpr int kN = 8; };
 template <> struct Chunk<float> { static constexpr int kN = 4; };
 
-// E elements from column `col` on of a row; columns past C read as 0.
-template <typename T, int E>
-__device__ __forceinline__ void load_row(const void *row, int col, int C, bool vec, float *x) {
-    if (vec) {
-        if (col < C) {
-            if constexpr (E == 8) {
-                const bf16x8 f = *(const REX_GLOBAL bf16x8 *)(static_cast<const char *>(row) + col * 2);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(f[i]);
-            } else {
-                const f32x4 f = *(const REX_GLOBAL f32x4 *)(static_cast<const char *>(row) + col * 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = f[i];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) x[i] = 0.0f;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = col + i < C ? load_f32<T>(as_global<T>(row) + col + i) : 0.0f;
-    }
-}
-
 template <typename T, int E>
 __device__ __forceinline__ void store_row(void *row, int col, int C, bool vec, const float *x) {
     if (vec) {
@@ -62,11 +38,25 @@ __device__ __forceinline__ void store_row(void *row, int col, int C, bool vec, c
     }
 }
 
-// E parameters (binary32, 4-byte aligned) or `none` where there is no such array.
+// E parameters (binary32) or `none` where there is no such array; vec: 16 bytes at a time.
 template <int E>
-__device__ __forceinline__ void load_param(const float *p, int col, int C, float none, float *x) {
+__device__ __forceinline__ void load_param(const float *p, int col, int C, bool vec, float none, float *x) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = p && col + i < C ? as_global<float>(p)[col + i] : none;
+    for (int i = 0; i < E; ++i) x[i] = none;
+    if (!p) return;
+    if (vec) {
+        if (col < C) {
+#pragma unroll
+            for (int i = 0; i < E; i += 4) {
+                const f32x4 f = *(const REX_GLOBAL f32x4 *)(p + col + i);
+                x[i] = f[0], x[i + 1] = f[1], x[i + 2] = f[2], x[i + 3] = f[3];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (col + i < C) x[i] = as_global<float>(p)[col + i];
+    }
 }
 
 // Sums of two values over the TPR threads of a row; every one of them gets both.
@@ -92,101 +82,160 @@ __device__ __forceinline__ void row_sum(float &a, float &b, f32x2 (&mem)[2][16],
     }
 }
 
+// What a thread has of a row as it was read: conversion waits until it is used.
+template <typename T, int V>
+struct RowChunk {
+    u32x4 v[V];
+};
+template <typename T, int TPR, int V>
+__device__ __forceinline__ RowChunk<T, V> fetch(const void *base, int64_t row, int64_t stride, int t, int C,
+                                                bool vec) {
+    constexpr int E = Chunk<T>::kN;
+    const char *p = static_cast<const char *>(base) + row * stride * static_cast<int>(sizeof(T));
+    RowChunk<T, V> r;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int col = (k * TPR + t) * E;
+        r.v[k] = u32x4{};
+        if (vec) {
+            if (col < C) r.v[k] = *(const REX_GLOBAL u32x4 *)(p + col * static_cast<int>(sizeof(T)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (col + i < C) {
+                    const uint32_t bits = as_global<T>(p)[col + i];
+                    if constexpr (E == 8) r.v[k][i >> 1] |= bits << (16 * (i & 1));
+                }
+            if constexpr (E == 4) {
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if (col + i < C) r.v[k][i] = as_global<uint32_t>(p)[col + i];
+            }
+        }
+    }
+    return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ float value(const RowChunk<T, V> &r, int k, int i) {
+    if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? r.v[k][i >> 1] & 0xffff0000u : r.v[k][i >> 1] << 16);
+    else return __uint_as_float(r.v[k][i]);
+}
+
+// Rows go to the workgroups in runs; a thread keeps its columns' parameters from row to row
+// and has the next row's data on the way while it works on one.
 template <typename T, int TPR, int V>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(NormArgs a) {
-    constexpr int E = Chunk<T>::kN;
-    constexpr int kThreads = threads_of(TPR);
+    constexpr int E = Chunk<T>::kN, kThreads = threads_of(TPR), kSlots = kThreads / TPR;
     __shared__ f32x2 mem[2][16];
     int turn = 0;
-    const int t = threadIdx.x % TPR;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / TPR) + threadIdx.x / TPR;
-    const bool on = row < a.rows;                 // (one row per workgroup: always)
-    const int64_t r = on ? row : a.rows - 1;
+    const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
     const float inv = 1.0f / static_cast<float>(a.C);
-    float y[V][E];
-    float stat[4] = {};
+    const bool single = a.rows_per_gate == 1;
 
+    // sum over the row of f(element)
+    auto total = [&](auto f) {
+        float s = 0.0f, none = 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int i = 0; i < E; ++i) s = f(s, k, i);
+        row_sum<TPR>(s, none, mem, turn);
+        return s;
+    };
     // deviations from the mean in place, their 1 / sqrt in rstd
     auto norm = [&](float (&v)[V][E], float &mean, float &rstd) {
-        float s = 0.0f, none = 0.0f;
         mean = 0.0f;
         if (a.layer) {
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-#pragma unroll
-                for (int i = 0; i < E; ++i) s += v[k][i];
-            row_sum<TPR>(s, none, mem, turn);
-            mean = s * inv;
+            mean = total([&](float s, int k, int i) { return s + v[k][i]; }) * inv;
 #pragma unroll
             for (int k = 0; k < V; ++k)
 #pragma unroll
                 for (int i = 0; i < E; ++i) v[k][i] = (k * TPR + t) * E + i < a.C ? v[k][i] - mean : 0.0f;
         }
-        s = none = 0.0f;
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-#pragma unroll
-            for (int i = 0; i < E; ++i) s = fmaf(v[k][i], v[k][i], s);
-        row_sum<TPR>(s, none, mem, turn);
-        rstd = 1.0f / sqrtf(s * inv + a.eps);
+        rstd = 1.0f / sqrtf(total([&](float s, int k, int i) { return fmaf(v[k][i], v[k][i], s); }) * inv + a.eps);
     };
 
-    const char *px = static_cast<const char *>(a.x) + r * a.x_stride * static_cast<int>(sizeof(T));
+    float w1[V][E], c1[V][E], w2[V][E], c2[V][E], gate[V][E];
 #pragma unroll
-    for (int k = 0; k < V; ++k) load_row<T, E>(px, (k * TPR + t) * E, a.C, a.vec, y[k]);
-    if (a.branch) {
-        float z[V][E];
-        const char *pb = static_cast<const char *>(a.branch) + r * a.b_stride * static_cast<int>(sizeof(T));
+    for (int k = 0; k < V; ++k) {
+        const int col = (k * TPR + t) * E;
+        load_param<E>(a.w1, col, a.C, a.pvec, 1.0f, w1[k]);
+        load_param<E>(a.c1, col, a.C, a.pvec, 0.0f, c1[k]);
+        load_param<E>(a.w2, col, a.C, a.pvec, 1.0f, w2[k]);
+        load_param<E>(a.c2, col, a.C, a.pvec, 0.0f, c2[k]);
 #pragma unroll
-        for (int k = 0; k < V; ++k) load_row<T, E>(pb, (k * TPR + t) * E, a.C, a.vec, z[k]);
-        norm(z, stat[0], stat[1]);
-        const float *gate = a.gate ? a.gate + r / a.rows_per_gate * a.C : nullptr;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int col = (k * TPR + t) * E;
-            float w[E], c[E], g[E];
-            load_param<E>(a.w1, col, a.C, 1.0f, w);
-            load_param<E>(a.c1, col, a.C, 0.0f, c);
-            load_param<E>(gate, col, a.C, 1.0f, g);
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                y[k][i] = fmaf(a.alpha * g[i], fmaf(z[k][i] * stat[1], w[i], c[i]), y[k][i]);
-            if (on && a.y)
-                store_row<T, E>(static_cast<T *>(a.y) + r * a.C, col, a.C, a.vec, y[k]);
-        }
-    } else if (a.y && on) {
+        for (int i = 0; i < E; ++i) gate[k][i] = a.alpha;
+    }
+    const int64_t begin = static_cast<int64_t>(blockIdx.x) * a.unit_rows, end = min(begin + a.unit_rows, a.rows);
+    // a slot past the last row repeats it and stores nothing
+    auto row_of = [&](int64_t first) { return min(first + slot, end - 1); };
+    RowChunk<T, V> x = fetch<T, TPR, V>(a.x, row_of(begin), a.x_stride, t, a.C, a.vec), b{};
+    if (a.branch) b = fetch<T, TPR, V>(a.branch, row_of(begin), a.b_stride, t, a.C, a.vec);
+    uint32_t had = 0xffffffffu;
+    for (int64_t first = begin; first < end; first += kSlots) {
+        const int64_t r = row_of(first);
+        const bool on = first + slot < end;
+        float y[V][E], stat[4] = {};
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            store_row<T, E>(static_cast<T *>(a.y) + r * a.C, (k * TPR + t) * E, a.C, a.vec, y[k]);
-    }
-    if (a.second) {
-        if (a.branch) {               // columns past C hold what an empty gate made of them
+#pragma unroll
+            for (int i = 0; i < E; ++i) y[k][i] = value(x, k, i);
+        if (a.gate) {
+            const uint32_t g = single ? static_cast<uint32_t>(r) : fdiv(static_cast<uint32_t>(r), a.gate_div);
+            if (g != had) {
+                had = g;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    load_param<E>(a.gate + static_cast<int64_t>(g) * a.C, (k * TPR + t) * E, a.C, a.pvec, 0.0f, gate[k]);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) gate[k][i] *= a.alpha;
+                }
+            }
+        }
+        RowChunk<T, V> nx{}, nb{};
+        if (first + kSlots < end) {
+            nx = fetch<T, TPR, V>(a.x, row_of(first + kSlots), a.x_stride, t, a.C, a.vec);
+            if (a.branch) nb = fetch<T, TPR, V>(a.branch, row_of(first + kSlots), a.b_stride, t, a.C, a.vec);
+        }
+        if (a.branch) {
+            float z[V][E];
 #pragma unroll
             for (int k = 0; k < V; ++k)
 #pragma unroll
-                for (int i = 0; i < E; ++i)
+                for (int i = 0; i < E; ++i) z[k][i] = value(b, k, i);
+            norm(z, stat[0], stat[1]);
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    y[k][i] = fmaf(gate[k][i], fmaf(z[k][i] * stat[1], w1[k][i], c1[k][i]), y[k][i]);
                     if ((k * TPR + t) * E + i >= a.C) y[k][i] = 0.0f;
+                }
         }
-        norm(y, stat[2], stat[3]);
+        if (a.y && on) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int col = (k * TPR + t) * E;
-            float w[E], c[E];
-            load_param<E>(a.w2, col, a.C, 1.0f, w);
-            load_param<E>(a.c2, col, a.C, 0.0f, c);
-#pragma unroll
-            for (int i = 0; i < E; ++i) y[k][i] = fmaf(y[k][i] * stat[3], w[i], c[i]);
-            if (on && a.u) store_row<T, E>(static_cast<T *>(a.u) + r * a.C, col, a.C, a.vec, y[k]);
+            for (int k = 0; k < V; ++k)
+                store_row<T, E>(static_cast<T *>(a.y) + r * a.C, (k * TPR + t) * E, a.C, a.vec, y[k]);
         }
+        if (a.second) {
+            norm(y, stat[2], stat[3]);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) y[k][i] = fmaf(y[k][i] * stat[3], w2[k][i], c2[k][i]);
+                if (on && a.u) store_row<T, E>(static_cast<T *>(a.u) + r * a.C, (k * TPR + t) * E, a.C, a.vec, y[k]);
+            }
+        }
+        if (a.stats && t == 0 && on)
+            *(REX_GLOBAL f32x4 *)(a.stats + r * 4) = f32x4{stat[0], stat[1], stat[2], stat[3]};
+        x = nx;
+        b = nb;
     }
-    if (a.stats && t == 0 && on)
-        *(REX_GLOBAL f32x4 *)(a.stats + r * 4) = f32x4{stat[0], stat[1], stat[2], stat[3]};
 }
 
 template <typename T, int TPR, int V>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(NormArgs a) {
-    constexpr int kThreads = threads_of(TPR);
-    constexpr int E = Chunk<T>::kN, kSlots = kThreads / TPR, kSize = sizeof(T);
+    constexpr int E = Chunk<T>::kN, kThreads = threads_of(TPR), kSlots = kThreads / TPR;
     extern __shared__ float cols[];               // [kSlots][C]
     __shared__ f32x2 mem[2][16];
     int turn = 0;
@@ -194,6 +243,16 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(NormArgs a) {
     const float inv = 1.0f / static_cast<float>(a.C);
     float sw1[V][E] = {}, sc1[V][E] = {}, sw2[V][E] = {}, sc2[V][E] = {}, sg[V][E] = {};
     const bool each = a.gate && a.rows_per_gate == 1;
+    float w1[V][E], c1[V][E], w2[V][E], gate[V][E];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int col = (k * TPR + t) * E;
+        load_param<E>(a.w1, col, a.C, a.pvec, 1.0f, w1[k]);
+        load_param<E>(a.c1, col, a.C, a.pvec, 0.0f, c1[k]);
+        load_param<E>(a.w2, col, a.C, a.pvec, 1.0f, w2[k]);
+#pragma unroll
+        for (int i = 0; i < E; ++i) gate[k][i] = 1.0f;
+    }
 
     // sums over the row slots, in order, to dst[C]
     auto flush = [&](const float (&s)[V][E], float *dst) {
@@ -227,110 +286,93 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(NormArgs a) {
         const int64_t seg = unit / a.gate_parts, in = (unit - seg * a.gate_parts) * a.unit_rows;
         const int64_t begin = seg * a.span + in;
         const int64_t end = min(min(begin + a.unit_rows, (seg + 1) * a.span), a.rows);
+        auto row_of = [&](int64_t first) { return min(first + slot, end - 1); };
+        auto load_gate = [&](int64_t g) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                load_param<E>(a.gate + g * a.C, (k * TPR + t) * E, a.C, a.pvec, 0.0f, gate[k]);
+        };
+        if (a.gate && !each) load_gate(seg);
+        RowChunk<T, V> x{}, b{}, gu{}, gy{};
+        auto fetch_all = [&](int64_t r) {
+            x = fetch<T, TPR, V>(a.x, r, a.x_stride, t, a.C, a.vec);
+            if (a.branch) b = fetch<T, TPR, V>(a.branch, r, a.b_stride, t, a.C, a.vec);
+            if (a.gu) gu = fetch<T, TPR, V>(a.gu, r, a.C, t, a.C, a.vec);
+            if (a.gy) gy = fetch<T, TPR, V>(a.gy, r, a.C, t, a.C, a.vec);
+        };
+        if (begin < end) fetch_all(row_of(begin));
         for (int64_t first = begin; first < end; first += kSlots) {
             const bool on = first + slot < end;
-            const int64_t r = on ? first + slot : end - 1;
+            const int64_t r = row_of(first);
             const f32x4 st = *(const REX_GLOBAL f32x4 *)(a.stats + r * 4);
-            float x[V][E], b[V][E], g[V][E];
-            const char *px = static_cast<const char *>(a.x) + r * a.x_stride * kSize;
-            const char *pb = static_cast<const char *>(a.branch) + r * a.b_stride * kSize;
-            const char *pu = static_cast<const char *>(a.gu) + r * a.C * kSize;
-            const char *py = static_cast<const char *>(a.gy) + r * a.C * kSize;
-            const float *gate = a.gate ? a.gate + r / a.rows_per_gate * a.C : nullptr;
-            // b: N1's normalised row; x: y, then the gradient of y
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int col = (k * TPR + t) * E;
-                load_row<T, E>(px, col, a.C, a.vec, x[k]);
-                if (a.branch) {
-                    load_row<T, E>(pb, col, a.C, a.vec, b[k]);
-                    float w[E], c[E], ga[E];
-                    load_param<E>(a.w1, col, a.C, 1.0f, w);
-                    load_param<E>(a.c1, col, a.C, 0.0f, c);
-                    load_param<E>(gate, col, a.C, 1.0f, ga);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        b[k][i] = (b[k][i] - st[0]) * st[1];
-                        x[k][i] = fmaf(a.alpha * ga[i], fmaf(b[k][i], w[i], c[i]), x[k][i]);
-                    }
-                }
-            }
+            if (each) load_gate(r);
+            // hat1: N1's normalised row; y: N2's, from y = x + alpha gate N1(branch); d: the
+            // gradient of y, g: upstream gradients times weights
+            float hat1[V][E], y[V][E], d[V][E], g[V][E];
             float s1 = 0.0f, s0 = 0.0f;
-            if (a.gu) {
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const int col = (k * TPR + t) * E;
-                    float u[E], w[E];
-                    load_row<T, E>(pu, col, a.C, a.vec, u);
-                    load_param<E>(a.w2, col, a.C, 1.0f, w);
+            for (int k = 0; k < V; ++k)
 #pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        x[k][i] = (x[k][i] - st[2]) * st[3];
-                        if (on) {
-                            sw2[k][i] = fmaf(u[i], x[k][i], sw2[k][i]);
-                            sc2[k][i] += u[i];
-                        }
-                        g[k][i] = u[i] * w[i];          // 0 past C, as u
-                        s1 = fmaf(g[k][i], x[k][i], s1);
-                        s0 += g[k][i];
+                for (int i = 0; i < E; ++i) {
+                    hat1[k][i] = (value(b, k, i) - st[0]) * st[1];
+                    y[k][i] = value(x, k, i);
+                    if (a.branch)
+                        y[k][i] = fmaf(a.alpha * gate[k][i], fmaf(hat1[k][i], w1[k][i], c1[k][i]), y[k][i]);
+                    y[k][i] = (y[k][i] - st[2]) * st[3];
+                    const float u = value(gu, k, i);
+                    if (on) {
+                        sw2[k][i] = fmaf(u, y[k][i], sw2[k][i]);
+                        sc2[k][i] += u;
                     }
+                    g[k][i] = u * w2[k][i];              // 0 past C, as u
+                    s1 = fmaf(g[k][i], y[k][i], s1);
+                    s0 += g[k][i];
+                    d[k][i] = value(gy, k, i);
                 }
+            if (first + kSlots < end) fetch_all(row_of(first + kSlots));
+            if (a.gu) {
                 row_sum<TPR>(s1, s0, mem, turn);
                 s1 *= inv;
                 s0 = a.layer ? s0 * inv : 0.0f;
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+#pragma unroll
+                    for (int i = 0; i < E; ++i) d[k][i] += st[3] * ((g[k][i] - s0) - y[k][i] * s1);
             }
+            if (on && a.gx) {
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    store_row<T, E>(static_cast<T *>(a.gx) + r * a.C, (k * TPR + t) * E, a.C, a.vec, d[k]);
+            }
+            if (!a.branch) continue;
             float m1 = 0.0f, m0 = 0.0f;
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int col = (k * TPR + t) * E;
-                float d[E];
+            for (int k = 0; k < V; ++k)
 #pragma unroll
-                for (int i = 0; i < E; ++i) d[i] = 0.0f;
-                if (a.gy) load_row<T, E>(py, col, a.C, a.vec, d);
-                if (a.gu) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i)
-                        d[i] += st[3] * ((g[k][i] - s0) - x[k][i] * s1);
+                for (int i = 0; i < E; ++i) {
+                    const int col = (k * TPR + t) * E + i;
+                    const float ad = col < a.C ? a.alpha * d[k][i] : 0.0f;
+                    const float gz = gate[k][i] * ad, dg = ad * fmaf(hat1[k][i], w1[k][i], c1[k][i]);
+                    if (on) {
+                        sg[k][i] += dg;
+                        sw1[k][i] = fmaf(gz, hat1[k][i], sw1[k][i]);
+                        sc1[k][i] += gz;
+                        if (each && a.ggate && col < a.C) as_global_mut<float>(a.ggate)[r * a.C + col] = dg;
+                    }
+                    g[k][i] = gz * w1[k][i];
+                    m1 = fmaf(g[k][i], hat1[k][i], m1);
+                    m0 += g[k][i];
                 }
-                if (on && a.gx) store_row<T, E>(static_cast<T *>(a.gx) + r * a.C, col, a.C, a.vec, d);
-                if (a.branch) {
-                    float w[E], c[E], ga[E], dg[E];
-                    load_param<E>(a.w1, col, a.C, 1.0f, w);
-                    load_param<E>(a.c1, col, a.C, 0.0f, c);
-                    load_param<E>(gate, col, a.C, 1.0f, ga);
+            row_sum<TPR>(m1, m0, mem, turn);
+            m1 *= inv;
+            m0 = a.layer ? m0 * inv : 0.0f;
+            if (on && a.gb) {
 #pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        const float ad = col + i < a.C ? a.alpha * d[i] : 0.0f;
-                        const float gz = ga[i] * ad;
-                        dg[i] = ad * fmaf(b[k][i], w[i], c[i]);
-                        if (on) {
-                            sg[k][i] += dg[i];
-                            sw1[k][i] = fmaf(gz, b[k][i], sw1[k][i]);
-                            sc1[k][i] += gz;
-                        }
-                        g[k][i] = gz * w[i];
-                        m1 = fmaf(g[k][i], b[k][i], m1);
-                        m0 += g[k][i];
-                    }
-                    if (each && on && a.ggate) {
+                for (int k = 0; k < V; ++k) {
+                    float e[E];
 #pragma unroll
-                        for (int i = 0; i < E; ++i)
-                            if (col + i < a.C) as_global_mut<float>(a.ggate)[r * a.C + col + i] = dg[i];
-                    }
-                }
-            }
-            if (a.branch) {
-                row_sum<TPR>(m1, m0, mem, turn);
-                m1 *= inv;
-                m0 = a.layer ? m0 * inv : 0.0f;
-                if (on && a.gb) {
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        float d[E];
-#pragma unroll
-                        for (int i = 0; i < E; ++i) d[i] = st[1] * ((g[k][i] - m0) - b[k][i] * m1);
-                        store_row<T, E>(static_cast<T *>(a.gb) + r * a.C, (k * TPR + t) * E, a.C, a.vec, d);
-                    }
+                    for (int i = 0; i < E; ++i) e[i] = st[1] * ((g[k][i] - m0) - hat1[k][i] * m1);
+                    store_row<T, E>(static_cast<T *>(a.gb) + r * a.C, (k * TPR + t) * E, a.C, a.vec, e);
                 }
             }
         }
@@ -383,10 +425,7 @@ __global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a, int gate
 
 template <typename T, int TPR, int V>
 void run_fwd(const NormArgs &a, hipStream_t s) {
-    constexpr int kThreads = threads_of(TPR);
-    constexpr int kSlots = kThreads / TPR;
-    hipLaunchKernelGGL((norm_fwd_kernel<T, TPR, V>), dim3(static_cast<uint32_t>((a.rows + kSlots - 1) / kSlots)),
-                       dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((norm_fwd_kernel<T, TPR, V>), dim3(a.blocks), dim3(threads_of(TPR)), 0, s, a);
 }
 template <typename T, int TPR, int V>
 void run_bwd(const NormArgs &a, hipStream_t s) {

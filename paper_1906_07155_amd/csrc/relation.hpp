@@ -2,12 +2,15 @@
 // the host API (relation_api.hip) and the kernel translation units.
 #pragma once
 
-#include "common.hpp"
+#include "internal.hpp"
 
 namespace rex {
 
 constexpr int kTile = 32;          // keys of one step of the attention, boxes of one page
-constexpr int kAttnWaves = 8;      // waves of one attention workgroup
+#ifndef REX_WAVES
+#define REX_WAVES 8
+#endif
+constexpr int kAttnWaves = REX_WAVES;      // waves of one attention workgroup
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -60,7 +63,7 @@ struct AttnArgs {
     float *rowstat;                     // [B][H][Nqp][2]: lse in units of log 2 (+inf: no row), delta
     float *hist;                        // [B * spans][H][nb * nb]
     int32_t Nqp;
-    int32_t span, spans;                // query tiles of one workgroup, runs of them per image
+    int32_t span, spans;                // key tiles of one workgroup, runs of them per image
     int32_t head_step;                  // heads of a group whose tables are in LDS together
 };
 
@@ -92,6 +95,7 @@ struct NormArgs {
     const void *x, *branch;
     int64_t x_stride, b_stride;
     int64_t rows, rows_per_gate;
+    FastDiv gate_div;                   // by rows_per_gate
     int32_t C;
     int32_t layer;
     float alpha, eps;
@@ -100,6 +104,7 @@ struct NormArgs {
     float *stats;
     int32_t second;                     // the second norm takes part
     int32_t vec;                        // rows can be read and written 16 bytes at a time
+    int32_t pvec;                       // parameters too
     // backward
     const void *gy, *gu;
     void *gx, *gb;
@@ -107,7 +112,8 @@ struct NormArgs {
     float *part;                        // [blocks][4][C]: sums for gw1, gc1, gw2, gc2
     float *gate_part;                   // [gates * gate_parts][C]
     int32_t gate_sum;                   // ggate is the sum of gate_part's rows
-    // A unit is a run of rows of one gate row: unit i holds rows from
+    // Forward: unit_rows rows for each of `blocks` workgroups.
+    // Backward: a unit is a run of rows of one gate row: unit i holds rows from
     // (i / gate_parts) * span + (i % gate_parts) * unit_rows on, span rows per gate row.
     int64_t units, span, gates;
     int32_t gate_parts, unit_rows, blocks;

@@ -24,6 +24,7 @@ from .binding import RE_DTYPE_BF16, _dtype_code, _need_cuda, _torch, check
 HEADER = os.path.join(os.path.dirname(binding.HERE), "include", "box_relation.h")
 
 MAX_DIM, MAX_HEADS, MAX_BUCKETS, MEMORY_PAGE = 128, 256, 31, 32
+FEW_KEYS = 64                       # RE_ATTN_FEW_KEYS
 NORMS = {"rms": 0, "layer": 1}      # RE_NORM_RMS, RE_NORM_LAYER
 
 _VP, _I32, _I64, _SZ, _D = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
@@ -78,23 +79,25 @@ def lib():
 # ---------------------------------------------------------------------------
 
 class _Call:
-    """One call's device and stream.  Tensors that the call allocates itself are handed to a
-    stream other than the current one with record_stream, so that their memory is not
-    given away while that stream still uses it."""
+    """One call's stream, and a `with` block's worth of its device where that is not the
+    current one.  Tensors that the call allocates itself are handed to a stream other than the
+    current one with record_stream, so that their memory is not given away while that stream
+    still uses it."""
+
+    __slots__ = ("device", "other", "stream", "guard")
 
     def __init__(self, like, stream):
         torch = _torch()
-        self.device = like.device
-        self.other = stream
-        if like.device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(like.device)
-            self.guard.__enter__()
-        else:
-            self.guard = None
-        self.stream = (stream if stream is not None
-                       else torch.cuda.current_stream(like.device)).cuda_stream
+        self.device, self.other, self.guard = like.device, stream, None
+        index = self.device.index
+        if index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.device)
+        # (torch.cuda.current_stream makes a Stream object: 1.9 us, the handle alone 0.1 us)
+        self.stream = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
     def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
         return self
 
     def __exit__(self, *exc):
@@ -163,10 +166,14 @@ def _lengths(t, batch: int, name: str):
         _dense(t, (batch,), name, _torch().int32)
 
 
-def _same_device(like, **tensors):
-    for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.device != like.device):
-            _need_cuda(t, name, like)
+def _same_device(like, names, tensors):
+    """Every given tensor (None skipped) is on the device of `like`."""
+    device = like.device
+    for t in tensors:
+        if t is not None and t.device != device:
+            for name, u in zip(names.split(), tensors):
+                if u is not None:
+                    _need_cuda(u, name, like)
 
 
 def _ptr(t):
@@ -202,8 +209,7 @@ def _attn_descriptor(q, k, v, scale, q_boxes, k_boxes, bias, first_exp, octave_s
             raise ValueError("k_mask must be bool or uint8 (got %s)" % k_mask.dtype)
         _dense(k_mask, (B, nk), "k_mask", k_mask.dtype)
     _need_cuda(q, "q")
-    _same_device(q, k=k, v=v, bias=bias, q_boxes=q_boxes, k_boxes=k_boxes, q_len=q_len,
-                 k_len=k_len, k_mask=k_mask)
+    _same_device(q, "k v bias q_boxes k_boxes q_len k_len k_mask", (k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask))
     if scale is None:
         scale = D ** -0.5
     return _ATTN.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), code, H, hkv, D, B, nq, nk,
@@ -235,9 +241,9 @@ def box_attn_fwd(q, k, v, *, scale: Optional[float] = None, q_boxes=None, k_boxe
     """Attention of q [B, Nq, H, D] over k, v [B, Nk, Hkv, D] (heads share keys where Hkv < H).
     bias: float32 [H, n, n] by bucket of (q_boxes [B, Nq, 4], k_boxes [B, Nk, 4]); q_len,
     k_len: int32 [B] valid rows; k_mask: bool [B, Nk], False leaves a key out; scale: D^-1/2
-    by default.  Returns (out, lse, out_f32): lse float32 [B, H, Nq] and (for bf16 data) out_f32,
-    `out` in float32, are what the backward takes, made where `save` is true or they are
-    given, else None."""
+    by default.  Returns (out, lse, out_f32): lse float32 [B, H, Nq] and (for bf16 data and up to
+    64 keys) out_f32, `out` in float32, are what the backward takes, made where `save` is true
+    or they are given, else None."""
     torch = _torch()
     d = _attn_descriptor(q, k, v, scale, q_boxes, k_boxes, bias, first_exp, octave_steps, q_len,
                          k_len, k_mask)
@@ -248,17 +254,17 @@ def box_attn_fwd(q, k, v, *, scale: Optional[float] = None, q_boxes=None, k_boxe
         _dense(out_f32, (B, nq, H, D), "out_f32", torch.float32)
     if lse is not None:
         _dense(lse, (B, H, nq), "lse", torch.float32)
-    _same_device(q, out=out, lse=lse, out_f32=out_f32)
+    _same_device(q, "out lse out_f32", (out, lse, out_f32))
     if workspace is not None:
         binding._workspace(workspace, q)
-        _same_device(q, workspace=workspace)
+        _same_device(q, "workspace", (workspace,))
     L = lib()
     with _Call(q, stream) as c:
         if out is None:
             out = c.empty((B, nq, H, D), q.dtype)
         if save and lse is None:
             lse = c.empty((B, H, nq), torch.float32)
-        if save and out_f32 is None and q.dtype == torch.bfloat16:
+        if save and out_f32 is None and q.dtype == torch.bfloat16 and k.shape[1] <= FEW_KEYS:
             out_f32 = c.empty((B, nq, H, D), torch.float32)
         need = 0
         if workspace is None:
@@ -293,11 +299,10 @@ def box_attn_bwd(grad_out, q, k, v, out, lse, out_f32=None, *, scale: Optional[f
         if bias is None:
             raise ValueError("grad_bias without a bias")
         _dense(grad_bias, bias.shape, "grad_bias", torch.float32)
-    _same_device(q, grad_out=grad_out, out=out, lse=lse, out_f32=out_f32, grad_q=grad_q,
-                 grad_k=grad_k, grad_v=grad_v, grad_bias=grad_bias)
+    _same_device(q, "grad_out out lse out_f32 grad_q grad_k grad_v grad_bias", (grad_out, out, lse, out_f32, grad_q, grad_k, grad_v, grad_bias))
     if workspace is not None:
         binding._workspace(workspace, q)
-        _same_device(q, workspace=workspace)
+        _same_device(q, "workspace", (workspace,))
     L = lib()
     with _Call(q, stream) as c:
         if grad_q is None:
@@ -348,7 +353,7 @@ def _memory_descriptor(memory):
     _dense(vs, (pages, hkv, p), "the memory's v_scale", torch.float32)
     _dense(boxes, (pages, p, 4), "the memory's boxes", torch.float32)
     _need_cuda(k, "the memory")
-    _same_device(k, v=v, k_scale=ks, v_scale=vs, boxes=boxes)
+    _same_device(k, "v k_scale v_scale boxes", (v, ks, vs, boxes))
     return _MEMORY.pack(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(),
                         boxes.data_ptr(), pages, hkv, dim), hkv, dim
 
@@ -358,7 +363,7 @@ def _slots(slots, like):
     if slots.dim() != 1:
         raise ValueError("slots must be 1-D")
     _dense(slots, (slots.shape[0],), "slots", torch.int64)
-    _same_device(like, slots=slots)
+    _same_device(like, "slots", (slots,))
     return slots.shape[0]
 
 
@@ -378,7 +383,7 @@ def box_memory_append(memory: Sequence, slots, k, v, boxes, stream=None) -> None
         raise TypeError("k and v must have one dtype (got %s, %s)" % (k.dtype, v.dtype))
     code = _dtype_code(k)
     _dense(boxes, (n, 4), "boxes", torch.float32)
-    _same_device(like, k=k, v=v, boxes=boxes)
+    _same_device(like, "k v boxes", (k, v, boxes))
     with _Call(like, stream) as c:
         check(lib().box_memory_append(d, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), code,
                                       _PAIR.pack(*k.stride()[:2]), _PAIR.pack(*v.stride()[:2]),
@@ -436,11 +441,10 @@ def box_memory_attn_fwd(q, memory: Sequence, pages, lengths, *, scale: Optional[
     if lse is not None:
         _dense(lse, (B, H, nq), "lse", torch.float32)
     _need_cuda(q, "q", memory[0])
-    _same_device(q, pages=pages, lengths=lengths, q_len=q_len, bias=bias, q_boxes=q_boxes, out=out,
-                 lse=lse)
+    _same_device(q, "pages lengths q_len bias q_boxes out lse", (pages, lengths, q_len, bias, q_boxes, out, lse))
     if workspace is not None:
         binding._workspace(workspace, q)
-        _same_device(q, workspace=workspace)
+        _same_device(q, "workspace", (workspace,))
     d = _RECALL.pack(q.data_ptr(), code, H, B, nq, pages.shape[1], *q.stride()[:3],
                      D ** -0.5 if scale is None else scale, n, first_exp, octave_steps,
                      _ptr(bias), _ptr(q_boxes), *strides, _ptr(q_len), pages.data_ptr(),
@@ -494,8 +498,7 @@ def _norm_descriptor(x, branch, gate, alpha, post_weight, post_bias, pre_weight,
         if t is not None:
             _dense(t, (c,), name, torch.float32)
     _need_cuda(x, "x")
-    _same_device(x, branch=branch, gate=gate, post_weight=post_weight, post_bias=post_bias,
-                 pre_weight=pre_weight, pre_bias=pre_bias)
+    _same_device(x, "branch gate post_weight post_bias pre_weight pre_bias", (branch, gate, post_weight, post_bias, pre_weight, pre_bias))
     return _NORM.pack(x.data_ptr(), _ptr(branch), x.stride(0), 0 if branch is None else branch.stride(0),
                       code, NORMS[norm], m, c, alpha, eps, gates, _ptr(gate), *map(_ptr, params))
 
@@ -522,7 +525,7 @@ def gated_norm_fwd(x, branch=None, *, gate=None, alpha: float = 1.0, post_weight
         raise ValueError("u without the second norm")
     if stats is not None:
         _dense(stats, (m, 4), "stats", torch.float32)
-    _same_device(x, y=y, u=u, stats=stats)
+    _same_device(x, "y u stats", (y, u, stats))
     with _Call(x, stream) as c:
         if y is None and branch is not None:
             y = c.empty((m, ch), x.dtype)
@@ -549,17 +552,24 @@ def gated_norm_bwd(grad_y, grad_u, x, branch, stats, *, gate=None, alpha: float 
         if t is not None:
             _dense(t, (m, ch), name, x.dtype)
     _dense(stats, (m, 4), "stats", torch.float32)
-    _same_device(x, grad_y=grad_y, grad_u=grad_u, stats=stats)
+    _same_device(x, "grad_y grad_u stats", (grad_y, grad_u, stats))
     if workspace is not None:
         binding._workspace(workspace, x)
-        _same_device(x, workspace=workspace)
+        _same_device(x, "workspace", (workspace,))
     L = lib()
     with _Call(x, stream) as c:
         gx = c.empty((m, ch), x.dtype)
         gb = None if branch is None else c.empty((m, ch), x.dtype)
-        small = [None if p is None else c.empty(tuple(p.shape), torch.float32)
-                 for p in (gate, post_weight if branch is not None else None,
-                           post_bias if branch is not None else None, pre_weight, pre_bias)]
+        params = (gate, post_weight, post_bias, pre_weight, pre_bias)
+        if branch is None:
+            params = (None, None, None, pre_weight, pre_bias)
+        sizes = [0 if p is None else p.numel() for p in params]
+        small = [None] * 5              # parts of one buffer, each at a multiple of 4 elements
+        if any(sizes):
+            room = [(n + 3) // 4 * 4 for n in sizes]
+            parts = c.empty((sum(room),), torch.float32).split_with_sizes(room)
+            small = [None if p is None else t if n == r and p.dim() == 1 else t[:n].view(p.shape)
+                     for p, t, n, r in zip(params, parts, sizes, room)]
         need = 0
         if workspace is None:
             need = _size(L.gated_norm_workspace_size, "gated_norm_workspace_size", d)
