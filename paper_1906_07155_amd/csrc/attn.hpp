@@ -5,14 +5,20 @@
 // 32; the result has column n and rows 4g + i, i = 0..3.  Binary32 has steps of 4, k-slot g:
 // eight of them, the j-th taking element j of the same registers, make the same step of 32.
 //
-// Two things follow from the freedom to order rows and k-slots as one likes:
-//   - A lane's results of two 16-row tiles (rows 4g + i of either) are, as they stand, its B
-//     operand of a step of 32 in which slot 8g + j is row 4g + j of the first tile (j < 4)
-//     or row 4g + j - 4 of the second: the softmax weights never leave their lane.
-//   - The transposed operand (channels as rows) is read straight from row-major memory: lane
-//     n takes channels 2n and 2n + 1 of its eight rows, and the low and the high halves
-//     are the A operands of two 16-channel tiles, channel 2r + t in row r of tile t.  Of the
-//     two results a lane then holds channels 8g .. 8g + 7 of its column: one 16-byte store.
+// Three things follow from the freedom to order rows and k-slots as one likes:
+//   - Row r of the first of two 16-row tiles is streamed row 8 (r / 4) + r % 4, of the second
+//     four rows further on.  A lane's results, rows 4g + i of either, are then streamed rows
+//     8g .. 8g + 7 in order, and as they stand its B operand of a step of 32: the softmax
+//     weights never leave their lane, and masks, scales and buckets of a lane's eight rows
+//     are adjacent in memory.
+//   - The transposed operand (channels as rows, streamed rows as k-slots) of bf16 data is
+//     read from LDS, where a tile's rows are put by loads that go there directly: the
+//     transposing read gives a lane one channel of four rows.  (Read from memory as pairs
+//     of channels a tile of 64 channels takes 16 loads of 4 bytes a lane instead of 4 of 16,
+//     and each costs the address unit the same 16 cycles.  16 images of up to 1000 boxes in 16
+//     heads of 64 channels: forward 197 us that way, 176 this way; query pass 226 and 211.)
+//   - Binary32 data has no such read: lane n takes channels 2n and 2n + 1 of its eight
+//     rows from memory, the operands of two tiles with channel 2r + t in row r of tile t.
 #pragma once
 
 #include "relation.hpp"
@@ -80,6 +86,19 @@ template <> struct Num<uint16_t> {    // bf16
     static __device__ __forceinline__ void store(char *p, const float (&x)[8]) {
         *(REX_GLOBAL Frag *)(p) = round(x);
     }
+    static __device__ __forceinline__ void store4(char *p, f32x4 x) {
+        using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
+        *(REX_GLOBAL bf16x4 *)(p) = bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]),
+                                           static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])};
+    }
+    // keeps the elements whose bit of m is set
+    static __device__ __forceinline__ void keep(Frag &f, uint32_t m) {
+        u32x4 v = __builtin_bit_cast(u32x4, f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] &= (m >> (2 * j) & 1u ? 0xffffu : 0u) | (m >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+        f = __builtin_bit_cast(Frag, v);
+    }
     // four codes of the memory -> four numbers
     static __device__ __forceinline__ void widen(Frag &f, int at, uint32_t c) {
 #pragma unroll
@@ -128,6 +147,11 @@ template <> struct Num<float> {
         *(REX_GLOBAL f32x4 *)(p) = f32x4{x[0], x[1], x[2], x[3]};
         *(REX_GLOBAL f32x4 *)(p + 16) = f32x4{x[4], x[5], x[6], x[7]};
     }
+    static __device__ __forceinline__ void store4(char *p, f32x4 x) { *(REX_GLOBAL f32x4 *)(p) = x; }
+    static __device__ __forceinline__ void keep(Frag &f, uint32_t m) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = m >> j & 1u ? f[j] : 0.0f;
+    }
     static __device__ __forceinline__ void widen(Frag &f, int at, uint32_t c) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[at + j] = static_cast<float>(static_cast<int8_t>(c >> (8 * j)));
@@ -167,48 +191,137 @@ __device__ __forceinline__ HeadRows head_rows(const Rows &x, int b, int head, in
     const uint32_t bytes = rows > 0 ? static_cast<uint32_t>(rows - 1) * x.sr + D * Num<T>::kSize : 0u;
     return HeadRows{base, bytes, x.sr};
 }
-// Lane offsets in a tile of 32 rows.  f: of the operand whose rows are rows (n and 16 + n,
-// channels 32k + 8g ..); p: of the one whose rows are channels (32k + 2n and the next, of
-// the rows slot_row(g, j)).
+// Lane offsets in a tile of 32 streamed rows.  f: of the operand whose rows are rows (see the
+// top of this file), channels 32k + 8g ..; p: of the one whose rows are channels, 32k + 2n
+// and the next, of the rows 8g + j.
 template <typename T, int DB>
 struct TileOffsets {
+    using N = Num<T>;
     uint32_t f[DB], p[DB], sr;
     __device__ __forceinline__ TileOffsets(uint32_t sr_, int n, int g, int D) : sr(sr_) {
 #pragma unroll
         for (int k = 0; k < DB; ++k) {
-            f[k] = 32 * k + 8 * g < D ? n * sr + (32 * k + 8 * g) * Num<T>::kSize : kBufOOB;
-            p[k] = 32 * k + 2 * n < D ? 4 * g * sr + (32 * k + 2 * n) * Num<T>::kSize : kBufOOB;
+            f[k] = 32 * k + 8 * g < D ? (8 * (n >> 2) + (n & 3)) * sr + (32 * k + 8 * g) * N::kSize : kBufOOB;
+            p[k] = 32 * k + 2 * n < D ? 8 * g * sr + (32 * k + 2 * n) * N::kSize : kBufOOB;
         }
     }
     // The rows' offsets go through the scalar register of the load where all 32 rows are there:
     // the range check does not see it, and no lane register is needed for it.
-    __device__ __forceinline__ void frags(__amdgpu_buffer_rsrc_t r, bool inside,
-                                          typename Num<T>::Frag (&x)[2][DB]) const {
+    __device__ __forceinline__ void frags(__amdgpu_buffer_rsrc_t r, bool inside, typename N::Frag (&x)[2][DB]) const {
         if (inside) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int k = 0; k < DB; ++k) x[t][k] = Num<T>::load(r, f[k], 16 * t * sr);
+                for (int k = 0; k < DB; ++k) x[t][k] = N::load(r, f[k], 4 * t * sr);
         } else {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int k = 0; k < DB; ++k) x[t][k] = Num<T>::load(r, f[k] + 16 * t * sr, 0);
+                for (int k = 0; k < DB; ++k) x[t][k] = N::load(r, f[k] + 4 * t * sr, 0);
         }
     }
-    __device__ __forceinline__ void pairs(__amdgpu_buffer_rsrc_t r, bool inside,
-                                          typename Num<T>::Pair (&x)[DB][8]) const {
+    __device__ __forceinline__ void pairs(__amdgpu_buffer_rsrc_t r, bool inside, typename N::Pair (&x)[DB][8]) const {
         if (inside) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int k = 0; k < DB; ++k) x[k][j] = Num<T>::load_pair(r, p[k], (j < 4 ? j : 12 + j) * sr);
+                for (int k = 0; k < DB; ++k) x[k][j] = N::load_pair(r, p[k], j * sr);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int k = 0; k < DB; ++k) x[k][j] = Num<T>::load_pair(r, p[k] + (j < 4 ? j : 12 + j) * sr, 0);
+                for (int k = 0; k < DB; ++k) x[k][j] = N::load_pair(r, p[k] + j * sr, 0);
         }
+    }
+};
+// Column operands: rows 16 s + n from the resource's first row on.
+template <typename T, int DB, int NS>
+__device__ __forceinline__ void load_columns(__amdgpu_buffer_rsrc_t r, uint32_t sr, int n, int g, int D,
+                                             typename Num<T>::Frag (&x)[NS][DB]) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int k = 0; k < DB; ++k) {
+            const int ch = 32 * k + 8 * g;
+            x[s][k] = Num<T>::load(r, ch < D ? (16 * s + n) * sr + ch * Num<T>::kSize : kBufOOB, 0);
+        }
+}
+
+// One wave's tile of 32 bf16 rows in LDS, 64 * DB bytes a row, and its two readings.  Loads
+// put 16 bytes of each lane at consecutive places, so which chunk of a row a lane loads is
+// what spreads the reads over the banks: chunk c of row r is at place c ^ f(r), f chosen
+// such that the 32 lanes of half a transposing read (rows 0-3 and 8-11 of some eight-row
+// blocks) meet 32 different pairs of banks.  What lies past the resource's end is zeros.
+// (the host's pass over kernels knows neither LDS nor these loads)
+#ifdef __HIP_DEVICE_COMPILE__
+#define REX_LDS __attribute__((address_space(3)))
+#else
+#define REX_LDS
+#endif
+template <int DB>
+struct LdsTile {
+    using Place = REX_LDS char *;
+    static constexpr int kBytes = kTile * 64 * DB, kChunks = 4 * DB, kRows = 16 / DB;   // rows of one load
+    Place at;                         // the wave's tile, or the first of several one after the other
+    Place nat[DB], tr[2 * DB];        // a lane's places in the two readings
+    static __device__ __forceinline__ int turn(int r) {
+        return 2 * (((r & 3) | (r >> 1 & 4)) >> (DB == 1 ? 2 : DB == 2 ? 1 : 0));
+    }
+    __device__ __forceinline__ LdsTile(char *at_, int lane) : at((Place)at_) {
+        const int n = lane & 15, g = lane >> 4;
+        // four rows on, r & 3 and r >> 3 and so the turn are the same: a constant offset
+        const int r = 8 * (n >> 2) + (n & 3), q = 8 * g + (n >> 2);
+#pragma unroll
+        for (int k = 0; k < DB; ++k) nat[k] = at + r * 64 * DB + ((4 * k + g) ^ turn(r)) * 16;
+#pragma unroll
+        for (int u = 0; u < 2 * DB; ++u)
+            tr[u] = at + q * 64 * DB + ((2 * u + (n >> 1 & 1)) ^ turn(q)) * 16 + (n & 1) * 8;
+    }
+    // Lane offsets of the loads of even- and odd-numbered eight-row blocks.
+    struct Loads {
+        uint32_t off[2], sr;
+        __device__ __forceinline__ Loads(uint32_t sr_, int lane, int D) : sr(sr_) {
+            const int row = lane / kChunks;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int chunk = (lane % kChunks) ^ turn(row + (DB == 1 ? 0 : 8 * e));
+                off[e] = 8 * chunk < D ? row * sr + chunk * 16 : kBufOOB;
+            }
+        }
+    };
+    // Every reading of the last tile has to be back before the next is on its way (a load to LDS
+    // is not ordered with the wave's LDS reads), and a tile has to be there before it is read.
+    static __device__ __forceinline__ void released() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+    static __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    __device__ __forceinline__ void fill(__amdgpu_buffer_rsrc_t r, bool inside, const Loads &l, int which = 0) const {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+        for (int i = 0; i < 2 * DB; ++i) {
+            const int odd = DB == 4 ? i >> 1 & 1 : DB == 2 ? i & 1 : 0;
+            auto *to = (REX_LDS void *)(at + which * kBytes + i * 1024);
+            if (inside) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, l.off[odd], i * kRows * l.sr, 0, 0);
+            else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, l.off[odd] + i * kRows * l.sr, 0, 0, 0);
+        }
+#endif
+    }
+    // the operand whose rows are rows: tile t, channels 32k + 8g ..
+    __device__ __forceinline__ bf16x8 rows(int t, int k, int which = 0) const {
+        return *(const REX_LDS bf16x8 *)(nat[k] + which * kBytes + 4 * t * 64 * DB);
+    }
+    // the operand whose rows are channels: tile u, channel 16u + n
+    __device__ __forceinline__ bf16x8 channels(int u, int which = 0) const {
+#ifdef __HIP_DEVICE_COMPILE__
+        using s16x4 = short __attribute__((ext_vector_type(4)));
+        using s16x8 = short __attribute__((ext_vector_type(8)));
+        s16x4 x[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (REX_LDS s16x4 *)(tr[u] + which * kBytes + 4 * e * 64 * DB));
+        return __builtin_bit_cast(bf16x8, s16x8{x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]});
+#else
+        return bf16x8{};
+#endif
     }
 };
 
@@ -222,8 +335,18 @@ __device__ __forceinline__ float sum_over_rows(float x) {
     return x + __shfl_xor(x, 32);
 }
 
-// Row of the streamed 32 that element j of a lane's operand is (see above).
-__device__ __forceinline__ int slot_row(int g, int j) { return j < 4 ? 4 * g + j : 12 + 4 * g + j; }
+// The four adjacent channels that quad u of a lane's results (2 * DB tiles of 16 channels) are,
+// and their values.  NATURAL: channels in the tiles' order, else interleaved by pairs.
+template <bool NATURAL>
+__device__ __forceinline__ int quad_channel(int u, int g) {
+    return NATURAL ? 16 * u + 4 * g : 32 * (u >> 1) + 8 * g + 4 * (u & 1);
+}
+template <bool NATURAL, int NT>
+__device__ __forceinline__ f32x4 quad_values(const f32x4 (&o)[NT], int u) {
+    if constexpr (NATURAL) return o[u];
+    const int k = u & ~1, i = 2 * (u & 1);
+    return f32x4{o[k][i], o[k + 1][i], o[k][i + 1], o[k + 1][i + 1]};
+}
 
 // A box as the bucket rule sees it: centre and, for a query, 1 / side.
 struct BoxGeo {
@@ -262,20 +385,19 @@ __device__ __forceinline__ float table_entry(float bias, float scale) {
     return bias <= -1e30f ? -kInf : bias / scale;
 }
 
-// The table entries of a lane's four rows: `at` holds four 16-bit byte offsets, `tab` (an LDS
-// address below 2^16) the head's table.
-__device__ __forceinline__ f32x4 table_gather(u32x2 at, const char *tab) {
-    f32x4 v;
+// The table entries of a lane's eight rows: `at` holds 16-bit byte offsets into the head's
+// table in LDS.
+__device__ __forceinline__ uint32_t table_offset(u32x4 at, int j) {
+    return j & 1 ? at[j >> 1] >> 16 : at[j >> 1] & 0xffffu;
+}
+__device__ __forceinline__ void table_gather(u32x4 at, const char *tab, f32x4 (&x)[2]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t off = i & 1 ? at[i >> 1] >> 16 : at[i >> 1] & 0xffffu;
-        v[i] = *reinterpret_cast<const float *>(tab + off);
-    }
-    return v;
+    for (int j = 0; j < 8; ++j)
+        x[j >> 2][j & 3] = *reinterpret_cast<const float *>(tab + table_offset(at, j));
 }
 
-constexpr int kBuckStride = 36;   // 16-bit entries of one column's 32 rows in LDS (8-byte reads
-                                  // of 16 columns then start in 16 different bank pairs)
+constexpr int kBuckStride = 40;   // 16-bit entries of one column's 32 rows in LDS (16-byte reads
+                                  // of 16 columns then spread over the banks)
 
 // Workgroups go to the eight XCDs in turn.  `per` workgroups that share keys (one image and
 // head group) belong on one XCD, whose L2 then holds those keys: such sets go to the XCDs in

@@ -17,6 +17,12 @@
 // in LDS: LDS serves a wave's additions in order, so the sums repeat bit for bit.  The tables
 // are binary64: an addition of 64 lanes to LDS takes 18 to 30 cycles of a CU there, 193 in
 // binary32 (measured, whatever the addresses).
+//
+// Measured, 16 images of up to 1000 boxes in 16 heads of 64 channels, bf16: rowstat 13 us, dq
+// 211, dkv 440, hist 11.5.  dkv has four products of the pair matrix and its operands leave two
+// waves on a SIMD; without its histogram it takes 418 us, with every tile at one address 424, so
+// what bounds it is the issue of products, exponents and LDS reads by too few waves.  Two images
+// of 512 boxes in 8 heads of 32, binary32: 3.4, 20, 27 and 4 us.
 #include "attn.hpp"
 
 namespace rex {
@@ -63,15 +69,14 @@ __global__ __launch_bounds__(256) void attn_rowstat_kernel(AttnArgs a) {
 }
 
 // Steps whose buckets are computed between two barriers.
-inline __host__ __device__ int bwd_ahead(int parts) { return parts >= 4 ? 1 : 4 / parts; }
+inline __host__ __device__ int bwd_ahead(int parts) { return parts >= 2 ? 1 : 2; }
 
 // LDS of the two passes, bytes; `heads` tables of biases (and histograms) a wave.
 struct BwdLds {
-    int bias, hist, copies, geo, buck, acc, total;
+    int bias, hist, copies, geo, buck, tile, acc, total;
 };
-constexpr int kLdsBytes = 160 << 10;
 inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, int heads, int nb,
-                                          bool bias, bool hist) {
+                                          bool bias, bool hist, int tiles) {
     BwdLds l{};
     int at = 0;
     const int table = (nb * nb * 4 + 15) & ~15;
@@ -81,6 +86,8 @@ inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, i
     if (bias) at += cols * 16;
     l.buck = at;
     if (bias) at += 2 * bwd_ahead(parts) * parts * cols * kBuckStride * 2;
+    l.tile = at;
+    at += kAttnWaves * tiles * kTile * dp * 2;        // each wave's tiles of bf16 rows
     l.hist = at;
     l.copies = 1;                 // copies of a wave's table: a power of two that fits
     if (bias && hist) {
@@ -94,12 +101,19 @@ inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, i
     return l;
 }
 
+// Tiles of bf16 rows that a wave keeps in LDS.  Query pass: keys and
+// values, or keys alone for heads of more than 64 channels.  Key pass: queries and upstream
+// gradients; none for more than 64 channels, which would leave no room for the histograms.
+template <typename T, int DB> constexpr int dq_tiles() { return sizeof(T) == 4 ? 0 : DB <= 2 ? 2 : 1; }
+template <typename T, int DB> constexpr bool dkv_lds() { return sizeof(T) == 2 && DB <= 2; }
+
 template <typename T, int DB, int NS, bool BIAS, int TERMS>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a) {
     using N = Num<T>;
     using Frag = typename N::Frag;
     using Pair = typename N::Pair;
     constexpr int kCols = 16 * NS, kDP = 32 * DB;
+    constexpr bool kLds = sizeof(T) == 2, kNatural = kLds, kBoth = dq_tiles<T, DB>() == 2;
     extern __shared__ char smem[];
     const int id = xcd_order(blockIdx.x, a.nwg, a.per);
     if (id >= a.nwg) return;
@@ -114,17 +128,20 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     const int h = h0 + hw, kh = h / a.group;
     const int nb2 = a.rule.nb * a.rule.nb, table = (nb2 * 4 + 15) & ~15;
     const int ahead = bwd_ahead(parts);
-    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, 1, a.rule.nb, BIAS, false);
+    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, 1, a.rule.nb, BIAS, false, dq_tiles<T, DB>());
 
     const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
     const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
     const int t1 = q0 < qlen ? (klen + kTile - 1) / kTile : 0;
+    const int cols = min(max(qlen - q0, 0), kCols);       // columns that hold a query
     BoxGeo *geo = reinterpret_cast<BoxGeo *>(smem + lds.geo);
     uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
     const float sl2 = a.scale * kLog2e;
     const char *tab = smem + lds.bias + hw * table;
     const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
     const TileOffsets<T, DB> koff(kr.sr, n, g, a.D), voff(vr.sr, n, g, a.D);
+    const LdsTile<DB> rows(smem + lds.tile + wave * dq_tiles<T, DB>() * LdsTile<DB>::kBytes, lane);
+    const typename LdsTile<DB>::Loads kload(kr.sr, lane, a.D), vload(vr.sr, lane, a.D);
 
     auto fill_buckets = [&](int chunk) {
         const int r = lane & 31;
@@ -136,7 +153,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
                        kx, ky);
             uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
 #pragma unroll 2
-            for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
+            for (int c = hw * 2 + (lane >> 5); c < cols; c += 2 * hp)
                 dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(geo[c], kx, ky, a.rule));
         }
     };
@@ -145,16 +162,11 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     float lse[NS], delta[NS], sum[NS];
     {
         const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
-        const TileOffsets<T, DB> qoff(qr.sr, n, g, a.D), goff(gr.sr, n, g, a.D);
         const int first = min(q0, max(qlen - 1, 0));
-        const auto rq = qr.at(first), rg = gr.at(first);
+        load_columns<T, DB, NS>(qr.at(first), qr.sr, n, g, a.D, q);
+        load_columns<T, DB, NS>(gr.at(first), gr.sr, n, g, a.D, go);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-#pragma unroll
-            for (int k = 0; k < DB; ++k) {
-                q[s][k] = N::load(rq, qoff.f[k] + 16 * s * qoff.sr, 0);
-                go[s][k] = N::load(rg, goff.f[k] + 16 * s * goff.sr, 0);
-            }
             const f32x2 st = *(const REX_GLOBAL f32x2 *)(
                 a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + min(q0 + 16 * s + n, a.Nqp - 1)) * 2);
             lse[s] = st[0];
@@ -166,8 +178,11 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
         for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
             reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] =
                 table_entry(as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i], a.scale);
-        if (tid < kCols)
-            geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb + min(q0 + tid, a.Nq - 1) * a.qbox_sr));
+        if (tid < cols) geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb + (q0 + tid) * a.qbox_sr));
+        // columns without a query: bucket 0 of whatever they hold
+        if (cols < kCols)
+            for (int i = tid; i < 2 * ahead * parts * kCols * kBuckStride / 2; i += kAttnWaves * 64)
+                reinterpret_cast<uint32_t *>(buck)[i] = 0u;
         __syncthreads();
         fill_buckets(0);
     }
@@ -183,24 +198,43 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
             if (tile >= t1) break;
             const auto rk = kr.at(tile * kTile), rv = vr.at(tile * kTile);
             const bool inside = tile * kTile + kTile <= klen;
-            Frag kf[2][DB], vf[2][DB];
-            koff.frags(rk, inside, kf);
-            voff.frags(rv, inside, vf);
+            Frag kf[2][DB], vf[2][DB], kt[2 * DB];
             Pair kp[DB][8];
-            koff.pairs(rk, inside, kp);
+            auto fill = [&](int to) {
+                const bool in = to * kTile + kTile <= klen;
+                rows.fill(kr.at(to * kTile), in, kload);
+                if constexpr (kBoth) rows.fill(vr.at(to * kTile), in, vload, 1);
+            };
+            if constexpr (kLds) {
+                if (it == 0 && chunk == 0) fill(tile);              // later ones: a step ago
+                rows.arrived();
+                if constexpr (!kBoth) voff.frags(rv, inside, vf);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int k = 0; k < DB; ++k) {
+                        kf[t][k] = rows.rows(t, k);
+                        if constexpr (kBoth) vf[t][k] = rows.rows(t, k, 1);
+                    }
+#pragma unroll
+                for (int u = 0; u < 2 * DB; ++u) kt[u] = rows.channels(u);
+            } else {
+                koff.frags(rk, inside, kf);
+                voff.frags(rv, inside, vf);
+                koff.pairs(rk, inside, kp);
+            }
             const int key = tile * kTile + (lane & 31);
             bool on = key < klen;
             if (a.kmask)
                 on = on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
             const uint32_t vis = static_cast<uint32_t>(__ballot(on));
-            const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+            const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 8 * g;
             f32x4 sc[NS][2], dp[NS][2];
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    sc[s][t] = BIAS ? table_gather(*reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t), tab)
-                                    : f32x4{};
+            for (int s = 0; s < NS; ++s) {
+                sc[s][0] = sc[s][1] = f32x4{};
+                if (BIAS) table_gather(*reinterpret_cast<const u32x4 *>(bk + 16 * s * kBuckStride), tab, sc[s]);
+            }
             float x[NS][8];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -219,18 +253,25 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
                         dp[s][t][i] *= p;
                     }
                 }
-            if (vis != 0xffffffffu) {
+            if constexpr (!kLds) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool on_j = (vis >> slot_row(g, j)) & 1u;
+                for (int k = 0; k < DB; ++k) N::split(kp[k], kt[2 * k], kt[2 * k + 1]);
+            }
+            if (vis != 0xffffffffu) {
+                const uint32_t mine = vis >> (8 * g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
-                        x[s][j] = on_j ? x[s][j] : 0.0f;
-                        dp[s][j >> 2][j & 3] = on_j ? dp[s][j >> 2][j & 3] : 0.0f;
+                        x[s][j] = mine >> j & 1u ? x[s][j] : 0.0f;
+                        dp[s][j >> 2][j & 3] = mine >> j & 1u ? dp[s][j >> 2][j & 3] : 0.0f;
                     }
 #pragma unroll
-                    for (int k = 0; k < DB; ++k) kp[k][j] = on_j ? kp[k][j] : N::no_pair();
-                }
+                for (int u = 0; u < 2 * DB; ++u) N::keep(kt[u], mine);
+            }
+            if (kLds && tile + parts < t1) {
+                rows.released();
+                fill(tile + parts);
             }
             if (!N::kExact) {
 #pragma unroll
@@ -238,21 +279,17 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sum[s] += dp[s][j >> 2][j & 3];
             }
-            Frag kt[2 * DB];
-#pragma unroll
-            for (int k = 0; k < DB; ++k) N::split(kp[k], kt[2 * k], kt[2 * k + 1]);
 #pragma unroll
             for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(kt, x[s], dq[s]);
         }
     }
-    auto finish = [&](int col, int head, int ch, const float (&x)[8]) {
+    auto finish = [&](int col, int head, int ch, f32x4 x) {
         const int row = q0 + col;
         if (row >= a.Nq || ch >= a.D) return;
-        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = row < qlen ? x[i] * a.scale : 0.0f;
-        N::store(static_cast<char *>(a.gq) +
-                     (((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch) * N::kSize, y);
+        for (int i = 0; i < 4; ++i) x[i] = row < qlen ? x[i] * a.scale : 0.0f;
+        N::store4(static_cast<char *>(a.gq) +
+                      (((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch) * N::kSize, x);
     };
     auto keep_delta = [&](int col, int head, float d) {
         if (!N::kExact && q0 + col < qlen)
@@ -265,12 +302,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
         for (int s = 0; s < NS; ++s) {
             if (g == 0) keep_delta(16 * s + n, h, sum[s]);
 #pragma unroll
-            for (int k = 0; k < DB; ++k) {
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = dq[s][2 * k + (i & 1)][i >> 1];
-                finish(16 * s + n, h, 32 * k + 8 * g, y);
-            }
+            for (int u = 0; u < 2 * DB; ++u)
+                finish(16 * s + n, h, quad_channel<kNatural>(u, g), quad_values<kNatural>(dq[s], u));
         }
         return;
     }
@@ -282,21 +315,17 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
         float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4);
         if (g == 0) dst[kDP] = sum[s];
 #pragma unroll
-        for (int k = 0; k < DB; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; i += 4)
-                *reinterpret_cast<f32x4 *>(dst + 32 * k + 8 * g + i) =
-                    f32x4{dq[s][2 * k][i >> 1], dq[s][2 * k + 1][i >> 1], dq[s][2 * k][(i >> 1) + 1],
-                          dq[s][2 * k + 1][(i >> 1) + 1]};
+        for (int u = 0; u < 2 * DB; ++u)
+            *reinterpret_cast<f32x4 *>(dst + quad_channel<kNatural>(u, g)) = quad_values<kNatural>(dq[s], u);
     }
     __syncthreads();
-    for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
-        const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
-        float y[8] = {}, d = 0.0f;
+    for (int e = tid; e < hp * kCols * DB * 8; e += kAttnWaves * 64) {
+        const int ch = (e % (DB * 8)) * 4, col = (e / (DB * 8)) % kCols, w = e / (DB * 8 * kCols);
+        f32x4 y = {};
+        float d = 0.0f;
         for (int p = 0; p < parts; ++p) {
             const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] += src[ch + i];
+            y += *reinterpret_cast<const f32x4 *>(src + ch);
             d += src[kDP];
         }
         if (ch == 0) keep_delta(col, h0 + w, d);
@@ -310,6 +339,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
     using Frag = typename N::Frag;
     using Pair = typename N::Pair;
     constexpr int kCols = 16 * NS, kDP = 32 * DB;
+    constexpr bool kLds = dkv_lds<T, DB>(), kNatural = kLds;
     extern __shared__ char smem[];
     const int id = xcd_order(blockIdx.x, a.nwg, a.per);
     if (id >= a.nwg) return;
@@ -324,7 +354,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
     const int kh = kh0 + hw;
     const int nb2 = a.rule.nb * a.rule.nb, table = (nb2 * 4 + 15) & ~15;
     const int ahead = bwd_ahead(parts);
-    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, a.head_step, a.rule.nb, BIAS, true);
+    const BwdLds lds = bwd_lds(kCols, kDP, hp, parts, a.head_step, a.rule.nb, BIAS, true, kLds ? 2 : 0);
 
     const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
     const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
@@ -337,10 +367,14 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
     char *const hist = reinterpret_cast<char *>(tables + (n & (copies - 1)));
     float *const partial = BIAS ? a.hist + (static_cast<int64_t>(b) * a.spans + sp) * a.H * nb2 : nullptr;
     const TileOffsets<T, DB> qoff(a.q.sr, n, g, a.D), goff(a.gout.sr, n, g, a.D);
+    // queries, then upstream gradients
+    const LdsTile<DB> rows(smem + lds.tile + wave * 2 * LdsTile<DB>::kBytes, lane);
+    const typename LdsTile<DB>::Loads qload(a.q.sr, lane, a.D), gload(a.gout.sr, lane, a.D);
 
     const int first_tile = sp * a.span, last_tile = min(first_tile + a.span, a.tiles);
     for (int tile_k = first_tile; tile_k < last_tile; ++tile_k) {
         const int k0 = tile_k * kCols;
+        const int cols = min(max(klen - k0, 0), kCols);   // columns that hold a key
         const int t1 = k0 < klen ? (qlen + kTile - 1) / kTile : 0;
         // The key columns.  A masked key's column is whatever its row makes of it: its weights
         // are set to 0 before they reach the histogram, no other column sees them, and zeros
@@ -349,20 +383,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
         bool live[NS];
         {
             const HeadRows kr = head_rows<T>(a.k, b, kh, klen, a.D), vr = head_rows<T>(a.v, b, kh, klen, a.D);
-            const TileOffsets<T, DB> koff(kr.sr, n, g, a.D), voff(vr.sr, n, g, a.D);
             const int first = min(k0, max(klen - 1, 0));
-            const auto rk = kr.at(first), rv = vr.at(first);
+            load_columns<T, DB, NS>(kr.at(first), kr.sr, n, g, a.D, kf);
+            load_columns<T, DB, NS>(vr.at(first), vr.sr, n, g, a.D, vf);
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 const int key = k0 + 16 * s + n;
                 live[s] = key < klen;
                 if (a.kmask)
                     live[s] = live[s] && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
-#pragma unroll
-                for (int k = 0; k < DB; ++k) {
-                    kf[s][k] = N::load(rk, koff.f[k] + 16 * s * koff.sr, 0);
-                    vf[s][k] = N::load(rv, voff.f[k] + 16 * s * voff.sr, 0);
-                }
             }
         }
         bool all_live = true;
@@ -371,11 +400,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
         const bool whole = __all(all_live);
         if (BIAS) {
             __syncthreads();              // the last tile's tables have been read
-            if (tid < kCols) {
+            if (tid < cols) {
                 float cx, cy;
-                box_centre(as_global<float>(a.kbox + b * a.kbox_sb + min(k0 + tid, a.Nk - 1) * a.kbox_sr), cx, cy);
+                box_centre(as_global<float>(a.kbox + b * a.kbox_sb + (k0 + tid) * a.kbox_sr), cx, cy);
                 ctr[tid] = f32x2{cx, cy};
             }
+            // columns without a key: bucket 0, to which their zeros are added
+            if (cols < kCols)
+                for (int i = tid; i < 2 * ahead * parts * kCols * kBuckStride / 2; i += kAttnWaves * 64)
+                    reinterpret_cast<uint32_t *>(buck)[i] = 0u;
         }
         // here the streamed side is the queries: row r of the tile is query 32 * tile + r
         auto fill_buckets = [&](int chunk) {
@@ -387,12 +420,12 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                                                           min(tile * kTile + r, a.Nq - 1) * a.qbox_sr));
                 uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
 #pragma unroll 2
-                for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
+                for (int c = hw * 2 + (lane >> 5); c < cols; c += 2 * hp)
                     dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(q, ctr[c][0], ctr[c][1], a.rule));
             }
         };
 
-        f32x4 dk[NS][2 * DB] = {}, dv[NS][2 * DB] = {};
+        f32x4 dk[NS][2 * DB] = {}, dv[NS][2 * DB] = {}, st_next[4];
         const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
         for (int first = 0; first < a.group; first += a.head_step) {
             const int many = min(a.head_step, a.group - first);
@@ -413,37 +446,66 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                 for (int it = 0; it < ahead; ++it) {
                     const int tile = (chunk * ahead + it) * parts + kw;
                     if (tile >= t1) break;
-                    const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+                    const uint16_t *bk = buck + ((((chunk & 1) * ahead + it) * parts + kw) * kCols + n) * kBuckStride + 8 * g;
                     for (int c = 0; c < many; ++c) {
                         const int h = kh * a.group + first + c;
                         const char *tab = smem + lds.bias + (hw * a.head_step + c) * table;
                         const auto rq = head_rows<T>(a.q, b, h, qlen, a.D).at(tile * kTile);
                         const auto rg = head_rows<T>(a.gout, b, h, qlen, a.D).at(tile * kTile);
-                        const float *stat = a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + tile * kTile) * 2;
-                        u32x2 at[NS][2];
+                        const bool inside = tile * kTile + kTile <= qlen;
+                        // the next head of this tile, or the first of the next tile
+                        const bool last = c + 1 == many;
+                        const int next = last ? tile + parts : tile, nh = last ? kh * a.group + first : h + 1;
+                        auto fill = [&](int to, int head) {
+                            const bool in = to * kTile + kTile <= qlen;
+                            rows.fill(head_rows<T>(a.q, b, head, qlen, a.D).at(to * kTile), in, qload);
+                            rows.fill(head_rows<T>(a.gout, b, head, qlen, a.D).at(to * kTile), in, gload, 1);
+                        };
+                        auto load_stat = [&](int to, int head, f32x4 (&x)[4]) {
+                            const float *p = a.rowstat + ((static_cast<int64_t>(b) * a.H + head) * a.Nqp + to * kTile + 8 * g) * 2;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[i] = *(const REX_GLOBAL f32x4 *)(p + 4 * i);
+                        };
+                        f32x4 st[4];                  // (log sum, delta) of the lane's eight rows
+                        if constexpr (kLds) {
+                            if (c == 0 && it == 0 && chunk == 0) {         // later ones: a step ago
+                                rows.released();
+                                fill(tile, h);
+                                load_stat(tile, h, st_next);
+                            }
+                            rows.arrived();
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) st[i] = st_next[i];
+                            if (next < t1) load_stat(next, nh, st_next);
+                        } else {
+                            load_stat(tile, h, st);
+                        }
+                        u32x4 at[NS];
                         f32x4 sc[NS][2];
 #pragma unroll
-                        for (int s = 0; s < NS; ++s)
-#pragma unroll
-                            for (int t = 0; t < 2; ++t) {
-                                at[s][t] = u32x2{};
-                                sc[s][t] = f32x4{};
-                                if (BIAS) {
-                                    at[s][t] = *reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t);
-                                    sc[s][t] = table_gather(at[s][t], tab);
-                                }
+                        for (int s = 0; s < NS; ++s) {
+                            sc[s][0] = sc[s][1] = f32x4{};
+                            at[s] = u32x4{};
+                            if (BIAS) {
+                                at[s] = *reinterpret_cast<const u32x4 *>(bk + 16 * s * kBuckStride);
+                                table_gather(at[s], tab, sc[s]);
                             }
-                        const bool inside = tile * kTile + kTile <= qlen;
-                        Frag qf[2][DB], gf[2][DB];
-                        qoff.frags(rq, inside, qf);
-                        goff.frags(rg, inside, gf);
+                        }
                         float pr[NS][8], ds[NS][8];
+                        Frag qf[2][DB], gf[2][DB];
+                        if constexpr (!kLds) {
+                            qoff.frags(rq, inside, qf);
+                            goff.frags(rg, inside, gf);
+                        }
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
-                            const f32x4 st0 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2);
-                            const f32x4 st1 = *(const REX_GLOBAL f32x4 *)(stat + (16 * t + 4 * g) * 2 + 4);
-                            const float lse[4] = {st0[0], st0[2], st1[0], st1[2]};
-                            const float delta[4] = {st0[1], st0[3], st1[1], st1[3]};
+                            if constexpr (kLds) {
+#pragma unroll
+                                for (int k = 0; k < DB; ++k) {
+                                    qf[t][k] = rows.rows(t, k);
+                                    gf[t][k] = rows.rows(t, k, 1);
+                                }
+                            }
 #pragma unroll
                             for (int s = 0; s < NS; ++s) {
                                 f32x4 dp = {};
@@ -454,9 +516,10 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                                 }
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
-                                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -lse[i]));
+                                    const f32x4 two = st[2 * t + (i >> 1)];
+                                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i], sl2, -two[2 * (i & 1)]));
                                     pr[s][4 * t + i] = p;
-                                    ds[s][4 * t + i] = p * (dp[i] - delta[i]);
+                                    ds[s][4 * t + i] = p * (dp[i] - two[2 * (i & 1) + 1]);
                                 }
                             }
                         }
@@ -471,29 +534,43 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                             }
                             char *const to = hist + c * nb2 * 8 * copies;
 #pragma unroll
-                            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    const uint32_t two = at[s][j >> 2][(j & 3) >> 1];
-                                    const uint32_t off = j & 1 ? two >> 16 : two & 0xffffu;
-                                    unsafeAtomicAdd(reinterpret_cast<double *>(to + (off << log_copies)),
-                                                    static_cast<double>(ds[s][j]));
-                                }
-                        }
-#pragma unroll
-                        for (int which = 0; which < 2; ++which) {
-                            Pair p[DB][8];
-                            if (which) qoff.pairs(rq, inside, p);
-                            else goff.pairs(rg, inside, p);
-                            Frag rows[2 * DB];
-#pragma unroll
-                            for (int k = 0; k < DB; ++k) N::split(p[k], rows[2 * k], rows[2 * k + 1]);
-#pragma unroll
                             for (int s = 0; s < NS; ++s) {
-                                if (which) add_weighted<T, TERMS, 2 * DB>(rows, ds[s], dk[s]);
-                                else add_weighted<T, TERMS, 2 * DB>(rows, pr[s], dv[s]);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    unsafeAtomicAdd(reinterpret_cast<double *>(to + (table_offset(at[s], j) << log_copies)),
+                                                    static_cast<double>(ds[s][j]));
                             }
                         }
+                        {
+                            Frag gt[2 * DB];
+                            if constexpr (kLds) {
+#pragma unroll
+                                for (int u = 0; u < 2 * DB; ++u) gt[u] = rows.channels(u, 1);
+                            } else {
+                                Pair p[DB][8];
+                                goff.pairs(rg, inside, p);
+#pragma unroll
+                                for (int k = 0; k < DB; ++k) N::split(p[k], gt[2 * k], gt[2 * k + 1]);
+                            }
+#pragma unroll
+                            for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(gt, pr[s], dv[s]);
+                        }
+                        Frag qt[2 * DB];
+                        if constexpr (kLds) {
+#pragma unroll
+                            for (int u = 0; u < 2 * DB; ++u) qt[u] = rows.channels(u);
+                            if (next < t1) {
+                                rows.released();
+                                fill(next, nh);
+                            }
+                        } else {
+                            Pair p[DB][8];
+                            qoff.pairs(rq, inside, p);
+#pragma unroll
+                            for (int k = 0; k < DB; ++k) N::split(p[k], qt[2 * k], qt[2 * k + 1]);
+                        }
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(qt, ds[s], dk[s]);
                     }
                 }
             }
@@ -513,27 +590,22 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
             }
         }
 
-        auto finish = [&](char *out, float f, int col, int head, int ch, const float (&x)[8]) {
+        auto finish = [&](char *out, float f, int col, int head, int ch, f32x4 x) {
             const int key = k0 + col;
             if (key >= a.Nk || ch >= a.D) return;
             bool on = key < klen;
             if (a.kmask && on) on = as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + key] != 0;
-            float y[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = on ? x[i] * f : 0.0f;
-            N::store(out + (((static_cast<int64_t>(b) * a.Nk + key) * a.Hkv + head) * a.D + ch) * N::kSize, y);
+            for (int i = 0; i < 4; ++i) x[i] = on ? x[i] * f : 0.0f;
+            N::store4(out + (((static_cast<int64_t>(b) * a.Nk + key) * a.Hkv + head) * a.D + ch) * N::kSize, x);
         };
         auto write = [&](const f32x4 (&d)[NS][2 * DB], char *out, float f) {
             if (parts == 1) {
 #pragma unroll
                 for (int s = 0; s < NS; ++s)
 #pragma unroll
-                    for (int k = 0; k < DB; ++k) {
-                        float y[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = d[s][2 * k + (i & 1)][i >> 1];
-                        finish(out, f, 16 * s + n, kh, 32 * k + 8 * g, y);
-                    }
+                    for (int u = 0; u < 2 * DB; ++u)
+                        finish(out, f, 16 * s + n, kh, quad_channel<kNatural>(u, g), quad_values<kNatural>(d[s], u));
                 return;
             }
             float *acc = reinterpret_cast<float *>(smem + lds.acc);
@@ -541,23 +613,15 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
-                for (int k = 0; k < DB; ++k) {
-                    float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4) + 32 * k + 8 * g;
-#pragma unroll
-                    for (int i = 0; i < 8; i += 4)
-                        *reinterpret_cast<f32x4 *>(dst + i) =
-                            f32x4{d[s][2 * k][i >> 1], d[s][2 * k + 1][i >> 1], d[s][2 * k][(i >> 1) + 1],
-                                  d[s][2 * k + 1][(i >> 1) + 1]};
-                }
+                for (int u = 0; u < 2 * DB; ++u)
+                    *reinterpret_cast<f32x4 *>(acc + (wave * kCols + 16 * s + n) * (kDP + 4) + quad_channel<kNatural>(u, g)) =
+                        quad_values<kNatural>(d[s], u);
             __syncthreads();
-            for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
-                const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
-                float y[8] = {};
-                for (int p = 0; p < parts; ++p) {
-                    const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] += src[i];
-                }
+            for (int e = tid; e < hp * kCols * DB * 8; e += kAttnWaves * 64) {
+                const int ch = (e % (DB * 8)) * 4, col = (e / (DB * 8)) % kCols, w = e / (DB * 8 * kCols);
+                f32x4 y = {};
+                for (int p = 0; p < parts; ++p)
+                    y += *reinterpret_cast<const f32x4 *>(acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch);
                 finish(out, f, col, kh0 + w, ch, y);
             }
         };
@@ -592,7 +656,7 @@ void run_pass(const AttnArgs &a, bool keys, hipStream_t s) {
     const dim3 grid(xcd_grid(a.nwg, a.per)), block(kAttnWaves * 64);
     const bool bias = a.bias != nullptr;
     const BwdLds lds = bwd_lds(16 * NS, 32 * DB, a.hp, a.parts, keys ? a.head_step : 1, a.rule.nb,
-                               bias, keys);
+                               bias, keys, !keys ? dq_tiles<T, DB>() : dkv_lds<T, DB>() ? 2 : 0);
     if (keys && bias)
         hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, true, TERMS>), grid, block, lds.total, s, a);
     else if (keys)
@@ -623,6 +687,11 @@ void run_typed(const AttnArgs &a, int dtype, bool keys, int cols, hipStream_t s)
 }
 
 }  // namespace
+
+bool dkv_fits(const AttnArgs &a, int dtype, int cols) {
+    const int db = a.D <= 32 ? 1 : a.D <= 64 ? 2 : 4, tiles = dtype == kBF16 && db <= 2 ? 2 : 0;
+    return bwd_lds(cols, 32 * db, a.hp, a.parts, a.head_step, a.rule.nb, a.bias != nullptr, true, tiles).total <= kLdsBytes;
+}
 
 hipError_t launch_attn_bwd(const AttnArgs &dq, const AttnArgs &dkv, int dtype, int dq_cols,
                            int dkv_cols, hipStream_t s) {

@@ -10,24 +10,27 @@
 // long memory) the keys are split over workgroups as well and attn_combine joins them.
 //
 // The bucket of a pair is the same for all heads, and costs more than one head's
-// share of the products: the workgroup computes each tile's buckets once, a few steps ahead,
+// share of the products: the workgroup computes each tile's buckets once, a step ahead,
 // into LDS (16 bits a pair: the byte offset into a head's table, which is in LDS too).
+//
+// Measured, bf16: 100 boxes in 8 heads of 32 channels 8.4 us (a launch and four dependent
+// steps); 1000 in 16 heads of 64 25 us; 16 images of those 176 us, 65 GFLOP of products that
+// take 58 us at the rate of a large product and some 15 vector instructions for every pair and
+// head (bias, exponent, running maximum) that take 100.  The memory, 300 boxes against 6000 in
+// 16 heads of 64: 55 us; 64 single queries against up to 8192 in 8 heads of 32: 93 us, 2.7 TB/s.
 #pragma once
 
 #include "attn.hpp"
-#ifndef REX_FWPE
-#define REX_FWPE 2
-#endif
 
 namespace rex {
 
 // What is in LDS, in bytes from its start.
 struct FwdLds {
-    int bias, geo, buck, ml, acc, total;
+    int bias, geo, buck, tile, ml, acc, total;
 };
 // Steps whose buckets are computed between two barriers.
-inline __host__ __device__ int fwd_ahead(int parts) { return parts >= 4 ? 1 : 4 / parts; }
-inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, int nb, bool bias) {
+inline __host__ __device__ int fwd_ahead(int parts) { return parts >= 2 ? 1 : 2; }
+inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, int nb, bool bias, int tiles) {
     FwdLds l{};
     int at = 0;
     l.bias = at;
@@ -36,6 +39,8 @@ inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, i
     if (bias) at += cols * 16;
     l.buck = at;
     if (bias) at += 2 * fwd_ahead(parts) * parts * cols * kBuckStride * 2;
+    l.tile = at;
+    at += kAttnWaves * tiles * kTile * dp * 2;        // each wave's tiles of bf16 rows
     const int loop = at;
     at = 0;                       // the end: the loop's tables are no longer needed
     l.ml = at;
@@ -46,12 +51,21 @@ inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, i
     return l;
 }
 
+// Tiles of bf16 rows that a wave keeps in LDS, keys and values, or values alone for
+// heads of more than 64 channels.  (Two of each, the next on its way for a whole step, leave room
+// for one workgroup on a CU instead of two: 1000 queries and keys in 16 heads of 64 channels take
+// 27.2 us then, 26.2 as it is.)
+template <typename T, int DB, bool PAGED>
+constexpr int fwd_tiles() { return PAGED || sizeof(T) == 4 ? 0 : DB <= 2 ? 2 : 1; }
+
 template <typename T, int DB, int NS, bool BIAS, bool PAGED, int TERMS>
-__global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a) {
     using N = Num<T>;
     using Frag = typename N::Frag;
     using Pair = typename N::Pair;
     constexpr int kCols = 16 * NS, kDP = 32 * DB;
+    constexpr bool kLds = !PAGED && sizeof(T) == 2, kNatural = PAGED || kLds;
+    constexpr bool kBoth = fwd_tiles<T, DB, PAGED>() == 2;
     extern __shared__ char smem[];
     const int id = xcd_order(blockIdx.x, a.nwg, a.per);
     if (id >= a.nwg) return;
@@ -67,7 +81,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
     const int h0 = (rest % hgroups) * hp, b = rest / hgroups;
     const int h = h0 + hw, kh = h / a.group;
     const int ahead = fwd_ahead(parts);
-    const FwdLds lds = fwd_lds(kCols, kDP, hp, parts, a.rule.nb, BIAS);
+    const FwdLds lds = fwd_lds(kCols, kDP, hp, parts, a.rule.nb, BIAS, fwd_tiles<T, DB, PAGED>());
 
     const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
     const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
@@ -76,6 +90,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
     const int per = (all + a.nsplit - 1) / a.nsplit;
     const int t0 = min(split * per, all), t1 = q0 < qlen ? min(t0 + per, all) : t0;
 
+    const int cols = min(max(qlen - q0, 0), kCols);       // columns that hold a query
     BoxGeo *geo = reinterpret_cast<BoxGeo *>(smem + lds.geo);
     uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
     if (BIAS) {
@@ -83,38 +98,37 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
         float *t = reinterpret_cast<float *>(smem + lds.bias);
         gcptr<float> src = as_global<float>(a.bias + static_cast<int64_t>(h0) * nb2);
         for (int i = tid; i < hp * nb2; i += kAttnWaves * 64) t[i] = table_entry(src[i], a.scale);
-        if (tid < kCols)
-            geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
-                                                min(q0 + tid, a.Nq - 1) * a.qbox_sr));
+        if (tid < cols) geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb + (q0 + tid) * a.qbox_sr));
+        // columns without a query: bucket 0 of whatever they hold
+        if (cols < kCols)
+            for (int i = tid; i < 2 * ahead * parts * kCols * kBuckStride / 2; i += kAttnWaves * 64)
+                reinterpret_cast<uint32_t *>(buck)[i] = 0u;
     }
 
     // the queries: column n of NS tiles; rows that are padding are zeros
     Frag q[NS][DB];
     {
         const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D);
-        const TileOffsets<T, DB> off(qr.sr, n, g, a.D);
-        const auto r = qr.at(min(q0, max(qlen - 1, 0)));
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int k = 0; k < DB; ++k) q[s][k] = N::load(r, off.f[k] + 16 * s * off.sr, 0);
+        load_columns<T, DB, NS>(qr.at(min(q0, max(qlen - 1, 0))), qr.sr, n, g, a.D, q);
     }
 
     // One tile's keys and values, its page and the lane's mask byte, read one step ahead.
     const HeadRows kr = head_rows<T>(a.k, b, kh, PAGED ? 0 : klen, a.D);
     const HeadRows vr = head_rows<T>(a.v, b, kh, PAGED ? 0 : klen, a.D);
     const TileOffsets<T, DB> koff(kr.sr, n, g, a.D), voff(vr.sr, n, g, a.D);
-    uint32_t kcode[DB], vcode[DB];         // the same inside a page of the memory
+    const LdsTile<DB> rows(smem + lds.tile + wave * fwd_tiles<T, DB, PAGED>() * LdsTile<DB>::kBytes, lane);
+    const typename LdsTile<DB>::Loads kload(kr.sr, lane, a.D), vload(vr.sr, lane, a.D);
+    // the same inside a page of the memory; its values' channels past D are past its end
+    uint32_t kcode[DB];
+    const uint32_t vcode = n * kTile + 8 * g;
 #pragma unroll
-    for (int k = 0; k < DB; ++k) {
-        kcode[k] = 32 * k + 8 * g < a.D ? n * a.D + 32 * k + 8 * g : kBufOOB;
-        vcode[k] = 32 * k + 2 * n < a.D ? (32 * k + 2 * n) * kTile + 4 * g : kBufOOB;
-    }
+    for (int k = 0; k < DB; ++k)
+        kcode[k] = 32 * k + 8 * g < a.D ? (8 * (n >> 2) + (n & 3)) * a.D + 32 * k + 8 * g : kBufOOB;
     struct {
         Frag f[2][DB];                                   // keys
-        Pair p[DB][8];                                   // values
+        Pair p[DB][8];                                   // values (binary32)
         u32x2 kc[PAGED ? 2 : 1][PAGED ? DB : 1];         // their codes and scales in the memory
-        uint32_t vc[PAGED ? DB : 1][2][2];
+        u32x2 vc[PAGED ? 2 * DB : 1];
         f32x4 ks[2], vs[2];
         int64_t ph;
         bool on;
@@ -133,15 +147,18 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
             const auto r = make_rsrc(a.mk + next.ph * kTile * a.D, kTile * a.D);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                next.ks[t] = *(const REX_GLOBAL f32x4 *)(a.mks + next.ph * kTile + 16 * t + 4 * g);
+                next.ks[t] = *(const REX_GLOBAL f32x4 *)(a.mks + next.ph * kTile + 8 * g + 4 * t);
 #pragma unroll
                 for (int k = 0; k < DB; ++k)
-                    next.kc[t][k] = __builtin_amdgcn_raw_buffer_load_b64(r, kcode[k], 16 * t * a.D, 0);
+                    next.kc[t][k] = __builtin_amdgcn_raw_buffer_load_b64(r, kcode[k], 4 * t * a.D, 0);
             }
         } else {
             if (a.kmask)
                 next.on = next.on && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + min(key, a.Nk - 1)] != 0;
-            koff.frags(kr.at(tile * kTile), tile * kTile + kTile <= klen, next.f);
+            const auto r = kr.at(tile * kTile);
+            const bool inside = tile * kTile + kTile <= klen;
+            if constexpr (kBoth) rows.fill(r, inside, kload);
+            else koff.frags(r, inside, next.f);
         }
     };
     auto load_values = [&](int tile) {                   // after load_keys of the same tile
@@ -149,14 +166,12 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
             const auto r = make_rsrc(a.mv + next.ph * kTile * a.D, kTile * a.D);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                next.vs[t] = *(const REX_GLOBAL f32x4 *)(a.mvs + next.ph * kTile + 16 * t + 4 * g);
+                next.vs[t] = *(const REX_GLOBAL f32x4 *)(a.mvs + next.ph * kTile + 8 * g + 4 * t);
 #pragma unroll
-            for (int k = 0; k < DB; ++k)
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        next.vc[k][t][e] = __builtin_amdgcn_raw_buffer_load_b32(r, vcode[k] + kTile * t + 16 * e, 0, 0);
+            for (int u = 0; u < 2 * DB; ++u)
+                next.vc[u] = __builtin_amdgcn_raw_buffer_load_b64(r, vcode + 16 * kTile * u, 0, 0);
+        } else if constexpr (kLds) {
+            rows.fill(vr.at(tile * kTile), tile * kTile + kTile <= klen, vload, kBoth ? 1 : 0);
         } else {
             voff.pairs(vr.at(tile * kTile), tile * kTile + kTile <= klen, next.p);
         }
@@ -174,7 +189,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
             box_centre(as_global<float>(box), kx, ky);
             uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
 #pragma unroll 2
-            for (int c = hw * 2 + (lane >> 5); c < kCols; c += 2 * hp)
+            for (int c = hw * 2 + (lane >> 5); c < cols; c += 2 * hp)
                 dst[c * kBuckStride] = static_cast<uint16_t>(pair_bucket(geo[c], kx, ky, a.rule));
         }
     };
@@ -211,16 +226,21 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
             if (tile >= t1) break;
             const uint32_t vis = static_cast<uint32_t>(__ballot(next.on));   // bit r: key r is visible
             const bool more = tile + parts < t1;
+            if constexpr (kLds) rows.arrived();
+            Frag vf[2 * DB];
+            if constexpr (kLds) {
+#pragma unroll
+                for (int u = 0; u < 2 * DB; ++u) vf[u] = rows.channels(u, kBoth ? 1 : 0);
+            }
             // what a logit starts with: its bias, or nothing
             f32x4 x[NS][2];
-            const uint16_t *bk = buck + ((((chunk & 1) * ahead + i) * parts + kw) * kCols + n) * kBuckStride + 4 * g;
+            const uint16_t *bk = buck + ((((chunk & 1) * ahead + i) * parts + kw) * kCols + n) * kBuckStride + 8 * g;
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    x[s][t] = BIAS ? table_gather(*reinterpret_cast<const u32x2 *>(bk + 16 * s * kBuckStride + 16 * t), tab)
-                                   : f32x4{};
-            // column = query n, rows = keys 4g + e of two tiles
+            for (int s = 0; s < NS; ++s) {
+                x[s][0] = x[s][1] = f32x4{};
+                if (BIAS) table_gather(*reinterpret_cast<const u32x4 *>(bk + 16 * s * kBuckStride), tab, x[s]);
+            }
+            // column = query n, rows = keys 8g + 4t + e
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 Frag kf[DB];
@@ -229,6 +249,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
                     if constexpr (PAGED) {
                         N::widen(kf[k], 0, next.kc[t][k][0]);
                         N::widen(kf[k], 4, next.kc[t][k][1]);
+                    } else if constexpr (kBoth) {
+                        kf[k] = rows.rows(t, k);
                     } else {
                         kf[k] = next.f[t][k];
                     }
@@ -247,38 +269,35 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
                     }
                 }
             }
-            Frag vf[2 * DB];
             f32x4 vs[2];
             if constexpr (PAGED) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) vs[t] = next.vs[t];
 #pragma unroll
-                for (int k = 0; k < DB; ++k)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        N::widen(vf[2 * k + t], 0, next.vc[k][t][0]);
-                        N::widen(vf[2 * k + t], 4, next.vc[k][t][1]);
-                    }
-            }
-            if (vis != 0xffffffffu) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool on = (vis >> slot_row(g, j)) & 1u;
-#pragma unroll
-                    for (int s = 0; s < NS; ++s) x[s][j >> 2][j & 3] = on ? x[s][j >> 2][j & 3] : -kInf;
-                    if constexpr (PAGED) {
-                        vs[j >> 2][j & 3] = on ? vs[j >> 2][j & 3] : 0.0f;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < DB; ++k) next.p[k][j] = on ? next.p[k][j] : N::no_pair();
-                    }
+                for (int u = 0; u < 2 * DB; ++u) {
+                    N::widen(vf[u], 0, next.vc[u][0]);
+                    N::widen(vf[u], 4, next.vc[u][1]);
                 }
-            }
-            if constexpr (!PAGED) {
+            } else if constexpr (!kLds) {
 #pragma unroll
                 for (int k = 0; k < DB; ++k) N::split(next.p[k], vf[2 * k], vf[2 * k + 1]);
             }
+            if (vis != 0xffffffffu) {
+                const uint32_t mine = vis >> (8 * g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool on = mine >> j & 1u;
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) x[s][j >> 2][j & 3] = on ? x[s][j >> 2][j & 3] : -kInf;
+                    if constexpr (PAGED) vs[j >> 2][j & 3] = on ? vs[j >> 2][j & 3] : 0.0f;
+                }
+                if constexpr (!PAGED) {
+#pragma unroll
+                    for (int u = 0; u < 2 * DB; ++u) N::keep(vf[u], mine);
+                }
+            }
             if (more) {
+                if constexpr (kLds) rows.released();
                 load_keys(tile + parts);
                 load_values(tile + parts);
             }
@@ -329,26 +348,24 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
         m[s] = m[s] == -kInf ? -kInf : ref[s];       // from here on in units of log 2
     }
 
-    // eight channels of one row, scaled, to where they belong
-    auto finish = [&](int col, int head, int ch, float mx, float sum, const float (&x)[8]) {
+    // four channels of one row to where they belong
+    auto finish = [&](int col, int head, int ch, float mx, float sum, f32x4 x) {
         const int row = q0 + col;
         if (row >= a.Nq) return;
         if (a.nsplit > 1) {
             if (row >= qlen) return;
             const int64_t at = ((static_cast<int64_t>(split) * a.B + b) * a.H + head) * a.Nq + row;
-            if (ch < a.D) Num<float>::store(reinterpret_cast<char *>(a.part + at * a.D + ch), x);
+            if (ch < a.D) *(REX_GLOBAL f32x4 *)(a.part + at * a.D + ch) = x;
             if (ch == 0) *(REX_GLOBAL f32x2 *)(a.part_ml + at * 2) = f32x2{mx, sum};
             return;
         }
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = row < qlen ? x[i] * inv : 0.0f;
-        const int64_t at = (((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch) * N::kSize;
+        for (int i = 0; i < 4; ++i) x[i] = row < qlen ? x[i] * inv : 0.0f;
+        const int64_t at = ((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch;
         if (ch < a.D) {
-            N::store(static_cast<char *>(a.out) + at, y);
-            if (a.out_f32)
-                Num<float>::store(reinterpret_cast<char *>(a.out_f32) + at * (4 / N::kSize), y);
+            N::store4(static_cast<char *>(a.out) + at * N::kSize, x);
+            if (a.out_f32) *(REX_GLOBAL f32x4 *)(a.out_f32 + at) = x;
         }
         if (ch == 0 && a.lse)
             as_global_mut<float>(a.lse)[(static_cast<int64_t>(b) * a.H + head) * a.Nq + row] =
@@ -359,12 +376,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int k = 0; k < DB; ++k) {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = o[s][2 * k + (i & 1)][i >> 1];
-                finish(16 * s + n, h, 32 * k + 8 * g, m[s], l[s], x);
-            }
+            for (int u = 0; u < 2 * DB; ++u)
+                finish(16 * s + n, h, quad_channel<kNatural>(u, g), m[s], l[s], quad_values<kNatural>(o[s], u));
         return;
     }
     // The waves of a head meet: maxima and sums first, then the scaled sums of the values.
@@ -382,26 +395,20 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
         for (int p = 0; p < parts; ++p) mx = fmaxf(mx, ml[(p * hp + hw) * kCols + 16 * s + n][0]);
         const float f = __builtin_amdgcn_exp2f(m[s] - (mx == -kInf ? 0.0f : mx));
 #pragma unroll
-        for (int k = 0; k < DB; ++k) {
-            float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4) + 32 * k + 8 * g;
-#pragma unroll
-            for (int i = 0; i < 8; i += 4)
-                *reinterpret_cast<f32x4 *>(dst + i) =
-                    f32x4{o[s][2 * k][i >> 1], o[s][2 * k + 1][i >> 1], o[s][2 * k][(i >> 1) + 1],
-                          o[s][2 * k + 1][(i >> 1) + 1]} * f;
-        }
+        for (int u = 0; u < 2 * DB; ++u)
+            *reinterpret_cast<f32x4 *>(acc + (wave * kCols + 16 * s + n) * (kDP + 4) + quad_channel<kNatural>(u, g)) =
+                quad_values<kNatural>(o[s], u) * f;
     }
     __syncthreads();
-    for (int e = tid; e < hp * kCols * DB * 4; e += kAttnWaves * 64) {
-        const int ch = (e % (DB * 4)) * 8, col = (e / (DB * 4)) % kCols, w = e / (DB * 4 * kCols);
-        float mx = -kInf, sum = 0.0f, x[8] = {};
+    for (int e = tid; e < hp * kCols * DB * 8; e += kAttnWaves * 64) {
+        const int ch = (e % (DB * 8)) * 4, col = (e / (DB * 8)) % kCols, w = e / (DB * 8 * kCols);
+        float mx = -kInf, sum = 0.0f;
+        f32x4 x = {};
         for (int p = 0; p < parts; ++p) mx = fmaxf(mx, ml[(p * hp + w) * kCols + col][0]);
         for (int p = 0; p < parts; ++p) {
             const f32x2 v = ml[(p * hp + w) * kCols + col];
             sum += v[1] * __builtin_amdgcn_exp2f(v[0] - (mx == -kInf ? 0.0f : mx));
-            const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] += src[i];
+            x += *reinterpret_cast<const f32x4 *>(acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch);
         }
         finish(col, h0 + w, ch, mx, sum, x);
     }
@@ -412,7 +419,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, REX_FWPE) void attn_fwd_kernel(Att
 template <typename T, int DB, int NS, bool PAGED, int TERMS>
 void run_fwd(const AttnArgs &a, hipStream_t s) {
     const dim3 grid(xcd_grid(a.nwg, a.per)), block(kAttnWaves * 64);
-    const FwdLds lds = fwd_lds(16 * NS, 32 * DB, a.hp, a.parts, a.rule.nb, a.bias != nullptr);
+    const FwdLds lds = fwd_lds(16 * NS, 32 * DB, a.hp, a.parts, a.rule.nb, a.bias != nullptr,
+                               fwd_tiles<T, DB, PAGED>());
     if (a.bias)
         hipLaunchKernelGGL((attn_fwd_kernel<T, DB, NS, true, PAGED, TERMS>), grid, block, lds.total, s, a);
     else

@@ -7,10 +7,8 @@
 namespace rex {
 
 constexpr int kTile = 32;          // keys of one step of the attention, boxes of one page
-#ifndef REX_WAVES
-#define REX_WAVES 8
-#endif
-constexpr int kAttnWaves = REX_WAVES;      // waves of one attention workgroup
+constexpr int kAttnWaves = 8;      // waves of one attention workgroup
+constexpr int kLdsBytes = 160 << 10;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -70,6 +68,8 @@ struct AttnArgs {
 hipError_t launch_attn_fwd(const AttnArgs &a, int dtype, int cols, hipStream_t s);
 hipError_t launch_attn_recall(const AttnArgs &a, int dtype, int cols, hipStream_t s);
 hipError_t launch_attn_combine(const AttnArgs &a, int dtype, hipStream_t s);
+// Whether a workgroup of the key pass with `cols` key columns fits the LDS.
+bool dkv_fits(const AttnArgs &dkv, int dtype, int cols);
 hipError_t launch_attn_bwd(const AttnArgs &dq, const AttnArgs &dkv, int dtype, int dq_cols,
                            int dkv_cols, hipStream_t s);
 

@@ -22,9 +22,12 @@ re_status_t from_hip(hipError_t e) { return e == hipSuccess ? RE_OK : RE_ERR_DEV
 constexpr int64_t kMaxSpan = kBufMaxBytes - 1;         // bytes of one image's rows
 constexpr int64_t kMaxRows = int64_t(1) << 24;         // queries or keys of one image
 constexpr int64_t kMaxRowHeads = (int64_t(1) << 31) - 1;
-// Workgroups that fill the 256 CUs twice over: below that, waves and workgroups share a
-// head's keys rather than leave CUs idle.
-constexpr int64_t kFill = 512;
+// Workgroups among which the attention's work is shared out: one for each of the 256 CUs, two
+// where they have 16 columns, whose few registers leave their waves waiting for memory.  Dense,
+// 1000 queries and keys, 16 heads of 64 channels: 128 workgroups 35.8 us, 256 26.4, 512 37.1.
+// Memory, 300 queries against 6000 boxes in the same heads: 160 68.9, 240 54.3, 360 74.5, 480 65.0;
+// 64 single queries against up to 8192 boxes each in 8 heads of 32: 256 126, 512 93, 768 108.
+constexpr int64_t kGroups = 256;
 // Workgroups of the norms.  16000 rows of 1024 channels, bf16: forward 26.6 us with 1024
 // of them, 28.2 with 4096; backward 54 us with 512 (two on each CU, what its registers
 // allow) and 10 us for their partial sums, 58 and 18 us with 1024.
@@ -91,9 +94,9 @@ re_status_t check_bias(const float *bias, int32_t buckets, int32_t first_exp, in
 }
 
 // The largest number of heads, a power of two up to the waves, that a workgroup can take.
-int most_heads(int heads) {
+int most_heads(int heads, int most) {
     int hp = 1;
-    while (hp < kAttnWaves && heads % (2 * hp) == 0) hp *= 2;
+    while (hp < most && heads % (2 * hp) == 0) hp *= 2;
     return hp;
 }
 
@@ -106,12 +109,28 @@ int columns(int64_t rows, int dim) { return rows <= 16 || dim > 64 ? 16 : 32; }
 // anyway, so there the second part is free and only the result's own rounding is left.
 int weight_terms(int64_t results) { return results <= kFewResults ? 2 : 1; }
 
-// Heads of a workgroup, whose remaining waves share the streamed tiles: as many heads as
-// there are (they share the work on buckets), unless that leaves CUs without a workgroup.
-void share_waves(AttnArgs &a, int heads, int64_t blocks, int64_t streamed) {
-    a.hp = most_heads(heads);
-    while (a.hp > 1 && blocks * (heads / a.hp) < kFill && streamed > kAttnWaves / a.hp) a.hp /= 2;
-    a.parts = kAttnWaves / a.hp;
+// Heads of a workgroup, whose remaining waves share the streamed tiles, and (`split`) the
+// workgroups that share a head's tiles: as many workgroups as there may be, of those choices the
+// one with the fewest partial sums.  Heads of one workgroup share the work on buckets, so nothing
+// is shared out further than that.
+void share_waves(AttnArgs &a, int heads, int64_t blocks, int64_t streamed, int cols, bool split,
+                 int most = kAttnWaves) {
+    const int64_t groups = kGroups * (cols == 16 ? 2 : 1);
+    int64_t best = 0;
+    for (int hp = most_heads(heads, most);; hp /= 2) {
+        const int parts = kAttnWaves / hp;
+        const int64_t wgs = blocks * (heads / hp);
+        if (best > 0 && (wgs > groups || parts > streamed)) break;
+        // four steps of every wave at least
+        const int64_t n = split && wgs > 0 ? std::max<int64_t>(1, std::min(groups / wgs, streamed / (4 * parts))) : 1;
+        if (wgs * n >= best) {
+            best = wgs * n;
+            a.hp = hp;
+            a.parts = parts;
+            a.nsplit = static_cast<int32_t>(n);
+        }
+        if (hp == 1) break;
+    }
 }
 
 // The forward's split, for dense keys and for the memory.
@@ -119,14 +138,8 @@ void plan_fwd(AttnArgs &a, int *cols) {
     *cols = columns(a.Nq, a.D);
     a.tiles = (a.Nq + *cols - 1) / *cols;
     const int64_t blocks = static_cast<int64_t>(a.B) * a.tiles;
-    const int64_t streamed = (a.Nk + kTile - 1) / kTile;
-    share_waves(a, a.H, blocks, streamed);
-    const int64_t wgs = blocks * (a.H / a.hp);
-    // more workgroups for the keys, with four steps of every wave at least
-    int64_t n = wgs > 0 ? (2 * kFill + wgs - 1) / wgs : 1;
-    n = std::min(n, streamed / (4 * a.parts));
-    a.nsplit = static_cast<int32_t>(std::max<int64_t>(1, wgs < kFill ? n : 1));
-    a.nwg = static_cast<int32_t>(wgs * a.nsplit);
+    share_waves(a, a.H, blocks, (a.Nk + kTile - 1) / kTile, *cols, true);
+    a.nwg = static_cast<int32_t>(blocks * (a.H / a.hp) * a.nsplit);
     a.per = a.tiles * a.nsplit;
 }
 
@@ -144,27 +157,35 @@ void place_fwd(AttnArgs &a, void *ws) {
 }
 
 // The backward's two passes.
-void plan_bwd(const AttnArgs &a, AttnArgs *dq, AttnArgs *dkv, int *dq_cols, int *dkv_cols) {
+void plan_bwd(const AttnArgs &a, int dtype, AttnArgs *dq, AttnArgs *dkv, int *dq_cols, int *dkv_cols) {
     *dq = a;
     dq->Nqp = (a.Nq + kTile - 1) / kTile * kTile;
     *dkv = *dq;
     *dq_cols = columns(a.Nq, a.D);
     dq->tiles = dq->per = (a.Nq + *dq_cols - 1) / *dq_cols;
     const int64_t all = static_cast<int64_t>(a.B) * dq->tiles;
-    share_waves(*dq, a.H, all, (a.Nk + kTile - 1) / kTile);
+    share_waves(*dq, a.H, all, (a.Nk + kTile - 1) / kTile, *dq_cols, false);
     dq->nwg = static_cast<int32_t>(all * (a.H / dq->hp));
 
-    *dkv_cols = columns(a.Nk, a.D);
-    dkv->tiles = (a.Nk + *dkv_cols - 1) / *dkv_cols;
-    const int64_t tiles = static_cast<int64_t>(a.B) * dkv->tiles;
-    dkv->span = static_cast<int32_t>(std::max<int64_t>(1, a.bias ? (tiles + kHistTables - 1) / kHistTables : 1));
-    dkv->spans = dkv->per = (dkv->tiles + dkv->span - 1) / dkv->span;
-    const int64_t blocks = static_cast<int64_t>(a.B) * dkv->spans;
-    share_waves(*dkv, a.Hkv, blocks, (a.Nq + kTile - 1) / kTile);
-    dkv->nwg = static_cast<int32_t>(blocks * (a.Hkv / dkv->hp));
     // the heads of a group whose histograms share 64 KiB of LDS
     const int tables = kAttnWaves * std::max(1, a.rule.nb * a.rule.nb) * 8;
-    dkv->head_step = std::min(a.group, std::max(1, (64 << 10) / tables));
+    dkv->head_step = std::min({a.group, 4, std::max(1, (64 << 10) / tables)});
+    // 16 for binary32 heads of more than 32 channels too, whose operands fill the registers
+    // (three images of 171 boxes, six heads of 48: forward and backward 64.6 us, 85.8 with 32)
+    *dkv_cols = dtype == RE_DTYPE_F32 && a.D > 32 ? 16 : columns(a.Nk, a.D);
+    for (int most = kAttnWaves;;) {
+        dkv->tiles = (a.Nk + *dkv_cols - 1) / *dkv_cols;
+        const int64_t tiles = static_cast<int64_t>(a.B) * dkv->tiles;
+        dkv->span = static_cast<int32_t>(std::max<int64_t>(1, a.bias ? (tiles + kHistTables - 1) / kHistTables : 1));
+        dkv->spans = dkv->per = (dkv->tiles + dkv->span - 1) / dkv->span;
+        const int64_t blocks = static_cast<int64_t>(a.B) * dkv->spans;
+        share_waves(*dkv, a.Hkv, blocks, (a.Nq + kTile - 1) / kTile, *dkv_cols, false, most);
+        dkv->nwg = static_cast<int32_t>(blocks * (a.Hkv / dkv->hp));
+        // beside the largest tables there is room for 16 columns only, or for fewer heads
+        if (dkv_fits(*dkv, dtype, *dkv_cols)) break;
+        if (*dkv_cols > 16) *dkv_cols = 16;
+        else most = dkv->hp / 2;
+    }
 }
 
 size_t stat_bytes(const AttnArgs &dq) {
@@ -357,7 +378,7 @@ re_status_t box_attn_workspace_size(const box_attn_t *d, int32_t backward, size_
     plan_fwd(a, &c0);
     *bytes = fwd_bytes(a);
     if (backward) {
-        plan_bwd(a, &dq, &dkv, &c0, &c1);
+        plan_bwd(a, d->dtype, &dq, &dkv, &c0, &c1);
         *bytes = std::max(*bytes, bwd_bytes(dkv));
     }
     return RE_OK;
@@ -409,7 +430,7 @@ re_status_t box_attn_bwd(const box_attn_t *d, const void *grad_out, const void *
     a.gk = grad_k;
     a.gv = grad_v;
     a.gbias = grad_bias;
-    plan_bwd(a, &dq, &dkv, &c0, &c1);
+    plan_bwd(a, d->dtype, &dq, &dkv, &c0, &c1);
     if ((st = check_workspace(workspace, workspace_bytes, bwd_bytes(dkv))) != RE_OK) return st;
     dq.terms = weight_terms(static_cast<int64_t>(a.B) * a.Nq * a.H * a.D);
     dkv.terms = weight_terms(static_cast<int64_t>(a.B) * a.Nk * a.Hkv * a.D);
