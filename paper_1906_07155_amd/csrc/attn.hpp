@@ -352,11 +352,15 @@ __device__ __forceinline__ f32x4 quad_values(const f32x4 (&o)[NT], int u) {
 struct BoxGeo {
     float cx, cy, ix, iy;
 };
-__device__ __forceinline__ void box_centre(const REX_GLOBAL float *b, float &cx, float &cy) {
+__device__ __forceinline__ f32x4 box_load(const float *p) {
+    gcptr<float> b = as_global<float>(p);
+    return f32x4{b[0], b[1], b[2], b[3]};
+}
+__device__ __forceinline__ void box_centre(f32x4 b, float &cx, float &cy) {
     cx = (b[0] + b[2]) * 0.5f;
     cy = (b[1] + b[3]) * 0.5f;
 }
-__device__ __forceinline__ BoxGeo box_geo(const REX_GLOBAL float *b) {
+__device__ __forceinline__ BoxGeo box_geo(f32x4 b) {
     BoxGeo o;
     box_centre(b, o.cx, o.cy);
     o.ix = 1.0f / fmaxf(b[2] - b[0], 1.0f);

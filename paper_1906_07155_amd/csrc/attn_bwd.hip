@@ -149,8 +149,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
             const int tile = (chunk * ahead + i) * parts + kw;
             if (tile >= t1) return;
             float kx, ky;
-            box_centre(as_global<float>(a.kbox + b * a.kbox_sb + min(tile * kTile + r, a.Nk - 1) * a.kbox_sr),
-                       kx, ky);
+            box_centre(box_load(a.kbox + b * a.kbox_sb + min(tile * kTile + r, a.Nk - 1) * a.kbox_sr), kx, ky);
             uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
 #pragma unroll 2
             for (int c = hw * 2 + (lane >> 5); c < cols; c += 2 * hp)
@@ -178,7 +177,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
         for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
             reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] =
                 table_entry(as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i], a.scale);
-        if (tid < cols) geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb + (q0 + tid) * a.qbox_sr));
+        if (tid < cols) geo[tid] = box_geo(box_load(a.qbox + b * a.qbox_sb + (q0 + tid) * a.qbox_sr));
         // columns without a query: bucket 0 of whatever they hold
         if (cols < kCols)
             for (int i = tid; i < 2 * ahead * parts * kCols * kBuckStride / 2; i += kAttnWaves * 64)
@@ -402,7 +401,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
             __syncthreads();              // the last tile's tables have been read
             if (tid < cols) {
                 float cx, cy;
-                box_centre(as_global<float>(a.kbox + b * a.kbox_sb + (k0 + tid) * a.kbox_sr), cx, cy);
+                box_centre(box_load(a.kbox + b * a.kbox_sb + (k0 + tid) * a.kbox_sr), cx, cy);
                 ctr[tid] = f32x2{cx, cy};
             }
             // columns without a key: bucket 0, to which their zeros are added
@@ -416,8 +415,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
             for (int i = 0; i < ahead; ++i) {
                 const int tile = (chunk * ahead + i) * parts + kw;
                 if (tile >= t1) return;
-                const BoxGeo q = box_geo(as_global<float>(a.qbox + b * a.qbox_sb +
-                                                          min(tile * kTile + r, a.Nq - 1) * a.qbox_sr));
+                const BoxGeo q = box_geo(box_load(a.qbox + b * a.qbox_sb + min(tile * kTile + r, a.Nq - 1) * a.qbox_sr));
                 uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
 #pragma unroll 2
                 for (int c = hw * 2 + (lane >> 5); c < cols; c += 2 * hp)

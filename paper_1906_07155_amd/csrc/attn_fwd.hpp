@@ -17,7 +17,7 @@
 // steps); 1000 in 16 heads of 64 25 us; 16 images of those 176 us, 65 GFLOP of products that
 // take 58 us at the rate of a large product and some 15 vector instructions for every pair and
 // head (bias, exponent, running maximum) that take 100.  The memory, 300 boxes against 6000 in
-// 16 heads of 64: 55 us; 64 single queries against up to 8192 in 8 heads of 32: 93 us, 2.7 TB/s.
+// 16 heads of 64: 53 us; 64 single queries against up to 8192 in 8 heads of 32: 78 us, 3.5 TB/s.
 #pragma once
 
 #include "attn.hpp"
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         float *t = reinterpret_cast<float *>(smem + lds.bias);
         gcptr<float> src = as_global<float>(a.bias + static_cast<int64_t>(h0) * nb2);
         for (int i = tid; i < hp * nb2; i += kAttnWaves * 64) t[i] = table_entry(src[i], a.scale);
-        if (tid < cols) geo[tid] = box_geo(as_global<float>(a.qbox + b * a.qbox_sb + (q0 + tid) * a.qbox_sr));
+        if (tid < cols) geo[tid] = box_geo(box_load(a.qbox + b * a.qbox_sb + (q0 + tid) * a.qbox_sr));
         // columns without a query: bucket 0 of whatever they hold
         if (cols < kCols)
             for (int i = tid; i < 2 * ahead * parts * kCols * kBuckStride / 2; i += kAttnWaves * 64)
@@ -133,15 +133,25 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         int64_t ph;
         bool on;
     } next;
-    auto page_of = [&](int tile) -> int {
-        const int p = a.pages[static_cast<int64_t>(b) * a.max_pages + tile];
-        return p >= 0 && p < a.num_pages ? p : -1;
-    };
+    // The pages of this wave's next 64 tiles are read at once, one by each lane.
+    struct Pages {
+        int v;
+        __device__ __forceinline__ int get(const AttnArgs &a, int b, int first, int parts, int step, int end) {
+            if ((step & 63) == 0) {
+                const int at = first + (step + static_cast<int>(threadIdx.x & 63)) * parts;
+                v = at < end ? as_global<int32_t>(a.pages)[static_cast<int64_t>(b) * a.max_pages + at] : -1;
+            }
+            const int p = __builtin_amdgcn_readlane(v, step & 63);
+            return p >= 0 && p < a.num_pages ? p : -1;
+        }
+    } kpages, bpages;
+    kpages.v = bpages.v = -1;
+    int kstep = 0;                                       // load_keys takes this wave's tiles in order
     auto load_keys = [&](int tile) {
         const int key = tile * kTile + (lane & 31);
         next.on = key < klen;
         if constexpr (PAGED) {
-            const int page = page_of(tile);
+            const int page = kpages.get(a, b, t0 + kw, parts, kstep++, t1);
             next.on = next.on && page >= 0;
             next.ph = static_cast<int64_t>(max(page, 0)) * a.Hkv + kh;
             const auto r = make_rsrc(a.mk + next.ph * kTile * a.D, kTile * a.D);
@@ -176,17 +186,28 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
             voff.pairs(vr.at(tile * kTile), tile * kTile + kTile <= klen, next.p);
         }
     };
-    // Buckets of the chunk's tiles against the workgroup's queries, by the waves that read them.
+    // Buckets of the chunk's tiles against the workgroup's queries, by the waves that read them;
+    // the boxes are read a chunk before.
+    f32x4 kb[2];
+    auto load_boxes = [&](int chunk) {
+        const int r = lane & 31;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int step = chunk * ahead + i, tile = t0 + step * parts + kw;
+            if (i >= ahead || tile >= t1) return;
+            if constexpr (PAGED)
+                kb[i] = *(const REX_GLOBAL f32x4 *)(
+                    a.mbox + (static_cast<int64_t>(max(bpages.get(a, b, t0 + kw, parts, step, t1), 0)) * kTile + r) * 4);
+            else kb[i] = box_load(a.kbox + b * a.kbox_sb + min(tile * kTile + r, a.Nk - 1) * a.kbox_sr);
+        }
+    };
     auto fill_buckets = [&](int chunk) {
         const int r = lane & 31;
-        for (int i = 0; i < ahead; ++i) {
-            const int tile = t0 + (chunk * ahead + i) * parts + kw;
-            if (tile >= t1) return;
-            const float *box;
-            if constexpr (PAGED) box = a.mbox + (static_cast<int64_t>(max(page_of(tile), 0)) * kTile + r) * 4;
-            else box = a.kbox + b * a.kbox_sb + min(tile * kTile + r, a.Nk - 1) * a.kbox_sr;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (i >= ahead || t0 + (chunk * ahead + i) * parts + kw >= t1) return;
             float kx, ky;
-            box_centre(as_global<float>(box), kx, ky);
+            box_centre(kb[i], kx, ky);
             uint16_t *dst = buck + (((chunk & 1) * ahead + i) * parts + kw) * kCols * kBuckStride + r;
 #pragma unroll 2
             for (int c = hw * 2 + (lane >> 5); c < cols; c += 2 * hp)
@@ -212,14 +233,17 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         load_values(t0 + kw);
     }
     if (BIAS) {
+        load_boxes(0);
         __syncthreads();
         fill_buckets(0);
+        load_boxes(1);
     }
 
     for (int chunk = 0; chunk < chunks; ++chunk) {
         if (BIAS) {
             __syncthreads();
             if (chunk + 1 < chunks) fill_buckets(chunk + 1);
+            load_boxes(chunk + 2);
         }
         for (int i = 0; i < ahead; ++i) {
             const int tile = t0 + (chunk * ahead + i) * parts + kw;

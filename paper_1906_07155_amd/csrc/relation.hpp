@@ -83,13 +83,14 @@ struct MemoryArgs {
     const void *k, *v;                  // append: element strides of row and head
     int64_t k_sr, k_sh, v_sr, v_sh;
     const float *boxes;
+    int32_t owned;                      // pages of one workgroup, where those share the work
     int32_t vec;                        // append: rows can be read 16 bytes at a time
     void *k_out, *v_out;                // read
     float *boxes_out;
 };
 
-hipError_t launch_memory_append(const MemoryArgs &a, int dtype, hipStream_t s);
-hipError_t launch_memory_read(const MemoryArgs &a, int dtype, hipStream_t s);
+hipError_t launch_memory_append(MemoryArgs a, int dtype, hipStream_t s);
+hipError_t launch_memory_read(MemoryArgs a, int dtype, hipStream_t s);
 
 struct NormArgs {
     const void *x, *branch;

@@ -26,7 +26,7 @@ constexpr int64_t kMaxRowHeads = (int64_t(1) << 31) - 1;
 // where they have 16 columns, whose few registers leave their waves waiting for memory.  Dense,
 // 1000 queries and keys, 16 heads of 64 channels: 128 workgroups 35.8 us, 256 26.4, 512 37.1.
 // Memory, 300 queries against 6000 boxes in the same heads: 160 68.9, 240 54.3, 360 74.5, 480 65.0;
-// 64 single queries against up to 8192 boxes each in 8 heads of 32: 256 126, 512 93, 768 108.
+// 64 single queries against up to 8192 boxes each in 8 heads of 32: 512 78, 1024 86.
 constexpr int64_t kGroups = 256;
 // Workgroups of the norms.  16000 rows of 1024 channels, bf16: forward 26.6 us with 1024
 // of them, 28.2 with 4096; backward 54 us with 512 (two on each CU, what its registers

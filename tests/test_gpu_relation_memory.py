@@ -72,6 +72,65 @@ def test_append_and_read(dtype, n, hkv, D, layout):
     assert all(float(t.abs().sum()) == 0.0 for t in rex.box_memory_read(m, rest))
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("pages,hkv,D,n", [(64, 32, 128, 2048),      # every page full
+                                           (530, 32, 128, 2120),     # workgroups with two pages
+                                           (75, 112, 40, 2000)])
+def test_many_boxes(dt, pages, hkv, D, n):
+    """Calls with so many boxes that workgroups share them out by pages; what the call does not
+    name keeps what it held."""
+    log("memory many %d %d %d %d" % (pages, hkv, D, n))
+    rng = np.random.default_rng(n)
+    make = lambda *shape: torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(dt).cuda()
+    k, v = make(n, hkv, D), make(n, hkv, D)
+    boxes = torch.from_numpy(draw_boxes(rng, (n,))).cuda()
+    m = rex.box_memory(pages, hkv, D)
+    for t in m:
+        t.fill_(7)
+    want = [t.cpu().numpy().copy() for t in m]
+    slots = rng.permutation(pages * 32)[:n].astype(np.int64)
+    out = slots.copy()
+    out[::97] = [-5, pages * 32, 1 << 40][n % 3]           # some outside the memory
+    rex.box_memory_append(m, torch.from_numpy(out).cuda(), k, v, boxes)
+    inside = np.flatnonzero((out >= 0) & (out < pages * 32))
+    p, at = out[inside] // 32, out[inside] % 32
+    (kc, ks), (vc, vs) = O.encode(k.float().cpu().numpy()), O.encode(v.float().cpu().numpy())
+    want[0][p, :, at], want[2][p, :, at] = kc[inside], ks[inside]
+    want[1][p, :, :, at], want[3][p, :, at] = vc[inside], vs[inside]
+    want[4][p, at] = boxes.cpu().numpy()[inside]
+    for got, w in zip(m, want):
+        assert np.array_equal(got.cpu().numpy(), w)
+    # read back in another order, some slots several times and some outside
+    ask = rng.choice(out, n + 8)
+    gk, gv, gb = rex.box_memory_read(m, torch.from_numpy(ask).cuda(), dt)
+    there = (ask >= 0) & (ask < pages * 32)
+    p, at = np.where(there, ask, 0) // 32, np.where(there, ask, 0) % 32
+    mask = there[:, None, None]
+    product = lambda code, scale: torch.from_numpy(
+        np.where(mask, code.astype(np.float32) * scale[..., None], np.float32(0))).to(dt)
+    assert torch.equal(gk.cpu(), product(want[0][p, :, at], want[2][p, :, at]))
+    assert torch.equal(gv.cpu(), product(want[1][p, :, :, at], want[3][p, :, at]))
+    assert np.array_equal(gb.cpu().numpy(), np.where(there[:, None], want[4][p, at], np.float32(0)))
+
+
+def test_many_reads_of_few_slots():
+    """One page's boxes asked for more often than a workgroup's list holds."""
+    log("memory many reads")
+    rng = np.random.default_rng(3)
+    hkv, D, n = 32, 64, 9000
+    m = rex.box_memory(2, hkv, D)
+    slots = torch.arange(64, device="cuda")
+    k = torch.from_numpy(rng.standard_normal((64, hkv, D)).astype(np.float32)).cuda()
+    boxes = torch.from_numpy(draw_boxes(rng, (64,))).cuda()
+    rex.box_memory_append(m, slots, k, k.flip(0), boxes)
+    ask = torch.from_numpy(rng.choice([3, 40, 5, -1], n, p=[0.8, 0.1, 0.05, 0.05])).cuda()
+    one = rex.box_memory_read(m, slots)
+    got = rex.box_memory_read(m, ask)
+    for g, w in zip(got, one):
+        w = torch.where((ask >= 0).view(-1, *[1] * (w.dim() - 1)), w[ask.clamp(min=0)], torch.zeros_like(w[:1]))
+        assert torch.equal(g, w)
+
+
 def test_slots_outside_and_values_that_are_no_numbers():
     log("memory slots")
     m = rex.box_memory(2, 2, 16)
