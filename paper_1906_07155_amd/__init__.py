@@ -18,11 +18,15 @@ __all__ = ["RoIExtractError", "box_nms", "box_nms_batched", "deform_roi_pool_bwd
            "zero_grad", "roi_extract",
            "RoIAlignFunction", "box_attn_bwd", "box_attn_fwd", "box_attn_workspace_size",
            "box_memory", "box_memory_append", "box_memory_attn_fwd", "box_memory_read",
-           "gated_norm_bwd", "gated_norm_fwd"]
+           "gated_norm_bwd", "gated_norm_fwd",
+           "BoxMemory", "RelationHead", "box_attention", "gated_norm"]
 
 
 def __getattr__(name):
     if name in ("roi_extract", "RoIAlignFunction"):
         from . import extractor
         return getattr(extractor, name)
+    if name in ("BoxMemory", "RelationHead", "box_attention", "gated_norm"):
+        from . import relation_head
+        return getattr(relation_head, name)
     raise AttributeError(name)
