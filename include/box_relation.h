@@ -18,8 +18,8 @@
  * Data of RE_DTYPE_BF16 or RE_DTYPE_F32; parameters (bias, weights, gates), their gradients
  * and statistics are binary32.  Products of bf16 data are exact and summed in binary32; the
  * weights of the softmax and the gradient of the logits are rounded to bf16 where they
- * multiply bf16 data (to two such parts where the results are few), and every result is
- * rounded once when it is stored.
+ * multiply bf16 data (to two or three such parts where the results are few), and every result
+ * is rounded once when it is stored.
  */
 #ifndef BOX_RELATION_H
 #define BOX_RELATION_H
@@ -63,7 +63,8 @@ typedef struct {
     int32_t dim;
     int64_t batch, num_q, num_k;
     /* element strides of batch, row and head, multiples of 16 bytes (channels are
-     * adjacent); bases 16-byte aligned; the rows of one image span less than 2^31 bytes */
+     * adjacent); bases 16-byte aligned; the rows of one image and 32 more span less than
+     * 2^30 bytes (RE_ERR_UNSUPPORTED) */
     int64_t q_stride[3], k_stride[3], v_stride[3];
     float scale;              /* finite, at least 1e-20 */
     int32_t buckets;          /* odd, in [1, RE_ATTN_MAX_BUCKETS]; 0 without bias */

@@ -209,7 +209,8 @@ def _attn_descriptor(q, k, v, scale, q_boxes, k_boxes, bias, first_exp, octave_s
             raise ValueError("k_mask must be bool or uint8 (got %s)" % k_mask.dtype)
         _dense(k_mask, (B, nk), "k_mask", k_mask.dtype)
     _need_cuda(q, "q")
-    _same_device(q, "k v bias q_boxes k_boxes q_len k_len k_mask", (k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask))
+    _same_device(q, "k v bias q_boxes k_boxes q_len k_len k_mask",
+                 (k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask))
     if scale is None:
         scale = D ** -0.5
     return _ATTN.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), code, H, hkv, D, B, nq, nk,
@@ -299,7 +300,8 @@ def box_attn_bwd(grad_out, q, k, v, out, lse, out_f32=None, *, scale: Optional[f
         if bias is None:
             raise ValueError("grad_bias without a bias")
         _dense(grad_bias, bias.shape, "grad_bias", torch.float32)
-    _same_device(q, "grad_out out lse out_f32 grad_q grad_k grad_v grad_bias", (grad_out, out, lse, out_f32, grad_q, grad_k, grad_v, grad_bias))
+    _same_device(q, "grad_out out lse out_f32 grad_q grad_k grad_v grad_bias",
+                 (grad_out, out, lse, out_f32, grad_q, grad_k, grad_v, grad_bias))
     if workspace is not None:
         binding._workspace(workspace, q)
         _same_device(q, "workspace", (workspace,))
@@ -441,7 +443,8 @@ def box_memory_attn_fwd(q, memory: Sequence, pages, lengths, *, scale: Optional[
     if lse is not None:
         _dense(lse, (B, H, nq), "lse", torch.float32)
     _need_cuda(q, "q", memory[0])
-    _same_device(q, "pages lengths q_len bias q_boxes out lse", (pages, lengths, q_len, bias, q_boxes, out, lse))
+    _same_device(q, "pages lengths q_len bias q_boxes out lse",
+                 (pages, lengths, q_len, bias, q_boxes, out, lse))
     if workspace is not None:
         binding._workspace(workspace, q)
         _same_device(q, "workspace", (workspace,))
@@ -498,9 +501,11 @@ def _norm_descriptor(x, branch, gate, alpha, post_weight, post_bias, pre_weight,
         if t is not None:
             _dense(t, (c,), name, torch.float32)
     _need_cuda(x, "x")
-    _same_device(x, "branch gate post_weight post_bias pre_weight pre_bias", (branch, gate, post_weight, post_bias, pre_weight, pre_bias))
-    return _NORM.pack(x.data_ptr(), _ptr(branch), x.stride(0), 0 if branch is None else branch.stride(0),
-                      code, NORMS[norm], m, c, alpha, eps, gates, _ptr(gate), *map(_ptr, params))
+    _same_device(x, "branch gate post_weight post_bias pre_weight pre_bias",
+                 (branch, gate, post_weight, post_bias, pre_weight, pre_bias))
+    return _NORM.pack(x.data_ptr(), _ptr(branch), x.stride(0),
+                      0 if branch is None else branch.stride(0), code, NORMS[norm], m, c, alpha,
+                      eps, gates, _ptr(gate), *map(_ptr, params))
 
 
 def gated_norm_fwd(x, branch=None, *, gate=None, alpha: float = 1.0, post_weight=None,

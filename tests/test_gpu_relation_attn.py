@@ -345,3 +345,39 @@ def test_many_tiles_share_a_histogram():
     log("attn many tiles")
     c = Case("f32", 90, 24 * 32, 3, 1, 1, 8, 3, seed=9)
     c.check(c.both(), "many tiles")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_largest_tables_of_eight_heads_in_one_workgroup(dtype, D):
+    """One step of keys (and of queries): a workgroup takes eight heads, whose tables and tiles come
+    near to all of its LDS; heads that share keys, four at a time with small tables."""
+    log("attn tables %s %d" % (dtype, D))
+    for shape in ((2, 31, 30, 16, 8, D, 31), (2, 30, 32, 8, 8, D, 31), (3, 32, 17, 8, 1, D, 15), (1, 70, 33, 16, 16, D, 31)):
+        c = Case(dtype, *shape, seed=13)
+        c.check(c.both(), str(shape))
+
+
+def test_tensors_on_the_host_are_refused():
+    log("attn host tensors")
+    c = Case("f32", 1, 4, 4, 2, 2, 8, 3)
+    for name, bad in (("bias", c.geo["bias"].cpu()), ("q_boxes", c.geo["q_boxes"].cpu()),
+                      ("k_len", torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises(ValueError, match=name):
+            rex.box_attn_fwd(c.q, c.k, c.v, **dict(c.args(), **{name: bad}))
+    with pytest.raises(ValueError, match="v must be"):
+        rex.box_attn_fwd(c.q, c.k, c.v.cpu())
+    out, lse, _ = c.fwd(save=True)
+    with pytest.raises(ValueError, match="lse"):
+        rex.box_attn_bwd(c.g, c.q, c.k, c.v, out, lse.cpu(), **c.args())
+    with pytest.raises(ValueError, match="grad_out"):
+        rex.box_attn_bwd(c.g[:, :3], c.q, c.k, c.v, out, lse, **c.args())
+    m = rex.box_memory(2, 2, 8)
+    with pytest.raises(ValueError, match="slots"):
+        rex.box_memory_read(m, torch.zeros(3, dtype=torch.int64))
+    with pytest.raises(ValueError, match="pages"):
+        rex.box_memory_attn_fwd(c.q, m, torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32).cuda())
+    with pytest.raises(ValueError, match="post_weight"):
+        rex.gated_norm_fwd(c.q[0, :, 0], c.k[0, :, 0], post_weight=torch.ones(8))
+    with pytest.raises(rex.RoIExtractError):
+        rex.box_attn_fwd(c.q, c.k, c.v, scale=0.0)
