@@ -10,11 +10,13 @@
 //                (8 bytes a box, from L2), and each of its waves takes a (page, head): the values
 //                pass through LDS, and 64 adjacent bytes of the page are one access.
 // Shuffled slots, binary32, 16 heads of 64 channels, append / read, us, the first and the second:
-// 2048 pages, 8000 boxes 70 / 53 and 73 / 34, 16000 boxes 134 / 102 and 101 / 55; 4000 boxes
-// 38 / 28 and 56 / 26.  bf16, 32768 pages, 16000 boxes in 8 heads of 64: 73 / 50 and 180 / 104; 512
-// pages, 16000 boxes in 8 heads of 32: 34 / 18 and 39 / 16.  So the second takes a call with four
+// 2048 pages, 8000 boxes 69 / 53 and 62 / 33, 16000 boxes 134 / 102 and 95 / 53; 4000 boxes
+// 38 / 28 and 48 / 26.  bf16, 32768 pages, 16000 boxes in 8 heads of 64: 72 / 51 and 177 / 110; 512
+// pages, 16000 boxes in 8 heads of 32: 34 / 18 and 38 / 18.  So the second takes a call with four
 // boxes for each page of the memory and 2^23 values.  Its 16000 boxes are 333 MB both ways, 68 us
-// at the rate of a large copy; lines of a page that are written in part cost their reading too.
+// at the rate of a large copy.  What bounds the second is latency: a wave's (page, head) has few
+// boxes, and each goes from its slot over its row to LDS and to the page (16 waves of a workgroup:
+// append 105 us as a kernel alone, 8 waves 119).
 #include <algorithm>
 
 #include "attn.hpp"
@@ -137,9 +139,9 @@ __global__ __launch_bounds__(256) void memory_read_kernel(MemoryArgs a) {
 
 constexpr int kOwners = 512, kOwned = 256;      // workgroups, and the most pages of one
 constexpr int64_t kManyValues = 1 << 23;
-constexpr int kOwnWaves = 8, kOwnThreads = kOwnWaves * 64;
+constexpr int kOwnWaves = 16, kOwnThreads = kOwnWaves * 64;
 constexpr int kRow = kTile + 4;                 // bytes of a row of a page's values in LDS
-constexpr int kSlotLoads = 4;                   // slots that a thread has on their way
+constexpr int kSlotLoads = 2;                   // slots that a thread has on their way
 constexpr int kList = 2 * kSlotLoads * kOwnThreads;
 
 // The places of the set bits of `m`, in order.
