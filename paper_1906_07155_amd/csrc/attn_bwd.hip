@@ -19,7 +19,7 @@
 // binary32 (measured, whatever the addresses).
 //
 // Measured, 16 images of up to 1000 boxes in 16 heads of 64 channels, bf16: rowstat 13 us, dq
-// 211, dkv 440, hist 11.5.  dkv has four products of the pair matrix and its operands leave two
+// 211, dkv 440, hist 4.  dkv has four products of the pair matrix and its operands leave two
 // waves on a SIMD; without its histogram it takes 418 us, with every tile at one address 424, so
 // what bounds it is the issue of products, exponents and LDS reads by too few waves.  Two images
 // of 512 boxes in 8 heads of 32, binary32: 3.4, 20, 27 and 4 us.
@@ -638,6 +638,7 @@ __global__ __launch_bounds__(1024) void attn_hist_kernel(AttnArgs a) {
     if (i < n) {
         gcptr<float> src = as_global<float>(a.hist);
         const int chunks = a.B * a.spans;
+#pragma unroll 8
         for (int c = slice; c < chunks; c += 16) sum += src[c * n + i];
     }
     part[slice][threadIdx.x & 63] = sum;

@@ -413,8 +413,11 @@ __global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a, int gate
     }
     if (!dst) return;                             // the whole workgroup
     float s = 0.0f;
-    if (col < a.C)
+    if (col < a.C) {
+        // eight loads on their way at once: one after the other 32 of them took 10 us
+#pragma unroll 8
         for (int64_t i = slice; i < n; i += 16) s += as_global<float>(src)[i * step + col];
+    }
     part[slice][threadIdx.x & 63] = s;
     __syncthreads();
     if (slice == 0 && col < a.C) {
