@@ -161,11 +161,19 @@ __global__ __launch_bounds__(kOwnThreads) void memory_append_pages_kernel(Memory
     char *const tile = smem + owned * kTile * 4 + kOwnWaves * 64 + wave * a.D * kRow;
     for (int i = tid; i < owned * kTile; i += kOwnThreads) item[i] = -1;
     __syncthreads();
-#pragma unroll kSlotLoads
-    for (int i = tid; i < count; i += kOwnThreads) {
-        const int64_t slot = as_global<int64_t>(a.slots)[i], page = slot / kTile;
-        if (slot >= 0 && slot < a.num_slots && page % kOwners == blockIdx.x)
-            atomicMax(item + page / kOwners * kTile + slot % kTile, i);
+    for (int base = 0; base < count; base += 4 * kOwnThreads) {
+        int64_t slot[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = base + u * kOwnThreads + tid;
+            slot[u] = i < count ? as_global<int64_t>(a.slots)[i] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t page = slot[u] / kTile;
+            if (slot[u] >= 0 && slot[u] < a.num_slots && page % kOwners == blockIdx.x)
+                atomicMax(item + page / kOwners * kTile + slot[u] % kTile, base + u * kOwnThreads + tid);
+        }
     }
     __syncthreads();
     for (int e = tid; e < owned * kTile * 4; e += kOwnThreads) {
