@@ -121,18 +121,19 @@ class _Call:
 
 
 def _rows4(t, name: str, shape=None):
-    """A [batch, rows, heads, dim] tensor with adjacent channels."""
-    if t.dim() != 4 or (shape is not None and tuple(t.shape) != tuple(shape)):
+    """The strides of a [batch, rows, heads, dim] tensor with adjacent channels."""
+    if t.dim() != 4 or (shape is not None and t.shape != shape):
         raise ValueError("%s must be a 4-D [batch, rows, heads, dim] tensor%s (got %s)"
                          % (name, "" if shape is None else " of shape %s" % (tuple(shape),),
                             tuple(t.shape)))
-    if t.stride(3) != 1 and t.shape[3] > 1 and t.numel() > 0:
+    strides = t.stride()
+    if strides[3] != 1 and t.shape[3] > 1 and t.numel() > 0:
         raise ValueError("the channels of %s must be adjacent" % name)
-    return t
+    return strides
 
 
 def _dense(t, shape, name: str, dtype):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s (got %s %s)"
                          % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     return t
@@ -142,7 +143,7 @@ def _boxes(t, batch: int, num: int, name: str):
     torch = _torch()
     if t is None:
         raise ValueError("%s is required with a bias" % name)
-    if t.dtype != torch.float32 or tuple(t.shape) != (batch, num, 4):
+    if t.dtype != torch.float32 or t.shape != (batch, num, 4):
         raise ValueError("%s must be a float32 tensor of shape %s (got %s %s)"
                          % (name, (batch, num, 4), t.dtype, tuple(t.shape)))
     if t.numel() > 0 and t.stride(2) != 1:
@@ -184,12 +185,12 @@ def _attn_descriptor(q, k, v, scale, q_boxes, k_boxes, bias, first_exp, octave_s
                      k_len, k_mask):
     """box_attn_t of checked tensors, as bytes."""
     torch = _torch()
-    _rows4(q, "q")
+    qs, ks = _rows4(q, "q"), _rows4(k, "k")
     B, nq, H, D = q.shape
-    _rows4(k, "k")
-    nk, hkv = k.shape[1], k.shape[2]
-    _rows4(k, "k", (B, nk, hkv, D))
-    _rows4(v, "v", (B, nk, hkv, D))
+    _, nk, hkv, _ = k.shape
+    if k.shape != (B, nk, hkv, D):
+        _rows4(k, "k", (B, nk, hkv, D))
+    vs = _rows4(v, "v", k.shape)
     code = _dtype_code(q)
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise TypeError("q, k and v must have one dtype (got %s, %s, %s)"
@@ -214,7 +215,7 @@ def _attn_descriptor(q, k, v, scale, q_boxes, k_boxes, bias, first_exp, octave_s
     if scale is None:
         scale = D ** -0.5
     return _ATTN.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), code, H, hkv, D, B, nq, nk,
-                      *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], scale, n, first_exp,
+                      *qs[:3], *ks[:3], *vs[:3], scale, n, first_exp,
                       octave_steps, _ptr(bias), _ptr(q_boxes), _ptr(k_boxes), *boxes,
                       _ptr(q_len), _ptr(k_len), _ptr(k_mask))
 
@@ -420,7 +421,7 @@ def box_memory_attn_fwd(q, memory: Sequence, pages, lengths, *, scale: Optional[
     where `save` is true or it is given, else None."""
     torch = _torch()
     m, hkv, dim = _memory_descriptor(memory)
-    _rows4(q, "q")
+    qs = _rows4(q, "q")
     B, nq, H, D = q.shape
     if D != dim:
         raise ValueError("q has %d channels a head, the memory %d" % (D, dim))
@@ -448,7 +449,7 @@ def box_memory_attn_fwd(q, memory: Sequence, pages, lengths, *, scale: Optional[
     if workspace is not None:
         binding._workspace(workspace, q)
         _same_device(q, "workspace", (workspace,))
-    d = _RECALL.pack(q.data_ptr(), code, H, B, nq, pages.shape[1], *q.stride()[:3],
+    d = _RECALL.pack(q.data_ptr(), code, H, B, nq, pages.shape[1], *qs[:3],
                      D ** -0.5 if scale is None else scale, n, first_exp, octave_steps,
                      _ptr(bias), _ptr(q_boxes), *strides, _ptr(q_len), pages.data_ptr(),
                      lengths.data_ptr())
