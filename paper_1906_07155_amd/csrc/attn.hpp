@@ -16,7 +16,7 @@
 //     transposing read gives a lane one channel of four rows.  (Read from memory as pairs
 //     of channels a tile of 64 channels takes 16 loads of 4 bytes a lane instead of 4 of 16,
 //     and each costs the address unit the same 16 cycles.  16 images of up to 1000 boxes in 16
-//     heads of 64 channels: forward 197 us that way, 176 this way; query pass 226 and 211.)
+//     heads of 64 channels: forward 197 us that way, 173 this way.)
 //   - Binary32 data has no such read: lane n takes channels 2n and 2n + 1 of its eight
 //     rows from memory, the operands of two tiles with channel 2r + t in row r of tile t.
 #pragma once

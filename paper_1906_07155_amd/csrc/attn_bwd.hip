@@ -1,10 +1,10 @@
 // attn_bwd.hip -- the backward of the attention among boxes (box_attn_bwd).
 //
-//   rowstat   per (row, head): the row's log sum in units of log 2 (+inf where the row has no
-//             part), and delta = sum_c grad_out * out
-//   dq        query columns, keys streamed: grad_q, and for bf16 data delta again, as the sum
-//             of p dp in binary32.  `out` carries the rounding of the weights and its own, which
-//             is little in grad_q but would be the bias gradient's largest error (6e-4 of it)
+//   dq        query columns, keys streamed: grad_q; and for the key pass each row's log sum in
+//             units of log 2 (+inf where the row has no part) and delta = sum_c grad_out * out, for
+//             bf16 data as the sum of p dp in binary32: `out` carries the rounding of the weights
+//             and its own, which is little in grad_q but would be the bias gradient's largest
+//             error (6e-4 of it)
 //   dkv       key columns, queries streamed, over the heads that share the key head: grad_k,
 //             grad_v and the bias gradient
 //   hist      the bias gradient's partial tables added up
@@ -18,55 +18,16 @@
 // are binary64: an addition of 64 lanes to LDS takes 18 to 30 cycles of a CU there, 193 in
 // binary32 (measured, whatever the addresses).
 //
-// Measured, 16 images of up to 1000 boxes in 16 heads of 64 channels, bf16: rowstat 13 us, dq
-// 211, dkv 440, hist 4.  dkv has four products of the pair matrix and its operands leave two
+// Measured, 16 images of up to 1000 boxes in 16 heads of 64 channels, bf16: dq 227 us, dkv
+// 440, hist 4.  dkv has four products of the pair matrix and its operands leave two
 // waves on a SIMD; without its histogram it takes 418 us, with every tile at one address 424, so
 // what bounds it is the issue of products, exponents and LDS reads by too few waves.  Two images
-// of 512 boxes in 8 heads of 32, binary32: 3.4, 20, 27 and 4 us.
+// of 512 boxes in 8 heads of 32, binary32: 21, 27 and 4 us.
 #include "attn.hpp"
 
 namespace rex {
 
 namespace {
-
-template <typename T>
-__global__ __launch_bounds__(256) void attn_rowstat_kernel(AttnArgs a) {
-    using N = Num<T>;
-    using Frag = typename N::Frag;
-    const int lanes = a.D <= 32 ? 4 : a.D <= 64 ? 8 : 16, c = threadIdx.x & (lanes - 1);
-    const int64_t e = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / lanes;
-    // e = (b * Nqp + row) * H + h
-    const int h = static_cast<int>(e % a.H);
-    const int row = static_cast<int>(e / a.H % a.Nqp);
-    const int64_t b = e / (static_cast<int64_t>(a.H) * a.Nqp);
-    if (b >= a.B) return;
-    const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
-    const int64_t bh = b * a.H + h;
-    float lse = -kInf, delta = 0.0f;
-    if (row < qlen) {
-        lse = as_global<float>(a.flse)[bh * a.Nq + row];
-        if (8 * c < a.D) {
-            const int64_t at = (((b * a.Nq + row) * a.H + h) * a.D + 8 * c) * N::kSize;
-            const Frag g = N::load(static_cast<const char *>(a.gout.p) + at);
-            f32x8 o;
-            if (a.fout_f32) {
-                o = Num<float>::load(reinterpret_cast<const char *>(a.fout_f32) + at * (4 / N::kSize));
-            } else {
-                const Frag f = N::load(static_cast<const char *>(a.fout) + at);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = static_cast<float>(f[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) delta = fmaf(static_cast<float>(g[i]), o[i], delta);
-        }
-    }
-    for (int d = 1; d < lanes; d <<= 1) delta += __shfl_xor(delta, d);
-    if (c == 0) {
-        const bool none = lse == -kInf;
-        *(REX_GLOBAL f32x2 *)(a.rowstat + (bh * a.Nqp + row) * 2) =
-            none ? f32x2{kInf, 0.0f} : f32x2{lse * kLog2e, delta};
-    }
-}
 
 // Steps whose buckets are computed between two barriers.
 inline __host__ __device__ int bwd_ahead(int parts) { return parts >= 2 ? 1 : 2; }
@@ -161,16 +122,50 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     float lse[NS], delta[NS], sum[NS];
     {
         const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
+        const Rows out{a.fout, a.gout.sb, a.gout.sr, a.gout.sh};
         const int first = min(q0, max(qlen - 1, 0));
+        const int64_t bh = static_cast<int64_t>(b) * a.H + h;
+        Frag o[NS][DB];
         load_columns<T, DB, NS>(qr.at(first), qr.sr, n, g, a.D, q);
         load_columns<T, DB, NS>(gr.at(first), gr.sr, n, g, a.D, go);
+        load_columns<T, DB, NS>(head_rows<T>(out, b, h, qlen, a.D).at(first), gr.sr, n, g, a.D, o);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) lse[s] = as_global<float>(a.flse)[bh * a.Nq + min(q0 + 16 * s + n, a.Nq - 1)];
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            const f32x2 st = *(const REX_GLOBAL f32x2 *)(
-                a.rowstat + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + min(q0 + 16 * s + n, a.Nqp - 1)) * 2);
-            lse[s] = st[0];
-            delta[s] = st[1];
+            const int row = q0 + 16 * s + n;
+            float d = 0.0f;
+#pragma unroll
+            for (int k = 0; k < DB; ++k) {
+                const int ch = 32 * k + 8 * g;
+                if (a.fout_f32) {                        // few keys: not rounded
+                    if (row >= qlen || ch >= a.D) continue;
+                    const f32x8 x = Num<float>::load(reinterpret_cast<const char *>(
+                        a.fout_f32 + ((static_cast<int64_t>(b) * a.Nq + row) * a.H + h) * a.D + ch));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d = fmaf(static_cast<float>(go[s][k][i]), x[i], d);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        d = fmaf(static_cast<float>(go[s][k][i]), static_cast<float>(o[s][k][i]), d);
+                }
+            }
+            d = sum_over_rows(d);
+            const bool none = row >= qlen || lse[s] == -kInf;
+            lse[s] = none ? kInf : lse[s] * kLog2e;
+            delta[s] = none ? 0.0f : d;
             sum[s] = 0.0f;
+            // for the key pass; delta of bf16 data follows at the end
+            gptr<float> st = as_global_mut<float>(a.rowstat) + (bh * a.Nqp + row) * 2;
+            if (kw == 0 && g == 0 && row < a.Nqp) {
+                st[0] = lse[s];
+                if (N::kExact || row >= qlen) st[1] = delta[s];
+            }
+            // 16 columns: the rows that fill up the last 32
+            if (NS == 1 && kw == 0 && g == 1 && q0 + 16 >= a.Nq && row + 16 < a.Nqp) {
+                st[32] = kInf;
+                st[33] = 0.0f;
+            }
         }
     }
     if (BIAS) {
@@ -694,13 +689,6 @@ bool dkv_fits(const AttnArgs &a, int dtype, int cols) {
 
 hipError_t launch_attn_bwd(const AttnArgs &dq, const AttnArgs &dkv, int dtype, int dq_cols,
                            int dkv_cols, hipStream_t s) {
-    const int lanes = dq.D <= 32 ? 4 : dq.D <= 64 ? 8 : 16;
-    const int64_t n = static_cast<int64_t>(dq.B) * dq.H * dq.Nqp * lanes;
-    const dim3 grid(static_cast<uint32_t>((n + 255) / 256));
-    if (n > 0 && dtype == kBF16)
-        hipLaunchKernelGGL((attn_rowstat_kernel<uint16_t>), grid, dim3(256), 0, s, dq);
-    else if (n > 0)
-        hipLaunchKernelGGL((attn_rowstat_kernel<float>), grid, dim3(256), 0, s, dq);
     run_typed(dq, dtype, false, dq_cols, s);
     run_typed(dkv, dtype, true, dkv_cols, s);
     if (dkv.bias) {

@@ -14,7 +14,7 @@
 // into LDS (16 bits a pair: the byte offset into a head's table, which is in LDS too).
 //
 // Measured, bf16: 100 boxes in 8 heads of 32 channels 8.4 us (a launch and four dependent
-// steps); 1000 in 16 heads of 64 25 us; 16 images of those 176 us, 65 GFLOP of products that
+// steps); 1000 in 16 heads of 64 25 us; 16 images of those 173 us, 65 GFLOP of products that
 // take 58 us at the rate of a large product and some 15 vector instructions for every pair and
 // head (bias, exponent, running maximum) that take 100.  The memory, 300 boxes against 6000 in
 // 16 heads of 64: 53 us; 64 single queries against up to 8192 in 8 heads of 32: 78 us, 3.5 TB/s.
