@@ -136,18 +136,19 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
             const int row = q0 + 16 * s + n;
             float d = 0.0f;
 #pragma unroll
-            for (int k = 0; k < DB; ++k) {
-                const int ch = 32 * k + 8 * g;
-                if (a.fout_f32) {                        // few keys: not rounded
-                    if (row >= qlen || ch >= a.D) continue;
-                    const f32x8 x = Num<float>::load(reinterpret_cast<const char *>(
-                        a.fout_f32 + ((static_cast<int64_t>(b) * a.Nq + row) * a.H + h) * a.D + ch));
+            for (int k = 0; k < DB; ++k)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d = fmaf(static_cast<float>(go[s][k][i]), x[i], d);
-                } else {
+                for (int i = 0; i < 8; ++i)
+                    d = fmaf(static_cast<float>(go[s][k][i]), static_cast<float>(o[s][k][i]), d);
+            if (!N::kExact && a.fout_f32) {              // few keys: of what was not rounded
+                d = 0.0f;
+                const int64_t at = ((static_cast<int64_t>(b) * a.Nq + min(row, a.Nq - 1)) * a.H + h) * a.D;
+#pragma unroll 1
+                for (int ch = 8 * g; ch < a.D; ch += 32) {
+                    const f32x8 x = Num<float>::load(reinterpret_cast<const char *>(a.fout_f32 + at + ch));
+                    const Frag y = N::load(static_cast<const char *>(a.gout.p) + (at + ch) * N::kSize);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        d = fmaf(static_cast<float>(go[s][k][i]), static_cast<float>(o[s][k][i]), d);
+                    for (int i = 0; i < 8; ++i) d = fmaf(static_cast<float>(y[i]), x[i], d);
                 }
             }
             d = sum_over_rows(d);
