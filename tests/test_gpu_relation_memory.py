@@ -250,6 +250,83 @@ def test_recall_splits_repeat_bit_for_bit():
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_recall_of_many_pages_by_one_wave(dtype):
+    """So many streams that a wave takes all of its stream's pages, more than it reads numbers of at
+    once: every stream remembers the same boxes in another order of pages."""
+    log("recall many pages %s" % dtype)
+    rng = np.random.default_rng(8)
+    streams, pages, H, D, nb = 512, 131, 8, 32, 15
+    m = rex.box_memory(pages, H, D)
+    n = pages * 32
+    k, v = (torch.from_numpy(rng.standard_normal((n, H, D)).astype(np.float32)).cuda() for _ in range(2))
+    kb, qb = draw_boxes(rng, (n,)), draw_boxes(rng, (streams, 1))
+    everything = torch.arange(n, device="cuda")
+    rex.box_memory_append(m, everything, k, v, torch.from_numpy(kb).cuda())
+    gk, gv, _ = rex.box_memory_read(m, everything)
+    bias = rng.standard_normal((H, nb, nb)).astype(np.float32)
+    q = torch.from_numpy(rng.standard_normal((streams, 1, H, D)).astype(np.float32)).to(DT[dtype]).cuda()
+    table = torch.from_numpy(np.stack([rng.permutation(pages) for _ in range(streams)]).astype(np.int32)).cuda()
+    out, lse = rex.box_memory_attn_fwd(q, m, table, torch.full((streams,), n, dtype=torch.int32, device="cuda"),
+                                       q_boxes=torch.from_numpy(qb).cuda(), bias=torch.from_numpy(bias).cuda(), save=True)
+    idx = O.buckets(qb[:, 0], kb, nb, -4, 1)[None]
+    ref = O.attn(f64(q).reshape(1, streams, H, D), f64(gk)[None], f64(gv)[None], D ** -0.5, idx,
+                 bias.reshape(H, -1).astype(np.float64))
+    e = 2 * (D + 8) * 2.0 ** -24 * max(ref["logit"], 1.0) + 2.0 ** -21 + (n + 64) * 2.0 ** -24
+    tol = (e + (2.0 ** -7 if dtype == "bf16" else 0.0)) * ref["out_abs"] + 1e-30
+    assert (np.abs(f64(out)[:, 0] - ref["out"][0]) <= tol[0]).all()
+    few = 3e-3 if dtype == "bf16" else 1e-5
+    assert np.linalg.norm(f64(out)[:, 0] - ref["out"][0]) <= few * np.linalg.norm(ref["out"])
+    assert np.all(np.abs(f64(lse)[:, :, 0].T - ref["lse"][0]) <= 2 * e + 2.0 ** -22 * np.abs(ref["lse"][0]))
+
+
+def test_memory_in_a_graph_and_on_another_stream():
+    """Append (both forms), read and recall recorded and replayed, with eager work between."""
+    log("memory graph")
+    rng = np.random.default_rng(12)
+    for pages, hkv, D, n in ((8, 4, 32, 100), (64, 32, 128, 2048)):
+        m = rex.box_memory(pages, hkv, D)
+        make = lambda *shape: torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).cuda()
+        k, v, q = make(n, hkv, D), make(n, hkv, D), make(2, 1, hkv, D)
+        boxes = torch.from_numpy(draw_boxes(rng, (n,))).cuda()
+        slots = torch.from_numpy(rng.permutation(pages * 32)[:n].astype(np.int64)).cuda()
+        table = torch.arange(pages, dtype=torch.int32, device="cuda").expand(2, -1).contiguous()
+        lengths = torch.tensor([pages * 32, 40], dtype=torch.int32, device="cuda")
+
+        def run():
+            rex.box_memory_append(m, slots, k, v, boxes)
+            return (*rex.box_memory_read(m, slots), rex.box_memory_attn_fwd(q, m, table, lengths)[0])
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            run()
+        torch.cuda.current_stream().wait_stream(side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = run()
+        for _ in range(4):
+            k.copy_(make(n, hkv, D))
+            v.copy_(make(n, hkv, D))
+            rex.box_memory_append(m, torch.arange(pages * 32, device="cuda"), *(make(pages * 32, hkv, D) for _ in range(2)),
+                                  torch.zeros(pages * 32, 4, device="cuda"))
+            rest = [t.clone() for t in m]
+            want = [t.clone() for t in run()]
+            for t, r in zip(m, rest):
+                t.copy_(r)
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        # on a given stream, with the current one busy elsewhere
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        rex.box_memory_append(m, slots, k, v, boxes, stream=other)
+        far = rex.box_memory_read(m, slots, stream=other)
+        out, _ = rex.box_memory_attn_fwd(q, m, table, lengths, stream=other)
+        torch.cuda.current_stream().wait_stream(other)
+        assert all(torch.equal(a, b) for a, b in zip((*far, out), want))
+
+
 def test_recall_query_lengths():
     log("recall q_len")
     r = Recall("f32", 3, 20, 100, 4, 4, 32, 7)
