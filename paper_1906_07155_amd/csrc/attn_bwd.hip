@@ -134,12 +134,13 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int row = q0 + 16 * s + n;
-            float d = 0.0f;
+            // out (rows) times grad_out (columns) has delta on its diagonal, summed as dp is: where a
+            // row sees one key and out is its value to the last bit, dp - delta is 0
+            f32x4 t = {};
 #pragma unroll
-            for (int k = 0; k < DB; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    d = fmaf(static_cast<float>(go[s][k][i]), static_cast<float>(o[s][k][i]), d);
+            for (int k = 0; k < DB; ++k) t = N::mma(o[s][k], go[s][k], t);
+            const float mine = n & 2 ? (n & 1 ? t[3] : t[2]) : (n & 1 ? t[1] : t[0]);
+            float d = g == n >> 2 ? mine : 0.0f;
             if (!N::kExact && a.fout_f32) {              // few keys: of what was not rounded
                 d = 0.0f;
                 const int64_t at = ((static_cast<int64_t>(b) * a.Nq + min(row, a.Nq - 1)) * a.H + h) * a.D;
