@@ -88,9 +88,9 @@ re_status_t box_attn_workspace_size(const box_attn_t *a, int32_t backward, size_
 
 /* out: [batch][num_q][heads][dim] dense, of a->dtype.  lse: [batch][heads][num_q] or NULL.
  * out_f32: as out in binary32, not rounded, or NULL.  The backward takes sum_c grad_out * out
- * from it where it is given: with a rounded `out` grad_q carries that rounding, which among
- * many keys is little beside its own, but with few (RE_ATTN_FEW_KEYS) is not.  With out_f32 the
- * weights multiply bf16 data in three parts instead of rounded.
+ * from it where it is given: with a rounded `out` grad_q carries that rounding, which shows where
+ * few keys have nearly all of a row's weight (as they have among RE_ATTN_FEW_KEYS and fewer).  With
+ * out_f32 the weights multiply bf16 data in three parts instead of rounded.
  * workspace: 256-byte aligned. */
 #define RE_ATTN_FEW_KEYS 64
 re_status_t box_attn_fwd(const box_attn_t *a, void *out, float *lse, float *out_f32,

@@ -245,9 +245,9 @@ def box_attn_fwd(q, k, v, *, scale: Optional[float] = None, q_boxes=None, k_boxe
     """Attention of q [B, Nq, H, D] over k, v [B, Nk, Hkv, D] (heads share keys where Hkv < H).
     bias: float32 [H, n, n] by bucket of (q_boxes [B, Nq, 4], k_boxes [B, Nk, 4]); q_len,
     k_len: int32 [B] valid rows; k_mask: bool [B, Nk], False leaves a key out; scale: D^-1/2
-    by default.  Returns (out, lse, out_f32): lse float32 [B, H, Nq] and (for bf16 data and up to
-    64 keys) out_f32, `out` in float32, are what the backward takes, made where `save` is true
-    or they are given, else None."""
+    by default.  Returns (out, lse, out_f32): lse float32 [B, H, Nq] and (for bf16 data) out_f32,
+    `out` in float32, are what the backward takes, made where `save` is true or they are given,
+    else None."""
     torch = _torch()
     d = _attn_descriptor(q, k, v, scale, q_boxes, k_boxes, bias, first_exp, octave_steps, q_len,
                          k_len, k_mask)
@@ -268,7 +268,7 @@ def box_attn_fwd(q, k, v, *, scale: Optional[float] = None, q_boxes=None, k_boxe
             out = c.empty((B, nq, H, D), q.dtype)
         if save and lse is None:
             lse = c.empty((B, H, nq), torch.float32)
-        if save and out_f32 is None and q.dtype == torch.bfloat16 and k.shape[1] <= FEW_KEYS:
+        if save and out_f32 is None and q.dtype == torch.bfloat16:
             out_f32 = c.empty((B, nq, H, D), torch.float32)
         need = 0
         if workspace is None:

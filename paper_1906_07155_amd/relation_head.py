@@ -64,6 +64,10 @@ class GatedNormFunction(torch.autograd.Function):
 def box_attention(q, k, v, *, bias=None, **geo):
     """relation.box_attn_fwd with gradients for q, k, v and bias.  Returns (out, lse); lse has
     no gradient.  `geo`: scale, q_boxes, k_boxes, first_exp, octave_steps, q_len, k_len, k_mask."""
+    if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, bias))):
+        relation._rows4(q, "q")
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+        return relation.box_attn_fwd(q, k, v, bias=bias, lse=lse, **geo)[:2]     # nothing else is kept
     return BoxAttnFunction.apply(q, k, v, bias, geo)
 
 
