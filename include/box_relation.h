@@ -45,7 +45,8 @@ extern "C" {
  * infinities included) has no effect on any result.
  *
  * An entry of bias at or below -1e30 (a type's lowest value, say) counts as -inf: its pairs
- * are left out.
+ * are left out.  Any other is a number: a row whose visible keys are all at -1e9 has the weights
+ * that it has with all of them at 0, and the gradients (lse alone is rounded at that size).
  *
  * The bucket of a pair says where the key's centre lies as seen from the query, in units of
  * the query's sides and by octaves: along x, every operation rounded to binary32,

@@ -383,10 +383,28 @@ __device__ __forceinline__ uint32_t pair_bucket(const BoxGeo &q, float kx, float
 }
 
 // An entry of a head's table in LDS, so that it can be what a logit's sum starts with: in
-// units of the plain products (divided by the scale).  Masks written as a type's lowest
-// value count as -inf: kept as numbers they would drown the logits they are added to.
+// units of the plain products (divided by the scale; what that takes past the finite numbers stays
+// finite).  Masks written as a type's lowest value count as -inf.
+constexpr float kLowest = -1e30f;
 __device__ __forceinline__ float table_entry(float bias, float scale) {
-    return bias <= -1e30f ? -kInf : bias / scale;
+    const float x = bias / scale;
+    return bias <= kLowest ? -kInf : fabsf(x) == kInf ? copysignf(3.4028234664e38f, x) : x;
+}
+// A table with a large entry (a mask of -1e9, say) is not used so: a row all of whose keys are at
+// such an entry needs the differences of its entries and of its products, which the entry would
+// drown.  Its sums start from (entry - offset) / scale, the offset being the row's largest entry, and
+// the entries are those in memory.  (Branches for that cost the other calls some 5 %: forward of 1000
+// boxes in 16 heads of 64 channels 26.2 us without them, 27.3 with; loops of its own in the same
+// kernels cost more, by the registers of both.)
+constexpr float kWideBias = 64.0f;
+__device__ __forceinline__ bool wide_table(const char *tab, int n, float scale, int lane) {
+    bool wide = false;
+#pragma unroll 4
+    for (int i = lane; i < n; i += 64) {
+        const float x = reinterpret_cast<const float *>(tab)[i];
+        wide |= x != -kInf && fabsf(x) * scale > kWideBias;
+    }
+    return __any(wide);
 }
 
 // The table entries of a lane's eight rows: `at` holds 16-bit byte offsets into the head's
@@ -398,6 +416,15 @@ __device__ __forceinline__ void table_gather(u32x4 at, const char *tab, f32x4 (&
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         x[j >> 2][j & 3] = *reinterpret_cast<const float *>(tab + table_offset(at, j));
+}
+// The same of a table in memory, natural units.
+__device__ __forceinline__ float wide_entry(const float *bias, uint32_t offset) {
+    const float x = as_global<float>(bias)[offset / 4];
+    return x <= kLowest ? -kInf : x;
+}
+__device__ __forceinline__ void wide_gather(u32x4 at, const float *bias, f32x4 (&x)[2]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j >> 2][j & 3] = wide_entry(bias, table_offset(at, j));
 }
 
 constexpr int kBuckStride = 40;   // 16-bit entries of one column's 32 rows in LDS (16-byte reads

@@ -13,6 +13,12 @@
 // the pair matrix instead of five), which costs less than adding one side's gradient with
 // atomics, and every element is written once and in a fixed order.
 //
+// A log sum far from 0 is no longer exact enough for that: beside an offset of -1e9 (a mask that all
+// of a row's keys carry) nothing is left of the sum itself, and weights made from it would be off
+// by any factor.  For such rows the query pass first finds the offset, the largest logit and the sum of
+// the weights again, in three sweeps of a wave over the keys; that takes about as long as the pass,
+// and only waves with such a row do it.
+//
 // The bias gradient is a histogram of ds by bucket.  Each wave adds into tables of its own
 // in LDS: LDS serves a wave's additions in order, so the sums repeat bit for bit.  The tables
 // are binary64: an addition of 64 lanes to LDS takes 18 to 30 cycles of a CU there, 193 in
@@ -61,6 +67,15 @@ inline __host__ __device__ BwdLds bwd_lds(int cols, int dp, int hp, int parts, i
     l.total = at > end ? at : end;
     return l;
 }
+
+// Rows whose log sum is this far from 0 get it anew: its rounding, and that of its product with log2 e,
+// would be up to 2^-17 of a weight and more.
+constexpr float kFarLse = 128.0f;
+// Their mark is the last bit of what the key pass is told (2^-24 of a log sum that is near).
+__device__ __forceinline__ float mark_row(float lse, bool far) {
+    return __uint_as_float((__float_as_uint(lse) & ~1u) | (far ? 1u : 0u));
+}
+__device__ __forceinline__ bool row_marked(float lse) { return __float_as_uint(lse) & 1u; }
 
 // Tiles of bf16 rows that a wave keeps in LDS.  Query pass: keys and
 // values, or keys alone for heads of more than 64 channels.  Key pass: queries and upstream
@@ -119,7 +134,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     };
 
     Frag q[NS][DB], go[NS][DB];
-    float lse[NS], delta[NS], sum[NS];
+    float lse[NS], delta[NS], sum[NS], natural_lse[NS];
     {
         const HeadRows qr = head_rows<T>(a.q, b, h, qlen, a.D), gr = head_rows<T>(a.gout, b, h, qlen, a.D);
         const Rows out{a.fout, a.gout.sb, a.gout.sr, a.gout.sh};
@@ -154,33 +169,115 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
             }
             d = sum_over_rows(d);
             const bool none = row >= qlen || lse[s] == -kInf;
-            lse[s] = none ? kInf : lse[s] * kLog2e;
+            natural_lse[s] = none ? 0.0f : lse[s];
+            lse[s] = none ? kInf : mark_row(lse[s] * kLog2e, false);
             delta[s] = none ? 0.0f : d;
             sum[s] = 0.0f;
-            // for the key pass; delta of bf16 data follows at the end
-            gptr<float> st = as_global_mut<float>(a.rowstat) + (bh * a.Nqp + row) * 2;
-            if (kw == 0 && g == 0 && row < a.Nqp) {
-                st[0] = lse[s];
-                if (N::kExact || row >= qlen) st[1] = delta[s];
-            }
-            // 16 columns: the rows that fill up the last 32
-            if (NS == 1 && kw == 0 && g == 1 && q0 + 16 >= a.Nq && row + 16 < a.Nqp) {
-                st[32] = kInf;
-                st[33] = 0.0f;
-            }
         }
     }
+    const float *const bias = BIAS ? a.bias + static_cast<int64_t>(h) * nb2 : nullptr;
+    bool wide = false;                  // (wide_table)
     if (BIAS) {
         for (int i = lane + 64 * kw; i < nb2; i += 64 * parts)
-            reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] =
-                table_entry(as_global<float>(a.bias)[static_cast<int64_t>(h) * nb2 + i], a.scale);
+            reinterpret_cast<float *>(smem + lds.bias + hw * table)[i] = table_entry(as_global<float>(bias)[i], a.scale);
         if (tid < cols) geo[tid] = box_geo(box_load(a.qbox + b * a.qbox_sb + (q0 + tid) * a.qbox_sr));
         // columns without a query: bucket 0 of whatever they hold
         if (cols < kCols)
             for (int i = tid; i < 2 * ahead * parts * kCols * kBuckStride / 2; i += kAttnWaves * 64)
                 reinterpret_cast<uint32_t *>(buck)[i] = 0u;
         __syncthreads();
+        wide = wide_table(tab, nb2, a.scale, lane);
         fill_buckets(0);
+    }
+    // What far rows' logits are relative to: their largest bias and their largest logit.
+    float offset[NS] = {}, peak[NS] = {};
+    bool far_rows = false;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) far_rows |= fabsf(natural_lse[s]) >= kFarLse;
+    far_rows = __any(far_rows);
+    // what a logit's sum starts with, from an entry of a wide table
+    const float per_scale = 1.0f / a.scale;
+    auto start = [&](float entry, int s) { return (entry - offset[s]) * per_scale; };
+    if (far_rows) {
+        float most[NS], most_bias[NS], total[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            most[s] = most_bias[s] = -kInf;
+            total[s] = 0.0f;
+        }
+        // 0: the largest bias (of wide tables), 1: the largest logit, 2: the sum
+        for (int sweep = wide ? 0 : 1; sweep < 3; ++sweep) {
+            for (int tile = 0; tile < t1; ++tile) {
+                f32x4 sc[NS][2] = {};
+                uint32_t on = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int key = tile * kTile + 8 * g + j, at = min(key, a.Nk - 1);
+                    bool live = key < klen;
+                    if (a.kmask) live = live && as_global<uint8_t>(a.kmask)[static_cast<int64_t>(b) * a.Nk + at] != 0;
+                    on |= live ? 1u << j : 0u;
+                    if (BIAS) {
+                        float kx, ky;
+                        box_centre(box_load(a.kbox + b * a.kbox_sb + at * a.kbox_sr), kx, ky);
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) {
+                            const uint32_t to = pair_bucket(geo[min(16 * s + n, max(cols - 1, 0))], kx, ky, a.rule);
+                            sc[s][j >> 2][j & 3] = wide ? wide_entry(bias, to) : *reinterpret_cast<const float *>(tab + to);
+                        }
+                    }
+                }
+                Frag kf[2][DB];
+                if (sweep > 0) koff.frags(kr.at(tile * kTile), tile * kTile + kTile <= klen, kf);
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float e = sc[s][j >> 2][j & 3];
+                        if (sweep == 0) most_bias[s] = on >> j & 1u ? fmaxf(most_bias[s], e) : most_bias[s];
+                        if (wide) sc[s][j >> 2][j & 3] = start(e, s);
+                    }
+                if (sweep == 0) continue;
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int k = 0; k < DB; ++k) sc[s][t] = N::mma(kf[t][k], q[s][k], sc[s][t]);
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float e = on >> j & 1u ? sc[s][j >> 2][j & 3] : -kInf;
+                        if (sweep == 1) most[s] = fmaxf(most[s], e);
+                        else total[s] += __builtin_amdgcn_exp2f((e - peak[s]) * sl2);
+                    }
+            }
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const bool is = fabsf(natural_lse[s]) >= kFarLse;
+                if (sweep == 0) offset[s] = is ? max_over_rows(most_bias[s]) : 0.0f;
+                else if (sweep == 1) peak[s] = is ? max_over_rows(most[s]) : 0.0f;
+                else if (is) lse[s] = mark_row(__builtin_amdgcn_logf(sum_over_rows(total[s])), true);
+            }
+        }
+    }
+    // for the key pass; delta of bf16 data follows at the end
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int row = q0 + 16 * s + n;
+        const int64_t at = ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + row) * 2;
+        gptr<float> st = as_global_mut<float>(a.rowstat) + at;
+        if (kw == 0 && g == 0 && row < a.Nqp) {
+            st[0] = lse[s];
+            if (N::kExact || row >= qlen) st[1] = delta[s];
+            if (far_rows) *(REX_GLOBAL f32x2 *)(a.rowfar + at) = f32x2{offset[s], peak[s]};
+            if (n == 0) as_global_mut<int32_t>(a.far)[(static_cast<int64_t>(b) * a.H + h) * (a.Nqp / 16) + row / 16] = far_rows;
+        }
+        // 16 columns: the rows that fill up the last 32
+        if (NS == 1 && kw == 0 && g == 1 && q0 + 16 >= a.Nq && row + 16 < a.Nqp) {
+            st[32] = kInf;
+            st[33] = 0.0f;
+        }
     }
     f32x4 dq[NS][2 * DB] = {};
     const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
@@ -253,8 +350,51 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
 #pragma unroll
                 for (int k = 0; k < DB; ++k) N::split(kp[k], kt[2 * k], kt[2 * k + 1]);
             }
-            if (vis != 0xffffffffu) {
+            if (vis != 0xffffffffu || __builtin_expect(wide || far_rows, 0)) {
                 const uint32_t mine = vis >> (8 * g);
+                if (__builtin_expect(wide || far_rows, 0)) {   // all of it anew, as the sweeps made their logits
+                    Frag ka[2][DB], va[2][DB];
+                    if constexpr (kLds) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int k = 0; k < DB; ++k) {
+                                ka[t][k] = rows.rows(t, k);
+                                if constexpr (kBoth) va[t][k] = rows.rows(t, k, 1);
+                            }
+                    } else {
+                        koff.frags(rk, inside, ka);
+                    }
+                    if constexpr (!kBoth) voff.frags(rv, inside, va);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        sc[s][0] = sc[s][1] = f32x4{};
+                        if (BIAS) {
+                            const u32x4 to = *reinterpret_cast<const u32x4 *>(bk + 16 * s * kBuckStride);
+                            if (wide) wide_gather(to, bias, sc[s]);
+                            else table_gather(to, tab, sc[s]);
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            dp[s][t] = f32x4{};
+                            if (wide) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) sc[s][t][i] = start(sc[s][t][i], s);
+                            }
+#pragma unroll
+                            for (int k = 0; k < DB; ++k) {
+                                sc[s][t] = N::mma(ka[t][k], q[s][k], sc[s][t]);
+                                dp[s][t] = N::mma(va[t][k], go[s][k], dp[s][t]);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float p = __builtin_amdgcn_exp2f(fmaf(sc[s][t][i] - peak[s], sl2, -lse[s]));
+                                x[s][4 * t + i] = p * (dp[s][t][i] - delta[s]);
+                                dp[s][t][i] *= p;
+                            }
+                        }
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -356,7 +496,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
     const int klen = a.klen ? min(max(a.klen[b], 0), a.Nk) : a.Nk;
     f32x2 *ctr = reinterpret_cast<f32x2 *>(smem + lds.geo);
     uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
-    const float sl2 = a.scale * kLog2e;
+    const float sl2 = a.scale * kLog2e, per_scale = 1.0f / a.scale;
     // entry off / 4 of the lane's copy of table c is at hist + c * nb2 * 8 * copies + off * 2 * copies
     const int copies = lds.copies, log_copies = 32 - __builtin_clz(copies);
     double *const tables = reinterpret_cast<double *>(smem + lds.hist) + wave * a.head_step * nb2 * copies;
@@ -422,8 +562,16 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
 
         f32x4 dk[NS][2 * DB] = {}, dv[NS][2 * DB] = {}, st_next[4];
         const int steps = (t1 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
+        uint32_t wides = 0, special = 0;  // heads of these whose tables are wide; and those with far rows
         for (int first = 0; first < a.group; first += a.head_step) {
             const int many = min(a.head_step, a.group - first);
+            special = 0;
+            for (int c = 0; c < many; ++c) {
+                gcptr<int32_t> far = as_global<int32_t>(a.far) + (static_cast<int64_t>(b) * a.H + kh * a.group + first + c) * (a.Nqp / 16);
+                bool some = false;
+                for (int i = lane; i < (a.Nq + 15) / 16; i += 64) some |= far[i] != 0;
+                special |= __any(some) ? 1u << c : 0u;
+            }
             if (BIAS) {
                 __syncthreads();          // the tables of the last heads have been read
                 for (int c = 0; c < many; ++c)
@@ -436,6 +584,12 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
             for (int chunk = 0; chunk < chunks; ++chunk) {
                 if (BIAS) {
                     __syncthreads();
+                    if (chunk == 0) {
+                        wides = 0;
+                        for (int c = 0; c < many; ++c)
+                            wides |= wide_table(smem + lds.bias + (hw * a.head_step + c) * table, nb2, a.scale, lane) ? 1u << c : 0u;
+                        special |= wides;
+                    }
                     if (chunk + 1 < chunks) fill_buckets(chunk + 1);
                 }
                 for (int it = 0; it < ahead; ++it) {
@@ -486,6 +640,26 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                                 table_gather(at[s], tab, sc[s]);
                             }
                         }
+                        // heads of wide tables or with far rows: what a row's logits are relative to
+                        const bool other = special >> c & 1u;
+                        f32x4 peak[2] = {};
+                        if (__builtin_expect(other, 0)) {
+                            const bool wide = wides >> c & 1u;
+                            const float *from = a.rowfar + ((static_cast<int64_t>(b) * a.H + h) * a.Nqp + tile * kTile + 8 * g) * 2;
+                            if (BIAS && wide) {
+#pragma unroll
+                                for (int s = 0; s < NS; ++s) wide_gather(at[s], a.bias + static_cast<int64_t>(h) * nb2, sc[s]);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                f32x2 x = {};
+                                if (row_marked(st[j >> 1][2 * (j & 1)])) x = *(const REX_GLOBAL f32x2 *)(from + 2 * j);
+                                peak[j >> 2][j & 3] = x[1];
+#pragma unroll
+                                for (int s = 0; s < NS; ++s)
+                                    if (wide) sc[s][j >> 2][j & 3] = (sc[s][j >> 2][j & 3] - x[0]) * per_scale;
+                            }
+                        }
                         float pr[NS][8], ds[NS][8];
                         Frag qf[2][DB], gf[2][DB];
                         if constexpr (!kLds) {
@@ -509,6 +683,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                                     sc[s][t] = N::mma(qf[t][k], kf[s][k], sc[s][t]);
                                     dp = N::mma(gf[t][k], vf[s][k], dp);
                                 }
+                                if (__builtin_expect(other, 0)) sc[s][t] -= peak[t];
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     const f32x4 two = st[2 * t + (i >> 1)];

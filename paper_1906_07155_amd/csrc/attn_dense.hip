@@ -6,7 +6,7 @@ namespace rex {
 namespace {
 
 // Joins the partial results of the key splits: a thread for eight channels of one row.
-// Reads nsplit * (D + 2) floats per row once: bytes bound.
+// Reads nsplit * (D + 4) floats per row once: bytes bound.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
     using N = Num<T>;
@@ -19,19 +19,18 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
     const int row = static_cast<int>(r % a.Nq), h = static_cast<int>(r / a.Nq % a.H);
     const int b = static_cast<int>(r / (static_cast<int64_t>(a.Nq) * a.H));
     const int qlen = a.qlen ? min(max(a.qlen[b], 0), a.Nq) : a.Nq;
-    float mx = -kInf, sum = 0.0f, x[8] = {};
+    float sum = 0.0f, x[8] = {};
+    SumRef to = load_ref(a.part_ml + r);
     if (row < qlen) {
-        for (int s = 0; s < a.nsplit; ++s)
-            mx = fmaxf(mx, as_global<float>(a.part_ml)[(s * rows + r) * 2]);
-        const float ref = mx == -kInf ? 0.0f : mx;
+        for (int s = 1; s < a.nsplit; ++s) reach(to, load_ref(a.part_ml + s * rows + r));
         for (int s = 0; s < a.nsplit; ++s) {
-            const f32x2 ml = *(const REX_GLOBAL f32x2 *)(a.part_ml + (s * rows + r) * 2);
-            const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
-            const f32x8 p = Num<float>::load(reinterpret_cast<const char *>(
+            const SumRef p = load_ref(a.part_ml + s * rows + r);
+            const float f = __builtin_amdgcn_exp2f(ref_gap(p, to));
+            const f32x8 y = Num<float>::load(reinterpret_cast<const char *>(
                 a.part + (s * rows + r) * a.D + ch));
-            sum = fmaf(ml[1], f, sum);
+            sum = fmaf(p.sum, f, sum);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = fmaf(p[i], f, x[i]);
+            for (int i = 0; i < 8; ++i) x[i] = fmaf(y[i], f, x[i]);
         }
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -41,7 +40,7 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
     N::store(static_cast<char *>(a.out) + at, x);
     if (a.out_f32) Num<float>::store(reinterpret_cast<char *>(a.out_f32) + at * (4 / N::kSize), x);
     if (ch == 0 && a.lse)
-        as_global_mut<float>(a.lse)[r] = sum != 0.0f ? (mx + log2f(sum)) * kLn2 : -kInf;
+        as_global_mut<float>(a.lse)[r] = row_lse(SumRef{to.offset, sum, to.rest});
 }
 
 }  // namespace

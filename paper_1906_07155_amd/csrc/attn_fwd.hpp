@@ -24,9 +24,12 @@
 
 namespace rex {
 
+// Exponents whose rounding is no longer far below 1: beyond, they are taken from the maximum itself.
+constexpr float kFarExponent = 1024.0f;
+
 // What is in LDS, in bytes from its start.
 struct FwdLds {
-    int bias, geo, buck, tile, ml, acc, total;
+    int bias, geo, buck, tile, ref, near, acc, total;
 };
 // Steps whose buckets are computed between two barriers.
 inline __host__ __device__ int fwd_ahead(int parts) { return parts >= 2 ? 1 : 2; }
@@ -43,8 +46,10 @@ inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, i
     at += kAttnWaves * tiles * kTile * dp * 2;        // each wave's tiles of bf16 rows
     const int loop = at;
     at = 0;                       // the end: the loop's tables are no longer needed
-    l.ml = at;
-    if (parts > 1) at += hp * parts * cols * 8;
+    l.ref = at;
+    if (parts > 1) at += hp * parts * cols * static_cast<int>(sizeof(SumRef));
+    l.near = at;
+    if (parts > 1) at += hp * parts * cols * 4;
     l.acc = at;
     if (parts > 1) at += hp * parts * cols * (dp + 4) * 4;
     l.total = at > loop ? at : loop;
@@ -57,6 +62,24 @@ inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, i
 // 27.2 us then, 26.2 as it is.)
 template <typename T, int DB, bool PAGED>
 constexpr int fwd_tiles() { return PAGED || sizeof(T) == 4 ? 0 : DB <= 2 ? 2 : 1; }
+
+// The sums of a row's parts are joined relative to the part whose exponent is the largest.  Both
+// differences are exact wherever they are small enough to matter; a part without a key has none.
+__device__ __forceinline__ float ref_gap(const SumRef &p, const SumRef &to) {
+    const float gap = (p.offset - to.offset) * kLog2e + static_cast<float>(p.rest - to.rest);
+    return p.rest == -static_cast<double>(kInf) ? -kInf : gap;
+}
+__device__ __forceinline__ void reach(SumRef &to, const SumRef &p) {
+    if (to.rest == -static_cast<double>(kInf) || ref_gap(p, to) > 0.0f) to = p;
+}
+__device__ __forceinline__ SumRef load_ref(const SumRef *p) {
+    const f32x4 x = *(const REX_GLOBAL f32x4 *)(p);
+    return __builtin_bit_cast(SumRef, x);
+}
+__device__ __forceinline__ float row_lse(const SumRef &r) {
+    if (r.sum == 0.0f) return -kInf;
+    return static_cast<float>((r.rest + log2f(r.sum)) * 0.69314718055994530942 + r.offset);
+}
 
 template <typename T, int DB, int NS, bool BIAS, bool PAGED, int TERMS>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a) {
@@ -93,8 +116,8 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
     const int cols = min(max(qlen - q0, 0), kCols);       // columns that hold a query
     BoxGeo *geo = reinterpret_cast<BoxGeo *>(smem + lds.geo);
     uint16_t *buck = reinterpret_cast<uint16_t *>(smem + lds.buck);
+    const int nb2 = a.rule.nb * a.rule.nb;
     if (BIAS) {
-        const int nb2 = a.rule.nb * a.rule.nb;
         float *t = reinterpret_cast<float *>(smem + lds.bias);
         gcptr<float> src = as_global<float>(a.bias + static_cast<int64_t>(h0) * nb2);
         for (int i = tid; i < hp * nb2; i += kAttnWaves * 64) t[i] = table_entry(src[i], a.scale);
@@ -216,16 +239,19 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
     };
 
     const float sl2 = a.scale * kLog2e;
-    const char *tab = smem + lds.bias + hw * a.rule.nb * a.rule.nb * 4;
+    const char *tab = smem + lds.bias + hw * nb2 * 4;
     f32x4 o[NS][2 * DB] = {};      // 16-channel tiles 2k, 2k + 1: even and odd channels
     // The running maximum, in units of the products; what exponents are taken from (m in units
-    // of log 2, 0 while there is no key); the sum.
-    float m[NS], ref[NS], l[NS];
-    const float slack = 8.0f / sl2;
+    // of log 2, 0 while there is no key); the sum.  Where logits are so large that m in units of
+    // log 2 would be off by a part of 1 (`far`), m is taken off the logits first and ref is 0.  With
+    // a wide table m and the products' sums are relative to the row's largest entry so far.
+    float m[NS], ref[NS], l[NS], offset[NS];
+    bool far = false, wide = false;     // (wide: wide_table)
+    const float slack = 8.0f / sl2, per_scale = 1.0f / a.scale;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
         m[s] = -kInf;
-        ref[s] = l[s] = 0.0f;
+        ref[s] = l[s] = offset[s] = 0.0f;
     }
     const int steps = (t1 - t0 + parts - 1) / parts, chunks = (steps + ahead - 1) / ahead;
     if (t0 + kw < t1) {
@@ -235,6 +261,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
     if (BIAS) {
         load_boxes(0);
         __syncthreads();
+        wide = far = wide_table(tab, nb2, a.scale, lane);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) offset[s] = wide ? -kInf : 0.0f;
         fill_buckets(0);
         load_boxes(1);
     }
@@ -263,6 +292,24 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
             for (int s = 0; s < NS; ++s) {
                 x[s][0] = x[s][1] = f32x4{};
                 if (BIAS) table_gather(*reinterpret_cast<const u32x4 *>(bk + 16 * s * kBuckStride), tab, x[s]);
+            }
+            if (BIAS && __builtin_expect(wide, 0)) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    wide_gather(*reinterpret_cast<const u32x4 *>(bk + 16 * s * kBuckStride),
+                                a.bias + static_cast<int64_t>(h) * nb2, x[s]);
+                    float top = -kInf;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) top = vis >> (8 * g + j) & 1u ? fmaxf(top, x[s][j >> 2][j & 3]) : top;
+                    top = max_over_rows(top);
+                    if (top > offset[s]) {       // m is where it was, as seen from the new offset
+                        m[s] -= (top - offset[s]) * per_scale;
+                        offset[s] = top;
+                    }
+                    const float from = offset[s] == -kInf ? 0.0f : offset[s];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[s][j >> 2][j & 3] = (x[s][j >> 2][j & 3] - from) * per_scale;
+                }
             }
             // column = query n, rows = keys 8g + 4t + e
 #pragma unroll
@@ -338,16 +385,27 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
                 for (int j = 1; j < 8; ++j) top[s] = fmaxf(top[s], x[s][j >> 2][j & 3]);
                 grew |= top[s] > m[s] + slack;
             }
-            if (__any(grew)) {
+            if (__any(grew) || far) {
+                bool large = false;
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
-                    const float mn = fmaxf(m[s], max_over_rows(top[s]));
-                    const float f = __builtin_amdgcn_exp2f((m[s] - (mn == -kInf ? 0.0f : mn)) * sl2);
+                    const float mn = fmaxf(m[s], max_over_rows(top[s])), from = mn == -kInf ? 0.0f : mn;
+                    const float f = __builtin_amdgcn_exp2f((m[s] - from) * sl2);
                     m[s] = mn;
-                    ref[s] = mn == -kInf ? 0.0f : mn * sl2;
+                    ref[s] = from * sl2;
+                    large |= fabsf(ref[s]) > kFarExponent;
                     l[s] *= f;
 #pragma unroll
                     for (int k = 0; k < 2 * DB; ++k) o[s][k] *= f;
+                }
+                far = far || __any(large);
+                if (__builtin_expect(far, 0)) {
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        ref[s] = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[s][j >> 2][j & 3] -= m[s] == -kInf ? 0.0f : m[s];
+                    }
                 }
             }
             float p[NS][8];
@@ -366,24 +424,25 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
             for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(vf, p[s], o[s]);
         }
     }
+    SumRef sums[NS];
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        l[s] = sum_over_rows(l[s]);
-        m[s] = m[s] == -kInf ? -kInf : ref[s];       // from here on in units of log 2
+        const double rest = far ? static_cast<double>(m[s]) * static_cast<double>(sl2) : ref[s];
+        sums[s] = SumRef{offset[s], sum_over_rows(l[s]), m[s] == -kInf ? -static_cast<double>(kInf) : rest};
     }
 
     // four channels of one row to where they belong
-    auto finish = [&](int col, int head, int ch, float mx, float sum, f32x4 x) {
+    auto finish = [&](int col, int head, int ch, const SumRef &r, f32x4 x) {
         const int row = q0 + col;
         if (row >= a.Nq) return;
         if (a.nsplit > 1) {
             if (row >= qlen) return;
             const int64_t at = ((static_cast<int64_t>(split) * a.B + b) * a.H + head) * a.Nq + row;
             if (ch < a.D) *(REX_GLOBAL f32x4 *)(a.part + at * a.D + ch) = x;
-            if (ch == 0) *(REX_GLOBAL f32x2 *)(a.part_ml + at * 2) = f32x2{mx, sum};
+            if (ch == 0) *(REX_GLOBAL f32x4 *)(a.part_ml + at) = __builtin_bit_cast(f32x4, r);
             return;
         }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float inv = r.sum == 0.0f ? 0.0f : 1.0f / r.sum;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = row < qlen ? x[i] * inv : 0.0f;
         const int64_t at = ((static_cast<int64_t>(b) * a.Nq + row) * a.H + head) * a.D + ch;
@@ -393,7 +452,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         }
         if (ch == 0 && a.lse)
             as_global_mut<float>(a.lse)[(static_cast<int64_t>(b) * a.H + head) * a.Nq + row] =
-                row < qlen && sum != 0.0f ? (mx + log2f(sum)) * kLn2 : -kInf;
+                row < qlen ? row_lse(r) : -kInf;
     };
 
     if (parts == 1) {
@@ -401,40 +460,62 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_fwd_kernel(AttnArgs a
         for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int u = 0; u < 2 * DB; ++u)
-                finish(16 * s + n, h, quad_channel<kNatural>(u, g), m[s], l[s], quad_values<kNatural>(o[s], u));
+                finish(16 * s + n, h, quad_channel<kNatural>(u, g), sums[s], quad_values<kNatural>(o[s], u));
         return;
     }
-    // The waves of a head meet: maxima and sums first, then the scaled sums of the values.
-    f32x2 *ml = reinterpret_cast<f32x2 *>(smem + lds.ml);
+    // The waves of a head meet: what their sums refer to first, then the scaled sums of the values,
+    // with that of the weights in the first of a row's four spare places.  A reference is one number
+    // in units of log 2, or (+inf, and what it stands for beside it) that of a wave whose logits are far.
+    float *near_refs = reinterpret_cast<float *>(smem + lds.near);
+    SumRef *far_refs = reinterpret_cast<SumRef *>(smem + lds.ref);
     float *acc = reinterpret_cast<float *>(smem + lds.acc);
+    auto join = [&](int head, int col) {
+        float top = -kInf;
+        for (int p = 0; p < parts; ++p) top = fmaxf(top, near_refs[(p * hp + head) * kCols + col]);
+        return top;
+    };
+    auto join_far = [&](int head, int col) {
+        SumRef to = far_refs[head * kCols + col];
+        for (int p = 1; p < parts; ++p) reach(to, far_refs[(p * hp + head) * kCols + col]);
+        return to;
+    };
     __syncthreads();                        // the tables of the loop are overwritten
     if (g == 0) {
 #pragma unroll
-        for (int s = 0; s < NS; ++s) ml[wave * kCols + 16 * s + n] = f32x2{m[s], l[s]};
+        for (int s = 0; s < NS; ++s) {
+            near_refs[wave * kCols + 16 * s + n] = m[s] == -kInf ? -kInf : far ? kInf : ref[s];
+            far_refs[wave * kCols + 16 * s + n] = sums[s];
+        }
     }
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        float mx = -kInf;
-        for (int p = 0; p < parts; ++p) mx = fmaxf(mx, ml[(p * hp + hw) * kCols + 16 * s + n][0]);
-        const float f = __builtin_amdgcn_exp2f(m[s] - (mx == -kInf ? 0.0f : mx));
+        const float top = join(hw, 16 * s + n);
+        float f = __builtin_amdgcn_exp2f((m[s] == -kInf ? -kInf : ref[s]) - (top == -kInf ? 0.0f : top));
+        if (top == kInf) f = __builtin_amdgcn_exp2f(ref_gap(sums[s], join_far(hw, 16 * s + n)));
+        float *dst = acc + (wave * kCols + 16 * s + n) * (kDP + 4);
+        if (g == 0) dst[kDP] = sums[s].sum * f;
 #pragma unroll
         for (int u = 0; u < 2 * DB; ++u)
-            *reinterpret_cast<f32x4 *>(acc + (wave * kCols + 16 * s + n) * (kDP + 4) + quad_channel<kNatural>(u, g)) =
-                quad_values<kNatural>(o[s], u) * f;
+            *reinterpret_cast<f32x4 *>(dst + quad_channel<kNatural>(u, g)) = quad_values<kNatural>(o[s], u) * f;
     }
     __syncthreads();
     for (int e = tid; e < hp * kCols * DB * 8; e += kAttnWaves * 64) {
         const int ch = (e % (DB * 8)) * 4, col = (e / (DB * 8)) % kCols, w = e / (DB * 8 * kCols);
-        float mx = -kInf, sum = 0.0f;
+        SumRef r{};
         f32x4 x = {};
-        for (int p = 0; p < parts; ++p) mx = fmaxf(mx, ml[(p * hp + w) * kCols + col][0]);
-        for (int p = 0; p < parts; ++p) {
-            const f32x2 v = ml[(p * hp + w) * kCols + col];
-            sum += v[1] * __builtin_amdgcn_exp2f(v[0] - (mx == -kInf ? 0.0f : mx));
-            x += *reinterpret_cast<const f32x4 *>(acc + ((p * hp + w) * kCols + col) * (kDP + 4) + ch);
+        if (ch == 0 && (a.lse || a.nsplit > 1)) {
+            const float top = join(w, col);
+            r.rest = top;
+            if (top == kInf) r = join_far(w, col);
         }
-        finish(col, h0 + w, ch, mx, sum, x);
+        r.sum = 0.0f;
+        for (int p = 0; p < parts; ++p) {
+            const float *src = acc + ((p * hp + w) * kCols + col) * (kDP + 4);
+            r.sum += src[kDP];
+            x += *reinterpret_cast<const f32x4 *>(src + ch);
+        }
+        finish(col, h0 + w, ch, r, x);
     }
 }
 

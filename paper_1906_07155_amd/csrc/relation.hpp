@@ -10,7 +10,6 @@ constexpr int kTile = 32;          // keys of one step of the attention, boxes o
 constexpr int kAttnWaves = 8;      // waves of one attention workgroup
 constexpr int kLdsBytes = 160 << 10;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 // One side's rows: [batch][row][head][channel], strides in bytes.
 struct Rows {
@@ -23,6 +22,15 @@ struct Rows {
 // clamped to [0, half].
 struct BucketRule {
     int32_t nb, half, shift, base;
+};
+
+// Sums of a row's weights: `sum` of them, relative to the exponent
+// offset * log2 e + rest (in units of log 2).  The two parts of it stay apart, since a large offset
+// (of the biases, natural) would swallow the rest, and the rest is binary64 for the sake of large
+// products.
+struct SumRef {
+    float offset, sum;
+    double rest;
 };
 
 struct AttnArgs {
@@ -46,7 +54,8 @@ struct AttnArgs {
     void *out;
     float *out_f32, *lse;
     int32_t terms;                      // parts of the weights that multiply bf16 data (add_weighted)
-    float *part, *part_ml;              // nsplit > 1: partial sums [nsplit][B][H][Nq][D], [..][2]
+    float *part;                        // nsplit > 1: partial sums [nsplit][B][H][Nq][D],
+    SumRef *part_ml;                   // and what they refer to [nsplit][B][H][Nq]
     int32_t nsplit;
     // how a workgroup's waves are shared out: heads x parts of the streamed side
     int32_t hp, parts;
@@ -59,6 +68,8 @@ struct AttnArgs {
     void *gq, *gk, *gv;
     float *gbias;
     float *rowstat;                     // [B][H][Nqp][2]: lse in units of log 2 (+inf: no row), delta
+    float *rowfar;                      // [B][H][Nqp][2]: of rows with a far lse, what it is relative to
+    int32_t *far;                       // [B][H][Nqp / 16]: whether there are such among 16 rows
     float *hist;                        // [B * spans][H][nb * nb]
     int32_t Nqp;
     int32_t span, spans;                // key tiles of one workgroup, runs of them per image

@@ -146,14 +146,14 @@ void plan_fwd(AttnArgs &a, int *cols) {
 size_t fwd_bytes(const AttnArgs &a) {
     if (a.nsplit <= 1) return 0;
     const size_t rows = static_cast<size_t>(a.nsplit) * a.B * a.H * a.Nq;
-    return align256(rows * a.D * 4) + align256(rows * 8);
+    return align256(rows * a.D * 4) + align256(rows * sizeof(SumRef));
 }
 
 void place_fwd(AttnArgs &a, void *ws) {
     if (a.nsplit <= 1) return;
     const size_t rows = static_cast<size_t>(a.nsplit) * a.B * a.H * a.Nq;
     a.part = static_cast<float *>(ws);
-    a.part_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(rows * a.D * 4));
+    a.part_ml = reinterpret_cast<SumRef *>(static_cast<char *>(ws) + align256(rows * a.D * 4));
 }
 
 // The backward's two passes.
@@ -188,12 +188,13 @@ void plan_bwd(const AttnArgs &a, int dtype, AttnArgs *dq, AttnArgs *dkv, int *dq
     }
 }
 
-size_t stat_bytes(const AttnArgs &dq) {
+size_t stat_bytes(const AttnArgs &dq) {          // of rowstat, and of rowfar
     return align256(static_cast<size_t>(dq.B) * dq.H * dq.Nqp * 8);
 }
+size_t far_bytes(const AttnArgs &dq) { return align256(static_cast<size_t>(dq.B) * dq.H * dq.Nqp / 4); }
 size_t bwd_bytes(const AttnArgs &dkv) {
     const size_t nb2 = static_cast<size_t>(dkv.rule.nb) * dkv.rule.nb;
-    return stat_bytes(dkv) + (dkv.bias ? align256(static_cast<size_t>(dkv.B) * dkv.spans * dkv.H * nb2 * 4) : 0);
+    return 2 * stat_bytes(dkv) + far_bytes(dkv) + (dkv.bias ? align256(static_cast<size_t>(dkv.B) * dkv.spans * dkv.H * nb2 * 4) : 0);
 }
 
 re_status_t attn_args(const box_attn_t *d, AttnArgs *a) {
@@ -434,8 +435,11 @@ re_status_t box_attn_bwd(const box_attn_t *d, const void *grad_out, const void *
     if ((st = check_workspace(workspace, workspace_bytes, bwd_bytes(dkv))) != RE_OK) return st;
     dq.terms = weight_terms(static_cast<int64_t>(a.B) * a.Nq * a.H * a.D);
     dkv.terms = weight_terms(static_cast<int64_t>(a.B) * a.Nk * a.Hkv * a.D);
-    dq.rowstat = dkv.rowstat = static_cast<float *>(workspace);
-    dkv.hist = reinterpret_cast<float *>(static_cast<char *>(workspace) + stat_bytes(dkv));
+    char *ws = static_cast<char *>(workspace);
+    dq.rowstat = dkv.rowstat = reinterpret_cast<float *>(ws);
+    dq.rowfar = dkv.rowfar = reinterpret_cast<float *>(ws += stat_bytes(dkv));
+    dq.far = dkv.far = reinterpret_cast<int32_t *>(ws += stat_bytes(dkv));
+    dkv.hist = reinterpret_cast<float *>(ws + far_bytes(dkv));
     return from_hip(launch_attn_bwd(dq, dkv, d->dtype, c0, c1, static_cast<hipStream_t>(stream)));
 }
 
