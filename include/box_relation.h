@@ -17,9 +17,8 @@
  *
  * Data of RE_DTYPE_BF16 or RE_DTYPE_F32; parameters (bias, weights, gates), their gradients
  * and statistics are binary32.  Products of bf16 data are exact and summed in binary32; the
- * weights of the softmax and the gradient of the logits are rounded to bf16 where they
- * multiply bf16 data (to two or three such parts where the results are few), and every result
- * is rounded once when it is stored.
+ * weights of the softmax and the gradient of the logits multiply bf16 data in two parts (all but
+ * 2^-17 of them, whatever the size of a call), and every result is rounded once when it is stored.
  */
 #ifndef BOX_RELATION_H
 #define BOX_RELATION_H
@@ -90,8 +89,8 @@ re_status_t box_attn_workspace_size(const box_attn_t *a, int32_t backward, size_
 /* out: [batch][num_q][heads][dim] dense, of a->dtype.  lse: [batch][heads][num_q] or NULL.
  * out_f32: as out in binary32, not rounded, or NULL.  The backward takes sum_c grad_out * out
  * from it where it is given: with a rounded `out` grad_q carries that rounding, which shows where
- * few keys have nearly all of a row's weight (as they have among RE_ATTN_FEW_KEYS and fewer).  With
- * out_f32 the weights multiply bf16 data in three parts instead of rounded.
+ * few keys have nearly all of a row's weight.  With out_f32 and no more than RE_ATTN_FEW_KEYS keys
+ * the weights multiply bf16 data in three parts, that is whole.
  * workspace: 256-byte aligned. */
 #define RE_ATTN_FEW_KEYS 64
 re_status_t box_attn_fwd(const box_attn_t *a, void *out, float *lse, float *out_f32,

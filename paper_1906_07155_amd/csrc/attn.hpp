@@ -70,7 +70,7 @@ template <> struct Num<uint16_t> {    // bf16
         for (int j = 0; j < 8; ++j) f[j] = static_cast<__bf16>(x[j]);
         return f;
     }
-    static constexpr bool kExact = false;     // round() cuts off
+    static constexpr bool kExact = false;     // round() rounds
     // x cut to bf16 (toward zero: one operation, and the rest is exact), and x left with what
     // that cut off
     static __device__ __forceinline__ Frag cut_off(float (&x)[8]) {
@@ -158,8 +158,11 @@ template <> struct Num<float> {
     }
 };
 
-// acc += A x for weights x of which bf16 takes the first TERMS parts of eight bits: 1 rounds
-// them, 2 leaves up to 2^-16 of them out, 3 nothing.
+// acc += A x for weights x of which bf16 takes the first TERMS parts of eight bits: 2 leaves up to
+// 2^-17 of them out, far below what rounding a bf16 result does, and 3 nothing.  (One part, that is
+// weights rounded to bf16, would add as much error as the result's own rounding: 2.3e-3 of the results'
+// norm instead of 1.7e-3.  16 images of up to 1000 boxes in 16 heads of 64 channels: forward 181 us
+// with one part, 210 with two, 232 with three; backward 700 and 756.)
 template <typename T, int TERMS, int NT>
 __device__ __forceinline__ void add_weighted(const typename Num<T>::Frag (&rows)[NT], float (&x)[8],
                                              f32x4 (&acc)[NT]) {

@@ -83,7 +83,7 @@ __device__ __forceinline__ bool row_marked(float lse) { return __float_as_uint(l
 template <typename T, int DB> constexpr int dq_tiles() { return sizeof(T) == 4 ? 0 : DB <= 2 ? 2 : 1; }
 template <typename T, int DB> constexpr bool dkv_lds() { return sizeof(T) == 2 && DB <= 2; }
 
-template <typename T, int DB, int NS, bool BIAS, int TERMS>
+template <typename T, int DB, int NS, bool BIAS>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a) {
     using N = Num<T>;
     using Frag = typename N::Frag;
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
             for (int k = 0; k < DB; ++k) t = N::mma(o[s][k], go[s][k], t);
             const float mine = n & 2 ? (n & 1 ? t[3] : t[2]) : (n & 1 ? t[1] : t[0]);
             float d = g == n >> 2 ? mine : 0.0f;
-            if (!N::kExact && a.fout_f32) {              // few keys: of what was not rounded
+            if (!N::kExact && a.fout_f32) {              // of what was not rounded
                 d = 0.0f;
                 const int64_t at = ((static_cast<int64_t>(b) * a.Nq + min(row, a.Nq - 1)) * a.H + h) * a.D;
 #pragma unroll 1
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
                     for (int j = 0; j < 8; ++j) sum[s] += dp[s][j >> 2][j & 3];
             }
 #pragma unroll
-            for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(kt, x[s], dq[s]);
+            for (int s = 0; s < NS; ++s) add_weighted<T, 2, 2 * DB>(kt, x[s], dq[s]);
         }
     }
     auto finish = [&](int col, int head, int ch, f32x4 x) {
@@ -469,7 +469,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
     }
 }
 
-template <typename T, int DB, int NS, bool BIAS, int TERMS>
+template <typename T, int DB, int NS, bool BIAS>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a) {
     using N = Num<T>;
     using Frag = typename N::Frag;
@@ -723,7 +723,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                                 for (int k = 0; k < DB; ++k) N::split(p[k], gt[2 * k], gt[2 * k + 1]);
                             }
 #pragma unroll
-                            for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(gt, pr[s], dv[s]);
+                            for (int s = 0; s < NS; ++s) add_weighted<T, 2, 2 * DB>(gt, pr[s], dv[s]);
                         }
                         Frag qt[2 * DB];
                         if constexpr (kLds) {
@@ -740,7 +740,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                             for (int k = 0; k < DB; ++k) N::split(p[k], qt[2 * k], qt[2 * k + 1]);
                         }
 #pragma unroll
-                        for (int s = 0; s < NS; ++s) add_weighted<T, TERMS, 2 * DB>(qt, ds[s], dk[s]);
+                        for (int s = 0; s < NS; ++s) add_weighted<T, 2, 2 * DB>(qt, ds[s], dk[s]);
                     }
                 }
             }
@@ -821,7 +821,7 @@ __global__ __launch_bounds__(1024) void attn_hist_kernel(AttnArgs a) {
     }
 }
 
-template <typename T, int DB, int NS, int TERMS>
+template <typename T, int DB, int NS>
 void run_pass(const AttnArgs &a, bool keys, hipStream_t s) {
     if (a.nwg == 0) return;
     const dim3 grid(xcd_grid(a.nwg, a.per)), block(kAttnWaves * 64);
@@ -829,32 +829,31 @@ void run_pass(const AttnArgs &a, bool keys, hipStream_t s) {
     const BwdLds lds = bwd_lds(16 * NS, 32 * DB, a.hp, a.parts, keys ? a.head_step : 1, a.rule.nb,
                                bias, keys, !keys ? dq_tiles<T, DB>() : dkv_lds<T, DB>() ? 2 : 0);
     if (keys && bias)
-        hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, true, TERMS>), grid, block, lds.total, s, a);
+        hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, true>), grid, block, lds.total, s, a);
     else if (keys)
-        hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, false, TERMS>), grid, block, lds.total, s, a);
+        hipLaunchKernelGGL((attn_dkv_kernel<T, DB, NS, false>), grid, block, lds.total, s, a);
     else if (bias)
-        hipLaunchKernelGGL((attn_dq_kernel<T, DB, NS, true, TERMS>), grid, block, lds.total, s, a);
+        hipLaunchKernelGGL((attn_dq_kernel<T, DB, NS, true>), grid, block, lds.total, s, a);
     else
-        hipLaunchKernelGGL((attn_dq_kernel<T, DB, NS, false, TERMS>), grid, block, lds.total, s, a);
+        hipLaunchKernelGGL((attn_dq_kernel<T, DB, NS, false>), grid, block, lds.total, s, a);
 }
 
-template <typename T, int TERMS>
+template <typename T>
 void run_sized(const AttnArgs &a, bool keys, int cols, hipStream_t s) {
     if (a.D <= 32) {
-        if (cols == 16) run_pass<T, 1, 1, TERMS>(a, keys, s);
-        else run_pass<T, 1, 2, TERMS>(a, keys, s);
+        if (cols == 16) run_pass<T, 1, 1>(a, keys, s);
+        else run_pass<T, 1, 2>(a, keys, s);
     } else if (a.D <= 64) {
-        if (cols == 16) run_pass<T, 2, 1, TERMS>(a, keys, s);
-        else run_pass<T, 2, 2, TERMS>(a, keys, s);
+        if (cols == 16) run_pass<T, 2, 1>(a, keys, s);
+        else run_pass<T, 2, 2>(a, keys, s);
     } else {
-        run_pass<T, 4, 1, TERMS>(a, keys, s);
+        run_pass<T, 4, 1>(a, keys, s);
     }
 }
 
 void run_typed(const AttnArgs &a, int dtype, bool keys, int cols, hipStream_t s) {
-    if (dtype == kF32) run_sized<float, 1>(a, keys, cols, s);
-    else if (a.terms > 1) run_sized<uint16_t, 2>(a, keys, cols, s);
-    else run_sized<uint16_t, 1>(a, keys, cols, s);
+    if (dtype == kF32) run_sized<float>(a, keys, cols, s);
+    else run_sized<uint16_t>(a, keys, cols, s);
 }
 
 }  // namespace

@@ -46,9 +46,9 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
 }  // namespace
 
 hipError_t launch_attn_fwd(const AttnArgs &a, int dtype, int cols, hipStream_t s) {
-    if (dtype == kF32) return run_fwd_sized<float, false, 1>(a, cols, s);
-    return a.terms > 1 ? run_fwd_sized<uint16_t, false, 3>(a, cols, s)
-                       : run_fwd_sized<uint16_t, false, 1>(a, cols, s);
+    if (dtype == kF32) return run_fwd_sized<float, false, 2>(a, cols, s);
+    return a.terms > 2 ? run_fwd_sized<uint16_t, false, 3>(a, cols, s)
+                       : run_fwd_sized<uint16_t, false, 2>(a, cols, s);
 }
 
 hipError_t launch_attn_combine(const AttnArgs &a, int dtype, hipStream_t s) {

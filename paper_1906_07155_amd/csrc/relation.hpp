@@ -53,7 +53,7 @@ struct AttnArgs {
     // forward
     void *out;
     float *out_f32, *lse;
-    int32_t terms;                      // parts of the weights that multiply bf16 data (add_weighted)
+    int32_t terms;                      // dense keys: parts of the weights that multiply bf16 data, 2 or 3
     float *part;                        // nsplit > 1: partial sums [nsplit][B][H][Nq][D],
     SumRef *part_ml;                   // and what they refer to [nsplit][B][H][Nq]
     int32_t nsplit;

@@ -33,7 +33,6 @@ constexpr int64_t kGroups = 256;
 // allow) and 4 us for their partial sums, 58 us with 1024 and twice the partial sums.
 constexpr int64_t kNormBlocks = 1024;
 constexpr int64_t kNormSums = 512;
-constexpr int64_t kFewResults = 1 << 15;
 constexpr int64_t kHistTables = 2048;                  // partial tables of the bias gradient
 
 // One side's rows, checked: element strides of batch, row and head, adjacent channels.
@@ -103,11 +102,6 @@ int most_heads(int heads, int most) {
 // Columns of a workgroup: 32, or 16 where there are no more, and for heads of more than 64
 // channels, whose sums would fill the registers.
 int columns(int64_t rows, int dim) { return rows <= 16 || dim > 64 ? 16 : 32; }
-
-// Parts of the softmax weights that multiply bf16 data.  One rounding of them adds as much
-// error as rounding the result does; a few thousand results wait for memory and launches
-// anyway, so there the second part is free and only the result's own rounding is left.
-int weight_terms(int64_t results) { return results <= kFewResults ? 2 : 1; }
 
 // Heads of a workgroup, whose remaining waves share the streamed tiles, and (`split`) the
 // workgroups that share a head's tiles: as many workgroups as there may be, of those choices the
@@ -399,8 +393,9 @@ re_status_t box_attn_fwd(const box_attn_t *d, void *out, float *lse, float *out_
     a.out = out;
     a.lse = lse;
     a.out_f32 = out_f32;
-    // out_f32 is what the backward subtracts from the logits' gradient: as exact as that is
-    a.terms = out_f32 ? 3 : weight_terms(static_cast<int64_t>(a.B) * a.Nq * a.H * a.D);
+    // out_f32 is what the backward subtracts from the logits' gradient: with few keys that may leave
+    // nothing (with one key it does), so all bits of the weights count
+    a.terms = out_f32 && a.Nk <= RE_ATTN_FEW_KEYS ? 3 : 2;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if ((st = from_hip(launch_attn_fwd(a, d->dtype, cols, s))) != RE_OK || a.nsplit == 1) return st;
     return from_hip(launch_attn_combine(a, d->dtype, s));
@@ -433,8 +428,6 @@ re_status_t box_attn_bwd(const box_attn_t *d, const void *grad_out, const void *
     a.gbias = grad_bias;
     plan_bwd(a, d->dtype, &dq, &dkv, &c0, &c1);
     if ((st = check_workspace(workspace, workspace_bytes, bwd_bytes(dkv))) != RE_OK) return st;
-    dq.terms = weight_terms(static_cast<int64_t>(a.B) * a.Nq * a.H * a.D);
-    dkv.terms = weight_terms(static_cast<int64_t>(a.B) * a.Nk * a.Hkv * a.D);
     char *ws = static_cast<char *>(workspace);
     dq.rowstat = dkv.rowstat = reinterpret_cast<float *>(ws);
     dq.rowfar = dkv.rowfar = reinterpret_cast<float *>(ws += stat_bytes(dkv));
@@ -533,7 +526,6 @@ re_status_t box_memory_attn_fwd(const box_memory_t *m, const box_recall_t *r, vo
     place_fwd(a, workspace);
     a.out = out;
     a.lse = lse;
-    a.terms = weight_terms(static_cast<int64_t>(a.B) * a.Nq * a.H * a.D);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if ((st = from_hip(launch_attn_recall(a, r->dtype, cols, s))) != RE_OK || a.nsplit == 1) return st;
     return from_hip(launch_attn_combine(a, r->dtype, s));

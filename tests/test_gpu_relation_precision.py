@@ -7,6 +7,7 @@ import paper_1906_07155_amd as rex
 import relation_oracle as O
 from gpu_helpers import log
 from test_gpu_relation_attn import Case, f64
+from test_gpu_relation_memory import Recall
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +57,36 @@ def test_saved_results_are_there_for_any_number_of_keys():
         q = c.q.clone().requires_grad_()
         rex.box_attention(q, c.k, c.v, **c.args())[0].backward(c.g)
         assert torch.equal(q.grad, c.both()["grad_q"])
+
+
+def rounded_only(name, have, ref, share):
+    """`have` is bf16 and as far from the 64-bit `ref` as rounding alone takes it.
+
+    What is rounded is off by 2^-17 of the weights and binary32 sums, `share` of them in all: norm-wise
+    2^-16 of the sums of absolute values is a bound with room.  The roundings themselves are as large as
+    those of the reference, up to which of two neighbours a value near the middle goes to (a
+    twentieth of them is more than that can make of thousands of values)."""
+    have, ref, share = f64(have), np.asarray(ref), np.asarray(share)
+    own = np.linalg.norm(f64(torch.from_numpy(ref).to(torch.bfloat16)) - ref)
+    err = np.linalg.norm(have - ref)
+    assert err <= 1.05 * own + 2.0 ** -16 * np.linalg.norm(share), (name, err / np.linalg.norm(ref), own / np.linalg.norm(ref))
+
+
+@pytest.mark.parametrize("shape", [(1, 100, 100, 8, 8, 32, 15), (2, 100, 100, 8, 8, 32, 15), (1, 300, 300, 8, 2, 64, 15),
+                                   (1, 200, 333, 4, 4, 128, 7), (4, 150, 150, 8, 8, 48, 0)], ids=str)
+def test_bf16_results_are_rounded_once(shape):
+    """In small calls and in large ones."""
+    log("precision bf16 %s" % (shape,))
+    c = Case("bf16", *shape, seed=31)
+    for got in (c.both(), {"out": c.fwd()[0]}):
+        for key in ("out", "grad_q", "grad_k", "grad_v"):
+            if key in got:
+                rounded_only(key, got[key], c.ref[key], c.ref[key + "_big"])
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 500, 8, 8, 32, 15), (2, 200, 400, 8, 4, 64, 15), (1, 150, 200, 2, 2, 128, 0)], ids=str)
+def test_bf16_results_of_the_memory_are_rounded_once(shape):
+    log("precision memory %s" % (shape,))
+    r = Recall("bf16", *shape, seed=32)
+    ref = O.attn(f64(r.q), r.k, r.v, r.D ** -0.5, r.idx, r.bias, None, r.lengths)
+    rounded_only("out", r.run()[0], ref["out"], ref["out_abs"])
