@@ -104,9 +104,8 @@ class BoxMemory:
         self.used = [0] * streams                       # boxes a stream remembers
         self._device_table = None
 
-    def take(self, counts: Sequence[int]):
-        """Places for counts[s] new boxes of each stream: int64 slots of all of them, stream
-        after stream.  Raises (and takes nothing) where the pool has too few pages."""
+    def check(self, counts: Sequence[int]) -> None:
+        """Raises where take(counts) would."""
         page = relation.MEMORY_PAGE
         most = page * (self.max_pages - 1)              # none of them meets a page of the same call
         if len(counts) != len(self.table) or any(c < 0 or c > most for c in counts):
@@ -118,19 +117,30 @@ class BoxMemory:
             need += min(total, self.max_pages) - len(pages) if total > len(pages) else 0
         if need > len(self.free):
             raise RuntimeError("the memory has %d free pages, %d are needed" % (len(self.free), need))
+
+    def take(self, counts: Sequence[int]):
+        """Places for counts[s] new boxes of each stream: int64 slots of all of them, stream
+        after stream.  Raises (and takes nothing) where the pool has too few pages."""
+        self.check(counts)
+        page = relation.MEMORY_PAGE
+        free, table, used = list(self.free), [list(p) for p in self.table], list(self.used)
         slots: List[int] = []
         for s, c in enumerate(counts):
-            pages = self.table[s]
-            for _ in range(c):
-                if self.used[s] == page * len(pages):
+            pages = table[s]
+            while c > 0:
+                if used[s] == page * len(pages):
                     if len(pages) == self.max_pages:
-                        self.free.append(pages.pop(0))
-                        self.used[s] -= page
-                    pages.append(self.free.pop())
-                slots.append(pages[-1] * page + self.used[s] % page)
-                self.used[s] += 1
-        self._device_table = None
-        return torch.tensor(slots, dtype=torch.int64, device=self.device)
+                        free.append(pages.pop(0))
+                        used[s] -= page
+                    pages.append(free.pop())
+                at = used[s] % page
+                n = min(c, page - at)
+                slots.extend(range(pages[-1] * page + at, pages[-1] * page + at + n))
+                used[s] += n
+                c -= n
+        made = torch.tensor(slots, dtype=torch.int64, device=self.device)
+        self.free, self.table, self.used, self._device_table = free, table, used, None
+        return made
 
     def forget(self, stream: int) -> None:
         """The stream's pages go back to the pool."""
@@ -233,11 +243,16 @@ class RelationHead(nn.Module):
             gate = torch.where(valid, x, torch.zeros_like(x)).sum(1) / lengths.clamp(min=1)[:, None].to(x.dtype)
 
         recalled = None
+        fresh = []                              # what each layer is to remember
         if memory is not None:
+            memory.check(host)
+            first = self.layers[0]
+            if len(memory.layers) != len(self.layers) or any(
+                    m[0].shape[1] != first.kv_heads or m[0].shape[3] != first.dim for m in memory.layers):
+                raise ValueError("the memory is not one of this head's: %d layers of %d heads of %d channels"
+                                 % (len(self.layers), first.kv_heads, first.dim))
             pages, remembered = memory.pages_and_lengths()
-            slots = memory.take(host)
             rows = torch.cat([torch.arange(k, device=x.device) + i * n for i, k in enumerate(host)])
-            kept = boxes.reshape(B * n, 4)[rows]
         _, u = gated_norm(x.reshape(B * n, c), pre_weight=self.layers[0].pre[0], norm=self.layers[0].norm)
         u = u.view(B, n, c)
         for i, layer in enumerate(self.layers):
@@ -245,8 +260,7 @@ class RelationHead(nn.Module):
                 def recalled(q, k, v, out, lse, bias, held=memory.layers[i]):
                     far, far_lse = relation.box_memory_attn_fwd(q, held, pages, remembered, bias=bias,
                                                                 q_boxes=boxes, q_len=lengths, save=True)
-                    relation.box_memory_append(held, slots, k.reshape(B * n, *k.shape[2:])[rows],
-                                               v.reshape(B * n, *v.shape[2:])[rows], kept)
+                    fresh.append((held, *(t.reshape(B * n, *t.shape[2:])[rows] for t in (k, v))))
                     # one softmax over both: far's share is exp(far_lse) of the sum of both
                     share = torch.where(far_lse == -torch.inf, torch.zeros_like(lse),
                                         torch.sigmoid(far_lse - lse)).transpose(1, 2)[..., None]
@@ -254,4 +268,9 @@ class RelationHead(nn.Module):
             last = i + 1 == len(self.layers)
             x, u = layer(x, u, gate, boxes, lengths, recalled, last,
                          None if last else self.layers[i + 1].pre[0])
+        if memory is not None:                  # nothing is taken or written before all of it is there
+            kept = boxes.reshape(B * n, 4)[rows].contiguous()
+            slots = memory.take(host)
+            for held, k, v in fresh:
+                relation.box_memory_append(held, slots, k, v, kept)
         return x
