@@ -224,8 +224,9 @@ class RelationHead(nn.Module):
 
     def forward(self, x, boxes, counts: Optional[Sequence[int]] = None, memory: Optional[BoxMemory] = None):
         """x [images, boxes, channels] float32 or bfloat16, boxes float32 [images, boxes, 4] (x1, y1,
-        x2, y2), counts: valid boxes of each image (host; None: all).  Rows past an image's count
-        come back as they are to x's residual sums and affect nothing else.  With a memory, image s
+        x2, y2), counts: valid boxes of each image (host; None: all).  Rows past an image's count are
+        0 in the result, and what they hold, NaN and infinities included, has no effect on it or
+        on any gradient.  With a memory, image s
         is the next frame of stream s: its boxes attend to each other and to what the stream
         remembers, and are remembered (inference only: the memory has no gradient)."""
         B, n, c = x.shape
@@ -237,10 +238,12 @@ class RelationHead(nn.Module):
         if len(host) != B or any(k < 0 or k > n for k in host):
             raise ValueError("counts must hold a number in [0, %d] for each of the %d images" % (n, B))
         lengths = None if counts is None else torch.tensor(host, dtype=torch.int32, device=x.device)
-        gate = x.mean(1) if n else x.new_zeros(B, c)
-        if lengths is not None:
+        if lengths is not None:                 # (chosen, not multiplied: 0 * NaN is NaN)
             valid = (torch.arange(n, device=x.device) < lengths[:, None])[..., None]
-            gate = torch.where(valid, x, torch.zeros_like(x)).sum(1) / lengths.clamp(min=1)[:, None].to(x.dtype)
+            x = torch.where(valid, x, torch.zeros_like(x))
+            gate = x.sum(1) / lengths.clamp(min=1)[:, None].to(x.dtype)
+        else:
+            gate = x.mean(1) if n else x.new_zeros(B, c)
 
         recalled = None
         fresh = []                              # what each layer is to remember
@@ -273,4 +276,4 @@ class RelationHead(nn.Module):
             slots = memory.take(host)
             for held, k, v in fresh:
                 relation.box_memory_append(held, slots, k, v, kept)
-        return x
+        return x if lengths is None else torch.where(valid, x, torch.zeros_like(x))
