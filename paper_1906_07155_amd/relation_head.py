@@ -241,7 +241,8 @@ class RelationHead(nn.Module):
         if lengths is not None:                 # (chosen, not multiplied: 0 * NaN is NaN)
             valid = (torch.arange(n, device=x.device) < lengths[:, None])[..., None]
             x = torch.where(valid, x, torch.zeros_like(x))
-            gate = x.sum(1) / lengths.clamp(min=1)[:, None].to(x.dtype)
+            # (in binary32: bf16 has no 257, and the sum would be rounded before it is divided)
+            gate = (x.sum(1, dtype=torch.float32) / lengths.clamp(min=1)[:, None]).to(x.dtype)
         else:
             gate = x.mean(1) if n else x.new_zeros(B, c)
 

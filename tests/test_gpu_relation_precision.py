@@ -90,3 +90,22 @@ def test_bf16_results_of_the_memory_are_rounded_once(shape):
     r = Recall("bf16", *shape, seed=32)
     ref = O.attn(f64(r.q), r.k, r.v, r.D ** -0.5, r.idx, r.bias, None, r.lengths)
     rounded_only("out", r.run()[0], ref["out"], ref["out_abs"])
+
+
+@pytest.mark.parametrize("n", [257, 771, 999])
+def test_the_gate_sees_the_mean_of_an_image(n):
+    """The mean over the counted boxes, rounded once to the features' type: at most 2^-8 of it (half a
+    spacing at the bottom of an octave), and binary32 sums of n terms."""
+    log("precision gate %d" % n)
+    torch.manual_seed(n)
+    head = rex.RelationHead(64, 4, layers=1).cuda().bfloat16()
+    x = (torch.randn(2, 1000, 64, device="cuda") + 1.0).bfloat16()
+    boxes = torch.rand(2, 1000, 4, device="cuda") * 100.0
+    seen = []
+    head.layers[0].gate.register_forward_hook(lambda module, args, out: seen.append(args[0].detach()))
+    with torch.no_grad():
+        head(x, boxes, [n, 1000])
+    for i, m in enumerate((n, 1000)):
+        want = f64(x[i, :m]).mean(0)
+        bound = 2.0 ** -8 * np.abs(want) + (m + 8) * 2.0 ** -24 * np.abs(f64(x[i, :m])).mean(0)
+        assert np.all(np.abs(f64(seen[0][i]) - want) <= bound), (m, (np.abs(f64(seen[0][i]) - want) / bound).max())
