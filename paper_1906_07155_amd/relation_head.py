@@ -187,10 +187,8 @@ class RelationLayer(nn.Module):
         B, n, c = x.shape
         split = [self.heads, self.kv_heads, self.kv_heads]
         q, k, v = self.qkv(u).view(B, n, sum(split), self.dim).split(split, 2)
-        out, lse = box_attention(q, k, v, bias=self.bias, q_boxes=boxes, k_boxes=boxes, q_len=lengths,
-                                 k_len=lengths)
-        if recall is not None:
-            out = recall(q, k, v, out, lse, self.bias)
+        geo = dict(bias=self.bias, q_boxes=boxes, k_boxes=boxes, q_len=lengths, k_len=lengths)
+        out = box_attention(q, k, v, **geo)[0] if recall is None else recall(q, k, v, geo)
         branch = self.proj(out.reshape(B * n, c))
         gate = torch.sigmoid(self.gate(gate)).float()
         x, u = gated_norm(x.reshape(B * n, c), branch, gate=gate, post_weight=self.post[0],
@@ -261,14 +259,16 @@ class RelationHead(nn.Module):
         u = u.view(B, n, c)
         for i, layer in enumerate(self.layers):
             if memory is not None:
-                def recalled(q, k, v, out, lse, bias, held=memory.layers[i]):
-                    far, far_lse = relation.box_memory_attn_fwd(q, held, pages, remembered, bias=bias,
-                                                                q_boxes=boxes, q_len=lengths, save=True)
+                def recalled(q, k, v, geo, held=memory.layers[i]):
+                    # both parts in binary32 (the memory's by binary32 queries), rounded when joined
+                    out, lse, full = relation.box_attn_fwd(q, k, v, save=True, **geo)
+                    far, far_lse = relation.box_memory_attn_fwd(q.float(), held, pages, remembered, q_boxes=boxes,
+                                                                bias=geo["bias"], q_len=lengths, save=True)
                     fresh.append((held, *(t.reshape(B * n, *t.shape[2:])[rows] for t in (k, v))))
                     # one softmax over both: far's share is exp(far_lse) of the sum of both
                     share = torch.where(far_lse == -torch.inf, torch.zeros_like(lse),
                                         torch.sigmoid(far_lse - lse)).transpose(1, 2)[..., None]
-                    return torch.lerp(out.float(), far.float(), share).to(out.dtype)
+                    return torch.lerp(out if full is None else full, far, share).to(out.dtype)
             last = i + 1 == len(self.layers)
             x, u = layer(x, u, gate, boxes, lengths, recalled, last,
                          None if last else self.layers[i + 1].pre[0])

@@ -6,7 +6,7 @@ import pytest
 import paper_1906_07155_amd as rex
 import relation_oracle as O
 from gpu_helpers import log
-from test_gpu_relation_attn import Case, f64
+from test_gpu_relation_attn import Case, draw_boxes, f64
 from test_gpu_relation_memory import Recall
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +109,36 @@ def test_the_gate_sees_the_mean_of_an_image(n):
         want = f64(x[i, :m]).mean(0)
         bound = 2.0 ** -8 * np.abs(want) + (m + 8) * 2.0 ** -24 * np.abs(f64(x[i, :m])).mean(0)
         assert np.all(np.abs(f64(seen[0][i]) - want) <= bound), (m, (np.abs(f64(seen[0][i]) - want) / bound).max())
+
+
+def test_a_frame_and_its_memory_are_joined_before_they_are_rounded():
+    """The layer's attention over a frame's own boxes and the remembered ones is one softmax."""
+    log("precision join")
+    torch.manual_seed(3)
+    rng = np.random.default_rng(3)
+    head = rex.RelationHead(256, 8, layers=1).cuda().bfloat16()
+    with torch.no_grad():
+        head.layers[0].bias.normal_()
+    memory = head.memory(num_pages=64, streams=2, max_pages=30)
+    seen = []
+    head.layers[0].qkv.register_forward_hook(lambda module, args, out: seen.append(out.detach()))
+    head.layers[0].proj.register_forward_hook(lambda module, args, out: seen.append(args[0].detach()))
+    counts = [200, 150]
+    for frame in range(3):
+        boxes = draw_boxes(rng, (2, 200))
+        x = torch.from_numpy(rng.standard_normal((2, 200, 256))).bfloat16().cuda()
+        pages, lengths = (t.cpu().numpy() for t in memory.pages_and_lengths())
+        held = [rex.box_memory_read(memory.layers[0], torch.from_numpy(p[np.arange(t) // 32].astype(np.int64) * 32 + np.arange(t) % 32).cuda())
+                for p, t in zip(pages, lengths)]
+        seen.clear()
+        with torch.no_grad():
+            head(x, torch.from_numpy(boxes).cuda(), counts, memory)
+        qkv, joined = seen[0].view(2, 200, 24, 32), seen[1].view(2, 200, 8, 32)
+        for s, n in enumerate(counts):
+            q, k, v = (f64(t)[None] for t in qkv[s, :n].split(8, 1))
+            hk, hv, hb = held[s]
+            kb = np.concatenate([boxes[s, :n], hb.cpu().numpy()])
+            idx = O.buckets(boxes[s, :n], kb, 15, -4, 1)[None]
+            ref = O.attn(q, np.concatenate([k, f64(hk)[None]], 1), np.concatenate([v, f64(hv)[None]], 1), 32 ** -0.5, idx,
+                         f64(head.layers[0].bias).reshape(8, -1))
+            rounded_only("frame %d" % frame, joined[s, :n][None], ref["out"], ref["out_abs"])
