@@ -177,9 +177,15 @@ class RelationLayer(nn.Module):
         self.pre = nn.ParameterList([nn.Parameter(torch.ones(channels)) for _ in range(2)])
 
     def _apply(self, fn, recurse=True):
+        own = lambda: (self.bias, *self.post, *self.pre)
+        kept = [(p.data, None if p.grad is None else p.grad.data) for p in own()]
         super()._apply(fn, recurse)
-        for p in (self.bias, *self.post, *self.pre):
-            p.data = p.data.float()
+        for p, (data, grad) in zip(own(), kept):        # as they were, not widened from another type
+            if p.dtype != torch.float32:
+                device = p.device
+                p.grad = None                           # (a gradient has its parameter's type)
+                p.data = data.to(device)
+                p.grad = None if grad is None else grad.to(device)
         return self
 
     def forward(self, x, u, gate, boxes, lengths, recall, last: bool, pre_next):
