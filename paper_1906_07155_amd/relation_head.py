@@ -22,19 +22,21 @@ from . import relation
 
 class BoxAttnFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, bias, geo):
-        out, lse, out_f32 = relation.box_attn_fwd(q, k, v, bias=bias, save=True, **geo)
-        ctx.save_for_backward(q, k, v, bias, out, lse, out_f32)
-        ctx.geo = geo
+    def forward(ctx, q, k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask, cfg):
+        geo = dict(bias=bias, q_boxes=q_boxes, k_boxes=k_boxes, q_len=q_len, k_len=k_len, k_mask=k_mask, **cfg)
+        out, lse, out_f32 = relation.box_attn_fwd(q, k, v, save=True, **geo)
+        ctx.save_for_backward(q, k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask, out, lse, out_f32)
+        ctx.cfg = cfg
         ctx.mark_non_differentiable(lse)
         return out, lse
 
     @staticmethod
     def backward(ctx, grad_out, _):
-        q, k, v, bias, out, lse, out_f32 = ctx.saved_tensors
-        gq, gk, gv, gb = relation.box_attn_bwd(grad_out.contiguous(), q, k, v, out, lse, out_f32,
-                                               bias=bias, **ctx.geo)
-        return gq, gk, gv, gb, None
+        q, k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask, out, lse, out_f32 = ctx.saved_tensors
+        grads = relation.box_attn_bwd(grad_out.contiguous(), q, k, v, out, lse, out_f32, bias=bias,
+                                      q_boxes=q_boxes, k_boxes=k_boxes, q_len=q_len, k_len=k_len,
+                                      k_mask=k_mask, **ctx.cfg)
+        return (*grads, None, None, None, None, None, None)
 
 
 class GatedNormFunction(torch.autograd.Function):
@@ -61,14 +63,16 @@ class GatedNormFunction(torch.autograd.Function):
         return (*grads, None, None)
 
 
-def box_attention(q, k, v, *, bias=None, **geo):
+def box_attention(q, k, v, *, bias=None, q_boxes=None, k_boxes=None, q_len=None, k_len=None, k_mask=None,
+                  **cfg):
     """relation.box_attn_fwd with gradients for q, k, v and bias.  Returns (out, lse); lse has
-    no gradient.  `geo`: scale, q_boxes, k_boxes, first_exp, octave_steps, q_len, k_len, k_mask."""
+    no gradient.  `cfg`: scale, first_exp, octave_steps."""
     if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, bias))):
         relation._rows4(q, "q")
         lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-        return relation.box_attn_fwd(q, k, v, bias=bias, lse=lse, **geo)[:2]     # nothing else is kept
-    return BoxAttnFunction.apply(q, k, v, bias, geo)
+        return relation.box_attn_fwd(q, k, v, bias=bias, q_boxes=q_boxes, k_boxes=k_boxes, q_len=q_len,
+                                     k_len=k_len, k_mask=k_mask, lse=lse, **cfg)[:2]     # nothing else is kept
+    return BoxAttnFunction.apply(q, k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask, cfg)
 
 
 def gated_norm(x, branch=None, *, gate=None, post_weight=None, post_bias=None, pre_weight=None,

@@ -1,0 +1,33 @@
+"""What the autograd functions keep for the backward is what torch knows about."""
+import pytest
+
+import paper_1906_07155_amd as rex
+from gpu_helpers import log
+from test_gpu_relation_attn import Case
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    rex.lib()
+
+
+@pytest.mark.parametrize("name", ["q_boxes", "k_boxes", "q_len", "k_len", "k_mask"])
+def test_inputs_written_before_the_backward_are_noticed(name):
+    log("autograd %s" % name)
+    c = Case("f32", 2, 20, 30, 4, 2, 16, 7, q_len=[20, 9], k_len=[30, 11], masked=0.2)
+    q = c.q.clone().requires_grad_()
+    args = c.args()
+    out, _ = rex.box_attention(q, c.k, c.v, **args)
+    out.backward(c.g)
+    want = q.grad.clone()
+    assert torch.equal(want, c.both()["grad_q"])
+    out, _ = rex.box_attention(q, c.k, c.v, **args)
+    args[name].copy_(torch.zeros_like(args[name]))          # the next batch's, say
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.backward(c.g)
