@@ -20,6 +20,32 @@ from torch import nn
 from . import relation
 
 
+class _Final(torch.autograd.Function):
+    """Gradients that have no gradient themselves."""
+
+    @staticmethod
+    def forward(ctx, _, *grads):
+        return tuple(g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("box_attention and gated_norm are once_differentiable: their gradients have none")
+
+
+def once(backward):
+    """A backward whose results, under create_graph, fail where they are differentiated again instead
+    of counting as constants (torch's once_differentiable does so only where the upstream gradient
+    itself wants one)."""
+    def wrapped(ctx, *upstream):
+        with torch.no_grad():
+            found = backward(ctx, *upstream)
+        if not torch.is_grad_enabled():
+            return found
+        given = iter(_Final.apply(torch.empty(0, requires_grad=True), *(g for g in found if g is not None)))
+        return tuple(None if g is None else next(given) for g in found)
+    return wrapped
+
+
 class BoxAttnFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask, cfg):
@@ -31,6 +57,7 @@ class BoxAttnFunction(torch.autograd.Function):
         return out, lse
 
     @staticmethod
+    @once
     def backward(ctx, grad_out, _):
         q, k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask, out, lse, out_f32 = ctx.saved_tensors
         grads = relation.box_attn_bwd(grad_out.contiguous(), q, k, v, out, lse, out_f32, bias=bias,
@@ -51,6 +78,7 @@ class GatedNormFunction(torch.autograd.Function):
         return (u if branch is None else y), (None if branch is None else u)
 
     @staticmethod
+    @once
     def backward(ctx, grad_y, grad_u):
         x, branch, gate, w1, c1, w2, c2, stats = ctx.saved_tensors
         if branch is None:                  # the one output is u

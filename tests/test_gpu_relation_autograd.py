@@ -31,3 +31,20 @@ def test_inputs_written_before_the_backward_are_noticed(name):
     args[name].copy_(torch.zeros_like(args[name]))          # the next batch's, say
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         out.backward(c.g)
+
+
+def test_second_derivatives_are_refused():
+    """The kernels have none; a gradient asked for with create_graph is no constant."""
+    log("autograd twice")
+    c = Case("f32", 1, 5, 6, 2, 2, 8, 3)
+    q = c.q.clone().requires_grad_()
+    out, _ = rex.box_attention(q, c.k, c.v, **c.args())
+    first, = torch.autograd.grad((out * c.g).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        ((first * first).sum() + (q * q).sum()).backward()
+    x = torch.randn(6, 16, device="cuda", requires_grad=True)
+    for branch in (None, torch.randn(6, 16, device="cuda")):
+        y, u = rex.gated_norm(x, branch)
+        first, = torch.autograd.grad((u * u).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            ((first * first).sum() + (x * x).sum()).backward()
