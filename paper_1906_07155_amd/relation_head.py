@@ -260,7 +260,8 @@ class RelationHead(nn.Module):
 
     def forward(self, x, boxes, counts: Optional[Sequence[int]] = None, memory: Optional[BoxMemory] = None):
         """x [images, boxes, channels] float32 or bfloat16, boxes float32 [images, boxes, 4] (x1, y1,
-        x2, y2), counts: valid boxes of each image (host; None: all).  Rows past an image's count are
+        x2, y2), counts: valid boxes of each image (a list, or a tensor, which is copied to
+        the host where it is not there; None: all).  Rows past an image's count are
         0 in the result, and what they hold, NaN and infinities included, has no effect on it or
         on any gradient.  With a memory, image s
         is the next frame of stream s: its boxes attend to each other and to what the stream
@@ -270,6 +271,8 @@ class RelationHead(nn.Module):
             raise RuntimeError("a memory is for inference: call under torch.no_grad()")
         if memory is not None and len(memory.table) != B:
             raise ValueError("the memory has %d streams, x %d images" % (len(memory.table), B))
+        if torch.is_tensor(counts):             # one copy, where the elements would be read one by one
+            counts = counts.tolist()
         host = [n] * B if counts is None else [int(k) for k in counts]
         if len(host) != B or any(k < 0 or k > n for k in host):
             raise ValueError("counts must hold a number in [0, %d] for each of the %d images" % (n, B))
