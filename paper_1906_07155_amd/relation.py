@@ -496,8 +496,8 @@ def _norm_descriptor(x, branch, gate, alpha, post_weight, post_bias, pre_weight,
     if gate is not None:
         if branch is None:
             raise ValueError("a gate needs a branch")
-        gates = gate.shape[0] if gate.dim() == 2 else 0
-        if gates < 1 or m % gates:
+        gates = gate.shape[0] if gate.dim() == 2 else -1
+        if gates < 0 or (gates == 0 and m > 0) or (gates > 0 and m % gates):
             raise ValueError("gate must be [gates, channels] with gates dividing the %d rows" % m)
         _dense(gate, (gates, c), "gate", torch.float32)
     params = (post_weight, post_bias, pre_weight, pre_bias)

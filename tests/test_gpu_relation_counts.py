@@ -35,3 +35,30 @@ def test_counts_on_the_device_are_read_at_once(monkeypatch):
         assert torch.equal(head(x, boxes, counts), want)
         with pytest.raises(ValueError, match="counts"):
             head(x, boxes, counts + 1)
+
+
+@pytest.mark.parametrize("shape", [(0, 20), (2, 0), (0, 0)], ids=str)
+def test_no_images_and_no_boxes(shape):
+    """A batch that nothing is left of: empty results and gradients of 0."""
+    log("counts empty %s" % (shape,))
+    head = make(2, 2)
+    x = torch.randn(*shape, 64, device="cuda", requires_grad=True)
+    boxes = torch.rand(*shape, 4, device="cuda")
+    for counts in (None, [0] * shape[0]):
+        head.zero_grad()
+        y = head(x, boxes, counts)
+        assert y.shape == x.shape
+        y.sum().backward()
+        assert x.grad.shape == x.shape
+        assert all(float(p.grad.abs().sum()) == 0.0 for p in head.parameters() if p.grad is not None)
+
+
+def test_gates_of_no_rows():
+    log("counts gates")
+    x, gate = torch.zeros(0, 16, device="cuda"), torch.zeros(0, 16, device="cuda")
+    y, u, stats = rex.gated_norm_fwd(x, x, gate=gate, save=True)
+    assert y.shape == u.shape == (0, 16)
+    grads = rex.gated_norm_bwd(y, u, x, x, stats, gate=gate, pre_weight=torch.ones(16, device="cuda"))
+    assert grads[2].shape == (0, 16) and float(grads[5].abs().sum()) == 0.0
+    with pytest.raises(ValueError, match="gate"):
+        rex.gated_norm_fwd(torch.zeros(3, 16, device="cuda"), torch.zeros(3, 16, device="cuda"), gate=gate)
