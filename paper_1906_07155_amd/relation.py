@@ -80,9 +80,9 @@ def lib():
 
 class _Call:
     """One call's stream, and a `with` block's worth of its device where that is not the
-    current one.  Tensors that the call allocates itself are handed to a stream other than the
-    current one with record_stream, so that their memory is not given away while that stream
-    still uses it."""
+    current one.  Tensors that a call on a given stream allocates itself come from that stream's
+    memory (what the current stream has given back may still be in use by what is enqueued there),
+    and the current stream, on which their user is, is recorded with them."""
 
     __slots__ = ("device", "other", "stream", "guard")
 
@@ -107,9 +107,12 @@ class _Call:
             self.guard.__exit__(*exc)
 
     def empty(self, shape, dtype):
-        t = _torch().empty(*shape, dtype=dtype, device=self.device)   # (0.4 us less than a tuple)
-        if self.other is not None:
-            t.record_stream(self.other)
+        torch = _torch()
+        if self.other is None:
+            return torch.empty(*shape, dtype=dtype, device=self.device)   # (0.4 us less than a tuple)
+        with torch.cuda.stream(self.other):
+            t = torch.empty(*shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))
         return t
 
     def workspace(self, given, need):
