@@ -13,7 +13,7 @@
 // 2048 pages, 8000 boxes 69 / 53 and 62 / 33, 16000 boxes 134 / 102 and 95 / 53; 4000 boxes
 // 38 / 28 and 48 / 26.  bf16, 32768 pages, 16000 boxes in 8 heads of 64: 72 / 51 and 177 / 110; 512
 // pages, 16000 boxes in 8 heads of 32: 34 / 18 and 38 / 18.  So the second takes a call with four
-// boxes for each page of the memory and 2^23 values.  Its 16000 boxes are 333 MB both ways, 68 us
+// boxes for each page of the memory and 2^23 values, where there are pages enough for its workgroups.  Its 16000 boxes are 333 MB both ways, 68 us
 // at the rate of a large copy.  What bounds the second is latency: a wave's (page, head) has few
 // boxes, and each goes from its slot over its row to LDS and to the page (16 waves of a workgroup:
 // append 105 us as a kernel alone, 8 waves 119).
@@ -138,6 +138,9 @@ __global__ __launch_bounds__(256) void memory_read_kernel(MemoryArgs a) {
 // ---------------------------------------------------------------------------
 
 constexpr int kOwners = 512, kOwned = 256;      // workgroups, and the most pages of one
+// Fewer pages leave most workgroups without one: 16000 reads in binary32, 8 heads of 128 channels, of
+// 128 pages 48 us (each box by itself 53), of 64 pages 74 (47), of 16 208 (47), of one 3206 (46).
+constexpr int kFewPages = 128;
 constexpr int64_t kManyValues = 1 << 23;
 constexpr int kOwnWaves = 16, kOwnThreads = kOwnWaves * 64;
 constexpr int kRow = kTile + 4;                 // bytes of a row of a page's values in LDS
@@ -348,7 +351,7 @@ dim3 memory_grid(const MemoryArgs &a) {
 bool by_pages(MemoryArgs &a) {
     const int64_t owned = (a.num_slots / kTile + kOwners - 1) / kOwners;
     a.owned = static_cast<int32_t>(std::min<int64_t>(owned, kOwned));
-    return owned <= kOwned && a.count * kTile >= 4 * a.num_slots && a.count * a.Hkv * a.D >= kManyValues;
+    return a.num_slots >= kFewPages * kTile && owned <= kOwned && a.count * kTile >= 4 * a.num_slots && a.count * a.Hkv * a.D >= kManyValues;
 }
 
 }  // namespace
