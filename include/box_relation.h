@@ -41,7 +41,8 @@ extern "C" {
  * over the visible keys: j < k_len[b] and k_mask[b][j] != 0.  A row without a visible key
  * (or whose every bias is -inf, see below) has out = 0 and lse = -inf.  Rows i >= q_len[b] are padding:
  * out = 0, lse = -inf, nothing of them is used.  What masked keys and padding hold (NaN and
- * infinities included) has no effect on any result.
+ * infinities included) has no effect on any result.  An infinity among the values of visible keys
+ * makes its channel infinite or NaN.
  *
  * An entry of bias at or below -1e30 (a type's lowest value, say) counts as -inf: its pairs
  * are left out.  Any other is a number: a row whose visible keys are all at -1e9 has the weights
@@ -82,7 +83,7 @@ typedef struct {
 } box_attn_t;
 
 /* Device workspace of box_attn_fwd and of box_attn_bwd (the larger, where `backward`):
- * partial sums where few rows meet many keys, and in the backward 8 bytes per (row, head)
+ * partial sums where few rows meet many keys, and in the backward 17 bytes per (row, head)
  * and the bias gradient's partial tables.  May be 0 bytes.  Host-only. */
 re_status_t box_attn_workspace_size(const box_attn_t *a, int32_t backward, size_t *bytes);
 

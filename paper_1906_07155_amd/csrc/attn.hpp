@@ -16,7 +16,7 @@
 //     transposing read gives a lane one channel of four rows.  (Read from memory as pairs
 //     of channels a tile of 64 channels takes 16 loads of 4 bytes a lane instead of 4 of 16,
 //     and each costs the address unit the same 16 cycles.  16 images of up to 1000 boxes in 16
-//     heads of 64 channels: forward 197 us that way, 173 this way.)
+//     heads of 64 channels, weights in one part: forward 197 us that way, 173 this way.)
 //   - Binary32 data has no such read: lane n takes channels 2n and 2n + 1 of its eight
 //     rows from memory, the operands of two tiles with channel 2r + t in row r of tile t.
 #pragma once
@@ -49,7 +49,6 @@ template <> struct Num<uint16_t> {    // bf16
     static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t soff) {
         return __builtin_amdgcn_raw_buffer_load_b32(r, off, soff, 0);
     }
-    static __device__ __forceinline__ Pair no_pair() { return 0u; }
     static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
@@ -125,7 +124,6 @@ template <> struct Num<float> {
     static __device__ __forceinline__ Pair load_pair(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t soff) {
         return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, soff, 0));
     }
-    static __device__ __forceinline__ Pair no_pair() { return Pair{}; }
     static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);

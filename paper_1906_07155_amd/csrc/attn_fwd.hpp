@@ -13,11 +13,14 @@
 // share of the products: the workgroup computes each tile's buckets once, a step ahead,
 // into LDS (16 bits a pair: the byte offset into a head's table, which is in LDS too).
 //
-// Measured, bf16: 100 boxes in 8 heads of 32 channels 8.4 us (a launch and four dependent
-// steps); 1000 in 16 heads of 64 25 us; 16 images of those 173 us, 65 GFLOP of products that
-// take 58 us at the rate of a large product and some 15 vector instructions for every pair and
-// head (bias, exponent, running maximum) that take 100.  The memory, 300 boxes against 6000 in
-// 16 heads of 64: 53 us; 64 single queries against up to 8192 in 8 heads of 32: 78 us, 3.5 TB/s.
+// Measured, bf16: 100 boxes in 8 heads of 32 channels 9.7 us (a launch and four dependent
+// steps); 1000 in 16 heads of 64 29.5 us; 16 images of 600 to 1000 of those and one of none 210 us:
+// some 40 GFLOP of products, 60 with the second part of the weights, that take 53 us at the rate of a
+// large product; vector instructions (bias, exponent, running maximum, parts of the weights) take half
+// of the CUs' time.  1000 boxes in 8 heads of 128: 43 us.  64 single queries against 1000 keys each in
+// 8 heads of 32: 23.5 us, in binary32 33.
+// The memory, 300 boxes against 6000 in 16 heads of 64: 56 us, in binary32 111; 64 single queries
+// against up to 8192 in 8 heads of 32: 83 us, 3.3 TB/s, in binary32 126.
 #pragma once
 
 #include "attn.hpp"
@@ -58,8 +61,8 @@ inline __host__ __device__ FwdLds fwd_lds(int cols, int dp, int hp, int parts, i
 
 // Tiles of bf16 rows that a wave keeps in LDS, keys and values, or values alone for
 // heads of more than 64 channels.  (Two of each, the next on its way for a whole step, leave room
-// for one workgroup on a CU instead of two: 1000 queries and keys in 16 heads of 64 channels take
-// 27.2 us then, 26.2 as it is.)
+// for one workgroup on a CU instead of two: 1000 queries and keys in 16 heads of 64 channels, weights in
+// one part, take 27.2 us then, 26.2 as it is.)
 template <typename T, int DB, bool PAGED>
 constexpr int fwd_tiles() { return PAGED || sizeof(T) == 4 ? 0 : DB <= 2 ? 2 : 1; }
 

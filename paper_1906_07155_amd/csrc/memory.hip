@@ -9,14 +9,14 @@
 //   many boxes   a workgroup owns some pages, finds the call's boxes in them by reading all slots
 //                (8 bytes a box, from L2), and each of its waves takes a (page, head): the values
 //                pass through LDS, and 64 adjacent bytes of the page are one access.
-// Shuffled slots, binary32, 16 heads of 64 channels, append / read, us, the first and the second:
-// 2048 pages, 8000 boxes 69 / 53 and 62 / 33, 16000 boxes 134 / 102 and 95 / 53; 4000 boxes
-// 38 / 28 and 48 / 26.  bf16, 32768 pages, 16000 boxes in 8 heads of 64: 72 / 51 and 177 / 110; 512
-// pages, 16000 boxes in 8 heads of 32: 34 / 18 and 38 / 18.  So the second takes a call with four
-// boxes for each page of the memory and 2^23 values, where there are pages enough for its workgroups.  Its 16000 boxes are 333 MB both ways, 68 us
-// at the rate of a large copy.  What bounds the second is latency: a wave's (page, head) has few
-// boxes, and each goes from its slot over its row to LDS and to the page (16 waves of a workgroup:
-// append 105 us as a kernel alone, 8 waves 119).
+// Shuffled slots, 2048 pages, 16 heads of 64 channels, 16000 boxes, append / read, us: binary32 134 / 102
+// the first way and 89 / 53 the second (the same slots read back; others: 101 / 66), bf16 123 / 92 and
+// 93 / 42; 4000 boxes 38 / 28 and 48 / 26.  bf16, 32768 pages, 16000 boxes in 8 heads of 64: 74 / 50 and
+// 177 / 110; 512 pages, 16000 boxes in 8 heads of 32: 34 / 18 and 38 / 18.  So the second takes a call
+// with four boxes for each page of the memory and 2^23 values, where there are pages enough for its
+// workgroups.  Its 16000 boxes are 333 MB both ways, 68 us at the rate of a large copy.  What bounds it is
+// latency: a wave's (page, head) has few boxes, and each goes from its slot over its row to LDS and
+// to the page (with slots in order 61 / 38).
 #include <algorithm>
 
 #include "attn.hpp"

@@ -24,9 +24,10 @@ constexpr int64_t kMaxRows = int64_t(1) << 24;         // queries or keys of one
 constexpr int64_t kMaxRowHeads = (int64_t(1) << 31) - 1;
 // Workgroups among which the attention's work is shared out: one for each of the 256 CUs, two
 // where they have 16 columns, whose few registers leave their waves waiting for memory.  Dense,
-// 1000 queries and keys, 16 heads of 64 channels: 128 workgroups 35.8 us, 256 26.4, 512 37.1.
-// Memory, 300 queries against 6000 boxes in the same heads: 160 68.9, 240 54.3, 360 74.5, 480 65.0;
-// 64 single queries against up to 8192 boxes each in 8 heads of 32: 512 78, 1024 86.
+// 1000 queries and keys, 16 heads of 64 channels: 128 workgroups 40 us, 256 29.5, 512 42.
+// Memory, 300 queries against 6000 boxes in the same heads, the joining of their parts with it: 80 of
+// them 90 us, 240 60, 480 73; 64 single queries against up to 8192 boxes each in 8 heads of 32: 256 109,
+// 512 83, 1024 93.
 constexpr int64_t kGroups = 256;
 // Workgroups of the norms.  16000 rows of 1024 channels, bf16: forward 26.6 us with 1024
 // of them, 28.2 with 4096; backward 54 us with 512 (two on each CU, what its registers
@@ -165,7 +166,7 @@ void plan_bwd(const AttnArgs &a, int dtype, AttnArgs *dq, AttnArgs *dkv, int *dq
     const int tables = kAttnWaves * std::max(1, a.rule.nb * a.rule.nb) * 8;
     dkv->head_step = std::min({a.group, 4, std::max(1, (64 << 10) / tables)});
     // 16 for binary32 heads of more than 32 channels too, whose operands fill the registers
-    // (three images of 171 boxes, six heads of 48: forward and backward 64.6 us, 85.8 with 32)
+    // (three images of 171 boxes, six heads of 48: 43 us, 83 with 32)
     *dkv_cols = dtype == RE_DTYPE_F32 && a.D > 32 ? 16 : columns(a.Nk, a.D);
     for (int most = kAttnWaves;;) {
         dkv->tiles = (a.Nk + *dkv_cols - 1) / *dkv_cols;
