@@ -110,8 +110,12 @@ def gated_norm(x, branch=None, *, gate=None, post_weight=None, post_bias=None, p
     without a branch, u None without the second norm."""
     if branch is None and not second:
         raise ValueError("neither a branch nor the second norm: nothing to do")
-    first, u = GatedNormFunction.apply(x, branch, gate, post_weight, post_bias, pre_weight, pre_bias,
-                                       dict(alpha=alpha, norm=norm, eps=eps), second)
+    cfg = dict(alpha=alpha, norm=norm, eps=eps)
+    given = (x, branch, gate, post_weight, post_bias, pre_weight, pre_bias)
+    if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given)):
+        return relation.gated_norm_fwd(x, branch, gate=gate, post_weight=post_weight, post_bias=post_bias,
+                                       pre_weight=pre_weight, pre_bias=pre_bias, second=second, **cfg)[:2]
+    first, u = GatedNormFunction.apply(*given, cfg, second)
     return (x, first) if branch is None else (first, u)
 
 

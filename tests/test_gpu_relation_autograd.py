@@ -48,3 +48,25 @@ def test_second_derivatives_are_refused():
         first, = torch.autograd.grad((u * u).sum(), x, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             ((first * first).sum() + (x * x).sum()).backward()
+
+
+def test_nothing_is_kept_where_no_gradient_is_asked_for(monkeypatch):
+    log("autograd inference")
+    from paper_1906_07155_amd import relation
+    c = Case("bf16", 1, 20, 90, 2, 2, 16, 3)
+    x, w = torch.randn(30, 64, device="cuda"), torch.ones(64, device="cuda", requires_grad=True)
+    want = rex.box_attention(c.q, c.k, c.v, **c.args()), rex.gated_norm(x, x, pre_weight=w), rex.gated_norm(x, pre_weight=w)
+    kept = []
+    for name in ("box_attn_fwd", "gated_norm_fwd"):
+        def call(*args, name=name, real=getattr(relation, name), **kw):
+            found = real(*args, **kw)
+            kept.append(found[2])
+            return found
+        monkeypatch.setattr(relation, name, call)
+    with torch.no_grad():
+        got = rex.box_attention(c.q, c.k, c.v, **c.args()), rex.gated_norm(x, x, pre_weight=w), rex.gated_norm(x, pre_weight=w)
+    assert kept == [None] * 3
+    for a, b in zip(got, want):
+        assert all(torch.equal(s, t.detach()) and not s.requires_grad for s, t in zip(a, b))
+    y, _ = rex.gated_norm(x, second=True, pre_weight=w.detach())
+    assert y is x and rex.gated_norm(x, x, second=False)[1] is None
