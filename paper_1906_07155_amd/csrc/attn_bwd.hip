@@ -372,16 +372,22 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dq_kernel(AttnArgs a)
                         sc[s][0] = sc[s][1] = f32x4{};
                         if (BIAS) {
                             const u32x4 to = *reinterpret_cast<const u32x4 *>(bk + 16 * s * kBuckStride);
-                            if (wide) wide_gather(to, bias, sc[s]);
-                            else table_gather(to, tab, sc[s]);
+                            if (wide) {
+                                wide_gather(to, bias, sc[s]);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) sc[s][j >> 2][j & 3] = start(sc[s][j >> 2][j & 3], s);
+                            } else {
+                                table_gather(to, tab, sc[s]);
+                            }
                         }
+                    }
+                    // No condition among the products: the compiler (ROCm 7.2) leaves out the wait for a
+                    // product's result where its first use stands behind a block that may be skipped.
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             dp[s][t] = f32x4{};
-                            if (wide) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) sc[s][t][i] = start(sc[s][t][i], s);
-                            }
 #pragma unroll
                             for (int k = 0; k < DB; ++k) {
                                 sc[s][t] = N::mma(ka[t][k], q[s][k], sc[s][t]);
@@ -684,7 +690,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_dkv_kernel(AttnArgs a
                                     sc[s][t] = N::mma(qf[t][k], kf[s][k], sc[s][t]);
                                     dp = N::mma(gf[t][k], vf[s][k], dp);
                                 }
-                                if (__builtin_expect(other, 0)) sc[s][t] -= peak[t];
+                                // 0 in most rows, but no condition here: the compiler (ROCm 7.2) leaves out
+                                // the wait for sc where a block that may be skipped stands before its use
+                                sc[s][t] -= peak[t];
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     const f32x4 two = st[2 * t + (i >> 1)];
