@@ -24,12 +24,12 @@
 // are binary64: an addition of 64 lanes to LDS takes 18 to 30 cycles of a CU there, 193 in
 // binary32 (measured, whatever the addresses).
 //
-// Measured, 16 images of up to 1000 boxes in 16 heads of 64 channels, bf16: dq 256 us, dkv
-// 498, hist 5.  dkv has four products of the pair matrix, two of them in two parts, and its operands
-// leave two waves on a SIMD; without its histogram it takes 355 us.  So what bounds it is LDS (reads of
+// Measured, 16 images of up to 1000 boxes in 16 heads of 64 channels, bf16: dq 262 us, dkv
+// 512, hist 5.  dkv has four products of the pair matrix, two of them in two parts, and its operands
+// leave two waves on a SIMD; without its histogram it takes 70 % of that.  So what bounds it is LDS (reads of
 // rows, biases and buckets, and the histogram: 38 % of the CUs' time, and 12 % of conflicts) and vector
-// instructions (38 %) from few waves.  8 heads of 128: 400, 865 and 8 us.  Two images of 512 boxes
-// in 8 heads of 32, binary32: 23, 28 and 4 us; of 128: 116, 165 and 4.
+// instructions (40 %) from few waves.  8 heads of 128: 395, 857 and 8 us.  Two images of 512 boxes
+// in 8 heads of 32, binary32: 23, 28 and 4 us; of 128: 117, 168 and 4.
 #include "attn.hpp"
 
 namespace rex {
