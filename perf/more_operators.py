@@ -94,10 +94,12 @@ def draw(rng):
         outs = rng.choice([_log_int(rng, 1, 4096), 8 * _log_int(rng, 4, 512)])
         rows = _log_int(rng, 1, max(1, min(16000, int(most / (ins * outs)))))
         # (what a sum that is 0 but for its rounding has for a slope is no number to compare:
-        # with relu the backward pass takes its saved results as given)
-        act = rng.choice(["none", "gelu", "silu"] + ["relu", "relu"] * (direction != "train"))
+        # relu's backward pass takes the forward's results as given; what the others keep is the
+        # library's own, so they run forward and backward)
+        act = rng.choice({"fwd": ["none", "relu", "relu", "gelu", "silu"], "bwd": ["none", "relu"],
+                          "train": ["none", "gelu", "silu"]}[direction])
         return _linear(rows, ins, outs, dtype, direction, act, bias=rng.random() < 0.8,
-                       residual=rng.random() < 0.3)
+                       residual=direction != "bwd" and rng.random() < 0.3)
     if kind == "logprob":
         classes = _log_int(rng, 2, 100003)
         rows = _log_int(rng, 1, max(1, min(16000, 8192 * 1231 // classes)))
@@ -163,8 +165,7 @@ def prepare(case, seed):
         if case["pass"] != "fwd":
             st["gy"] = randn(m, n, dtype=dt)
         if case["pass"] == "bwd":           # what the forward pass has kept
-            pre = None if case["act"] == "none" else randn(m, n)
-            st["saved"] = pre.clamp(min=0.0).to(dt) if case["act"] == "relu" else pre
+            st["saved"] = None if case["act"] == "none" else randn(m, n, dtype=dt).clamp(min=0.0)
         return st
 
     if kind == "logprob":
@@ -418,8 +419,8 @@ def work(case):
         m, n, k = case["rows"], case["outs"], case["ins"]
         x, w, y = m * k * size, n * k * size, m * n * size
         b = 4 * n if case["bias"] else 0
-        # (a smooth activation's argument is kept in binary32, relu's result as it is)
-        kept = {"none": 0, "relu": y}.get(case["act"], 4 * m * n)
+        # (one value for each of the sums is kept for the slopes; for relu that is y itself)
+        kept = 0 if case["act"] == "none" else y
         fwd = x + w + y * (2 if case["residual"] else 1) + b
         bwd = 2 * x + 2 * w + y + b
         total = {"fwd": fwd, "bwd": bwd + kept, "train": fwd + 2 * (kept if case["act"] != "relu" else 0) + bwd}
