@@ -1,0 +1,273 @@
+// gemm.hpp -- tiled products of the dense layers, out[m][n] = sum_k Q(m, k) P(n, k).
+//
+// A workgroup owns BM x BN results; both operands' tiles of 128 bytes of k (64 bf16, 32 binary32)
+// go to LDS by loads that write there directly, the next step's into a second buffer while this
+// step's products run.  P's rows are the rows of the 16x16 products and Q's their columns, so a
+// lane's four results of one product are adjacent in the output's row.
+//
+// Operands lie in memory with k adjacent, or transposed with their rows adjacent (the gradients'
+// products).  16-byte chunks of a tile's rows are spread over the banks by an exclusive or of the
+// chunk's number with bits of the row's (chosen on the loading side: a lane's load goes to a fixed
+// place, and which chunk it fetches is free):
+//   k adjacent: [row][k], 8 chunks a row; a lane reads a chunk of its row.  Rows are ordered as in
+//     attn.hpp, so that two products' rows are eight adjacent results of a lane.
+//   transposed: [k][row]; bf16 goes through the transposing read, binary32 reads four k one by one
+//     (its products take 32 cycles each: reading is no bound).
+//
+// Nothing outside an operand is used: chunks past the last row, and past the last k of the last
+// step, are given an offset that the range check answers with 0.
+#pragma once
+
+#include "linear.hpp"
+
+namespace rex {
+
+#ifdef __HIP_DEVICE_COMPILE__
+#define REX_LDS_LOAD(r, to, off) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (REX_LDS void *)(to), 16, off, 0, 0, 0)
+#else
+#define REX_LDS_LOAD(r, to, off) (void)0
+#endif
+
+// One operand's tile of ROWS rows.
+template <typename T, bool TR, int ROWS, int WAVES, bool WHOLE>
+struct Side {
+    static constexpr int kSize = sizeof(T), kChunk = 16 / kSize, kStep = 8 * kChunk;   // elements
+    static constexpr int kBytes = ROWS * 128, kLoads = ROWS / (8 * WAVES);             // of a wave
+    static constexpr int kPitch = TR ? ROWS * kSize : 128, kPieces = kPitch / 16;      // of a line
+    using Frag = std::conditional_t<kSize == 2, bf16x8, f32x4>;
+    using Place = REX_LDS char *;
+
+    // what the loads need: the lane's offsets, and the k and first row of its chunks in a step
+    const char *origin;
+    int64_t step_bytes;
+    uint32_t off[kLoads];
+    int k[kLoads], e[WHOLE ? 1 : kLoads];
+    int left_k, left_rows;
+    u32x4 held[WHOLE ? 1 : kLoads];
+
+    static __device__ __forceinline__ int turn(int line) {
+        if (!TR) return (line & 3) | (line >> 1 & 4);
+        if (kSize == 4) return 4 * (line >> 2 & 3);
+        return 2 * (((line & 3) | (line >> 1 & 4)) >> (ROWS == 64 ? 1 : 0));
+    }
+
+    __device__ __forceinline__ Side(const void *p, int64_t ld, int row0, int rows, int k0, int K, int wave, int lane) {
+        origin = static_cast<const char *>(p) + (TR ? k0 * ld + static_cast<int64_t>(row0) * kSize
+                                                    : row0 * ld + static_cast<int64_t>(k0) * kSize);
+        step_bytes = TR ? kStep * ld : kStep * kSize;
+        left_k = K - k0;
+        left_rows = rows - row0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int j = (i * WAVES + wave) * 64 + lane, line = j / kPieces;
+            const int chunk = (j % kPieces) ^ turn(line);
+            off[i] = static_cast<uint32_t>(line * ld) + chunk * 16;
+            k[i] = TR ? line : chunk * kChunk;
+            const int row = TR ? chunk * kChunk : line;
+            if (row >= left_rows) off[i] = kBufOOB;
+            if (!WHOLE) e[i] = row;
+        }
+    }
+
+    // the next step's tile on its way to `to` (WHOLE), or to registers
+    __device__ __forceinline__ void load(char *to, int wave) {
+        const auto r = make_rsrc(origin, kBufMaxBytes - 1);
+        if constexpr (WHOLE) {
+            const bool all = left_k >= kStep;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                REX_LDS_LOAD(r, to + (i * WAVES + wave) * 1024, all || k[i] < left_k ? off[i] : kBufOOB);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                uint32_t x[kChunk];
+#pragma unroll
+                for (int c = 0; c < kChunk; ++c) {
+                    const bool in = (TR ? k[i] : k[i] + c) < left_k && (TR ? e[i] + c : e[i]) < left_rows;
+                    const uint32_t at = in ? off[i] + c * kSize : kBufOOB;
+                    if constexpr (kSize == 2) x[c] = __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+                    else x[c] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if constexpr (kSize == 2) held[i][c] = x[2 * c] | x[2 * c + 1] << 16;
+                    else held[i][c] = x[c];
+                }
+            }
+        }
+        origin += step_bytes;
+        left_k -= kStep;
+    }
+    __device__ __forceinline__ void put(char *to, int wave, int lane) const {
+        if constexpr (!WHOLE) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                *reinterpret_cast<u32x4 *>(to + ((i * WAVES + wave) * 64 + lane) * 16) = held[i];
+        }
+    }
+
+    // Operands of the half s of a step, product t of the wave whose first row is `base`.
+    struct Reader {
+        int at[TR ? 1 : 2], row, n, g;
+        __device__ __forceinline__ Reader(int base, int lane) {
+            n = lane & 15;
+            g = lane >> 4;
+            row = base / 16;
+            if constexpr (!TR) {
+                const int line = base + 8 * (n >> 2) + (n & 3);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) at[s] = line * 128 + ((4 * s + g) ^ (n & 7)) * 16;
+            } else if constexpr (kSize == 2) {
+                at[0] = (8 * g + (n >> 2)) * kPitch + (n >> 1 & 1) * 16 + (n & 1) * 8;
+            } else {
+                at[0] = 4 * g * kPitch + n * 4;
+            }
+        }
+        __device__ __forceinline__ Frag get(const char *tile, int t, int s) const {
+            Place p = (Place)(const_cast<char *>(tile));
+            if constexpr (!TR) {
+                return *(const REX_LDS Frag *)(p + at[s] + (t >> 1) * 4096 + (t & 1) * 512);
+            } else if constexpr (kSize == 2) {
+#ifdef __HIP_DEVICE_COMPILE__
+                using s16x4 = short __attribute__((ext_vector_type(4)));
+                using s16x8 = short __attribute__((ext_vector_type(8)));
+                const int chunk = 2 * (row + t) ^ turn(8 * g + (n >> 2));
+                s16x4 x[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (REX_LDS s16x4 *)(p + at[0] + chunk * 16 + (32 * s + 4 * e) * kPitch));
+                return __builtin_bit_cast(Frag, s16x8{x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]});
+#else
+                return Frag{};
+#endif
+            } else {
+                Frag f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    f[j] = *(const REX_LDS float *)(p + at[0] + ((row + t) ^ g) * 64 + (16 * s + j) * kPitch);
+                return f;
+            }
+        }
+        // the first of the four rows that a lane's results of product t are (P side), or the row
+        // of its column (Q side)
+        __device__ __forceinline__ int result_row(int t) const {
+            return 16 * row + (TR ? 16 * t + 4 * g : 32 * (t >> 1) + 8 * g + 4 * (t & 1));
+        }
+        __device__ __forceinline__ int result_column(int t) const {
+            return 16 * row + (TR ? 16 * t + n : 32 * (t >> 1) + 8 * (n >> 2) + 4 * (t & 1) + (n & 3));
+        }
+    };
+};
+
+__device__ __forceinline__ f32x4 gemm_mma(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 gemm_mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// WM x WN waves of MT x NT products each.
+template <typename T, bool TP, bool TQ, int MT, int NT, int WM, int WN, bool WHOLE, int OCC>
+__global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
+    constexpr int kWaves = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN;
+    using P = Side<T, TP, BN, kWaves, WHOLE>;
+    using Q = Side<T, TQ, BM, kWaves, WHOLE>;
+    using Frag = typename P::Frag;
+    __shared__ __attribute__((aligned(16))) char smem[2][P::kBytes + Q::kBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Workgroups go to the eight XCDs in turn: each takes a run of neighbouring tiles, in groups of
+    // eight rows of tiles, whose operands its L2 then holds.
+    const int tiles = a.tiles_m * a.tiles_n, all = tiles * a.split;
+    int id = (blockIdx.x & 7) * ((all + 7) >> 3) + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= ((all + 7) >> 3) || id >= all) return;
+    const int part = id / tiles;
+    id -= part * tiles;
+    const int band = id / (8 * a.tiles_n), rows = min(8, a.tiles_m - 8 * band);
+    id -= band * 8 * a.tiles_n;
+    const int m0 = (8 * band + id % rows) * BM, n0 = id / rows * BN;
+
+    const int k0 = part * a.steps * P::kStep;
+    const int steps = min(a.steps, (a.K - k0 + P::kStep - 1) / P::kStep);
+    P p(a.p, a.ldp, n0, a.N, k0, a.K, wave, lane);
+    Q q(a.q, a.ldq, m0, a.M, k0, a.K, wave, lane);
+    const int wn = wave % WN, wm = wave / WN;
+    const typename P::Reader pr(wn * 16 * NT, lane);
+    const typename Q::Reader qr(wm * 16 * MT, lane);
+
+    f32x4 acc[MT][NT] = {};
+    p.load(smem[0], wave);
+    q.load(smem[0] + P::kBytes, wave);
+    for (int step = 0; step < steps; ++step) {
+        char *now = smem[step & 1], *then = smem[step & 1 ^ 1];
+        p.put(now, wave, lane);
+        q.put(now + P::kBytes, wave, lane);
+        // what this wave loaded is there, and what it read of the other buffer is back
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        Frag pf[2][NT], qf[2][MT];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) pf[s][t] = pr.get(now, t, s);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) qf[s][t] = qr.get(now + P::kBytes, t, s);
+        }
+        if (step + 1 < steps) {
+            p.load(then, wave);
+            q.load(then + P::kBytes, wave);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = gemm_mma(pf[s][j], qf[s][i], acc[i][j]);
+    }
+    // (the compiler leaves out the wait states between products and a use behind a branch)
+    asm volatile("s_nop 15" ::: "memory");
+
+    // Results go through LDS, each wave's to a place of its own, so that a row's are written by
+    // neighbouring lanes and the epilogue is there once.  16-byte chunks are spread over the banks by
+    // their row.
+    constexpr int kRound = MT > 4 ? 4 : MT, kQuads = 4 * NT;        // products' rows at a time
+    static_assert(kRound * NT * 1024 * kWaves <= static_cast<int>(sizeof(smem)), "results of a round");
+    __builtin_amdgcn_s_barrier();
+    f32x4 *stage = reinterpret_cast<f32x4 *>(&smem[0][0]) + wave * kRound * NT * 64;
+    const int wave_m = m0 + wm * 16 * MT, wave_n = n0 + wn * 16 * NT;
+#pragma unroll
+    for (int r = 0; r < MT; r += kRound) {
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int row = qr.result_column(r + i) - wm * 16 * MT - 16 * r;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int quad = (pr.result_row(j) - wn * 16 * NT) >> 2;
+                stage[row * kQuads + (quad ^ (row & (kQuads - 1)))] = acc[r + i][j];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 2
+        for (int i = lane; i < kRound * NT * 64; i += 64) {
+            const int row = i / kQuads, quad = i % kQuads;
+            const f32x4 x = stage[row * kQuads + (quad ^ (row & (kQuads - 1)))];
+            const int m = wave_m + 16 * r + row, n = wave_n + 4 * quad;
+            if (m >= a.M || n >= a.N) continue;
+            if (a.split > 1) store_part(a, part, m, n, x);
+            else finish4<T>(a, m, n, x);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+template <typename T, bool TP, bool TQ, int MT, int NT, int WM, int WN, bool WHOLE, int OCC>
+hipError_t run_gemm(const GemmArgs &a, hipStream_t s) {
+    const int64_t all = static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.split;
+    gemm_kernel<T, TP, TQ, MT, NT, WM, WN, WHOLE, OCC><<<static_cast<uint32_t>((all + 7) / 8 * 8), 64 * WM * WN, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace rex

@@ -1,0 +1,270 @@
+// head_api.hip -- the C ABI declared in include/box_head.h.
+//
+// As in api.hip, every argument is checked on the host before anything is enqueued, and no
+// HIP call is made on an error path.  How a product is cut up is a function of sizes, type and
+// alignment alone, so the workspace functions and the calls agree on it.
+#include <algorithm>
+#include <cmath>
+
+#include "box_head.h"
+#include "linear.hpp"
+
+using namespace rex;
+
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+bool valid_dtype(int32_t d) { return d == RE_DTYPE_F32 || d == RE_DTYPE_BF16; }
+int64_t dtype_size(int32_t d) { return d == RE_DTYPE_BF16 ? 2 : 4; }
+bool aligned(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+re_status_t from_hip(hipError_t e) { return e == hipSuccess ? RE_OK : RE_ERR_DEVICE; }
+
+re_status_t check_workspace(const void *ws, size_t have, size_t need) {
+    if (need == 0) return RE_OK;
+    if (!ws || have < need || !aligned(ws, 256)) return RE_ERR_WORKSPACE;
+    return RE_OK;
+}
+
+// One operand of a product: rows x cols elements, cols adjacent.
+struct Matrix {
+    const void *p;
+    int64_t rows, cols, stride;
+};
+// 16-byte chunks of rows and nothing else: what the fast kernels read.
+bool whole(const Matrix &x, int64_t size) {
+    return aligned(x.p, 16) && x.cols * size % 16 == 0 && x.stride * size % 16 == 0;
+}
+
+struct Product {
+    GemmArgs a;
+    GemmPlan plan;
+    bool tp, tq, skinny;
+    size_t bytes;               // of partial sums
+};
+
+// out[M][N] = q p^T, with q [M][K], or transposed [K][M], and p [N][K] or [K][N].
+//
+// A tile's rate is that of 256 workgroups of its kind at work; the last round of them is as long as
+// a full one, and parts of k fill the GPU where tiles do not, for one more pass over the results.
+// (Rates measured at 16000 x 2048 x 1024 in bf16 and 1024 x 12544 x 1024 in binary32.)
+void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq, int32_t dtype) {
+    const int64_t size = dtype_size(dtype), step = 128 / size;
+    g = Product{};
+    GemmArgs &a = g.a;
+    a.p = p.p;
+    a.q = q.p;
+    a.ldp = p.stride * size;
+    a.ldq = q.stride * size;
+    a.N = static_cast<int32_t>(tp ? p.cols : p.rows);
+    a.M = static_cast<int32_t>(tq ? q.cols : q.rows);
+    a.K = static_cast<int32_t>(tp ? p.rows : p.cols);
+    a.ldo = a.N;
+    a.split = 1;
+    g.tp = tp;
+    g.tq = tq;
+    g.plan.whole = whole(p, size) && whole(q, size);
+    const int64_t M = a.M, N = a.N, K = a.K;
+    if (!tp && !tq && M <= kSkinnyRows && g.plan.whole && K % 8 == 0) {
+        g.skinny = true;
+        const int64_t groups = (N + 15) / 16, steps = (K + 31) / 32;
+        a.split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(128 / groups, steps / 64)));
+        a.steps = static_cast<int32_t>((steps + a.split - 1) / a.split);
+        a.split = static_cast<int32_t>((steps + a.steps - 1) / a.steps);
+    } else {
+        struct Tile { int kind, bm, bn; double us; };       // us: of one step of k
+        static const Tile kBf16[] = {{kTileLarge, 256, 256, 2.2}, {kTileMiddle, 128, 128, 0.7}, {kTileSmall, 64, 64, 0.3}};
+        static const Tile kF32[] = {{kTileMiddle, 128, 128, 2.0}, {kTileSmall, 64, 64, 0.55}};
+        const bool bf16 = dtype == RE_DTYPE_BF16;
+        const Tile *all = bf16 ? kBf16 : kF32;
+        const int count = bf16 ? 3 : 2;
+        const int64_t steps = std::max<int64_t>(1, (K + step - 1) / step);
+        double best = 0;
+        for (int i = g.plan.whole ? 0 : count - 1; i < count; ++i) {
+            const int64_t tm = (M + all[i].bm - 1) / all[i].bm, tn = (N + all[i].bn - 1) / all[i].bn;
+            for (int64_t split = 1; split <= 64 && (split == 1 || (steps / split >= 4 && tm * tn * split <= 1024)); ++split) {
+                const int64_t each = (steps + split - 1) / split;
+                if (split > 1 && (steps + each - 1) / each != split) continue;
+                const double rounds = double((tm * tn * split + 255) / 256);
+                const double us = rounds * (double(each) * all[i].us + 2.0) +
+                                  (split > 1 ? 4.0 + 8e-6 * double(split) * double(M) * double(N) / 4.0 : 0.0);
+                if (best == 0 || us < best) {
+                    best = us;
+                    g.plan.tile = all[i].kind;
+                    a.tiles_m = static_cast<int32_t>(tm);
+                    a.tiles_n = static_cast<int32_t>(tn);
+                    a.split = static_cast<int32_t>(split);
+                    a.steps = static_cast<int32_t>(each);
+                }
+            }
+        }
+    }
+    g.bytes = a.split > 1 ? align256(static_cast<size_t>(a.split) * M * N * 4) : 0;
+}
+
+re_status_t run_product(Product &g, void *out, void *ws, int32_t dtype, hipStream_t s) {
+    GemmArgs &a = g.a;
+    a.out = out;
+    a.part = static_cast<float *>(ws);
+    const int64_t size = dtype_size(dtype);
+    a.vec = a.N % 4 == 0 && a.ldo % 4 == 0 && aligned(out, 4 * size) &&
+            (!a.residual || (a.ldr % 4 == 0 && aligned(a.residual, 4 * size))) && aligned(a.slope, 4 * size);
+    hipError_t e;
+    if (g.skinny) e = launch_skinny(a, dtype, s);
+    else if (dtype == RE_DTYPE_BF16) e = launch_gemm_bf16(a, g.plan, g.tp, g.tq, s);
+    else e = launch_gemm_f32(a, g.plan, g.tp, g.tq, s);
+    if (e == hipSuccess && a.split > 1) e = launch_gemm_join(a, dtype, s);
+    return from_hip(e);
+}
+
+re_status_t check_linear(const linear_act_t *d) {
+    if (!d || !valid_dtype(d->dtype)) return RE_ERR_INVALID_ARG;
+    if (d->act < RE_ACT_NONE || d->act > RE_ACT_SILU) return RE_ERR_INVALID_ARG;
+    if (d->rows < 0 || d->ins < 1 || d->outs < 1) return RE_ERR_INVALID_ARG;
+    const uintptr_t size = static_cast<uintptr_t>(dtype_size(d->dtype));
+    if (d->bias && (!valid_dtype(d->bias_dtype) || (d->bias_dtype == RE_DTYPE_BF16 && d->dtype != RE_DTYPE_BF16) ||
+                    !aligned(d->bias, static_cast<uintptr_t>(dtype_size(d->bias_dtype)))))
+        return RE_ERR_INVALID_ARG;
+    if (!d->weight || (d->rows > 0 && !d->x)) return RE_ERR_INVALID_ARG;
+    for (const void *p : {d->x, d->weight, d->residual})
+        if (!aligned(p, size)) return RE_ERR_INVALID_ARG;
+    const int64_t most = int64_t(1) << 40;
+    const int64_t xs = d->rows > 1 ? d->x_stride : 0, ws = d->outs > 1 ? d->weight_stride : 0;
+    for (int64_t v : {xs, ws, d->residual && d->rows > 1 ? d->residual_stride : 0})
+        if (v < 0 || v > most) return RE_ERR_INVALID_ARG;
+    if (d->rows > INT32_MAX || d->ins > RE_LINEAR_MAX_SIZE || d->outs > RE_LINEAR_MAX_SIZE) return RE_ERR_UNSUPPORTED;
+    for (int64_t v : {xs, ws, d->ins, d->outs})
+        if (256 * v * static_cast<int64_t>(size) >= kBufMaxBytes) return RE_ERR_UNSUPPORTED;
+    return RE_OK;
+}
+
+// Rows of a matrix with one row, or none, have no stride.
+Matrix matrix(const void *p, int64_t rows, int64_t cols, int64_t stride) {
+    return Matrix{p, rows, cols, rows > 1 ? stride : cols};
+}
+
+// Runs of rows for the column sums: about 1024 workgroups, but 16 rows at least.
+void plan_slope(SlopeArgs &a, int64_t size) {
+    const int64_t wide = (a.N + 1024 / size - 1) / (1024 / size);      // strips of 64 chunks of 16 bytes
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>({1024 / wide, 512, (a.M + 15) / 16}));
+    a.run = static_cast<int32_t>((a.M + blocks - 1) / blocks);
+    a.blocks = a.run > 0 ? static_cast<int32_t>((a.M + a.run - 1) / a.run) : 0;
+}
+
+struct Backward {
+    SlopeArgs slope;
+    Product x, weight;
+    size_t g_bytes, part_bytes, bytes;
+};
+// g: the gradient of t, grad_y or in the workspace.
+void plan_backward(const linear_act_t *d, const void *grad_y, Backward &b) {
+    const int64_t size = dtype_size(d->dtype);
+    b = Backward{};
+    b.slope.M = d->rows;
+    b.slope.N = static_cast<int32_t>(d->outs);
+    plan_slope(b.slope, size);
+    const Matrix g = matrix(grad_y, d->rows, d->outs, d->outs);
+    const Matrix w = matrix(d->weight, d->outs, d->ins, d->weight_stride);
+    const Matrix x = matrix(d->x, d->rows, d->ins, d->x_stride);
+    if (d->rows > 0) {
+        plan_product(b.x, w, true, g, false, d->dtype);
+        plan_product(b.weight, x, true, g, true, d->dtype);
+    }
+    b.g_bytes = d->act == RE_ACT_NONE ? 0 : align256(static_cast<size_t>(d->rows) * d->outs * size);
+    b.part_bytes = d->bias ? align256(static_cast<size_t>(b.slope.blocks) * d->outs * 4) : 0;
+    b.bytes = b.g_bytes + b.part_bytes + std::max(b.x.bytes, b.weight.bytes);
+}
+
+}  // namespace
+
+extern "C" {
+
+re_status_t linear_act_workspace_size(const linear_act_t *d, int32_t backward, size_t *bytes) {
+    if (!bytes) return RE_ERR_INVALID_ARG;
+    const re_status_t st = check_linear(d);
+    if (st != RE_OK) return st;
+    if (backward) {
+        // without an activation grad_y itself is an operand, whose alignment is not known yet
+        Backward b, c;
+        plan_backward(d, nullptr, b);
+        plan_backward(d, reinterpret_cast<const void *>(uintptr_t(d->act == RE_ACT_NONE ? 4 : 0)), c);
+        *bytes = std::max(b.bytes, c.bytes);
+    } else {
+        *bytes = 0;
+        if (d->rows > 0) {
+            Product g;
+            plan_product(g, matrix(d->weight, d->outs, d->ins, d->weight_stride), false,
+                         matrix(d->x, d->rows, d->ins, d->x_stride), false, d->dtype);
+            *bytes = g.bytes;
+        }
+    }
+    return RE_OK;
+}
+
+re_status_t linear_act_fwd(const linear_act_t *d, void *y, void *slope, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    re_status_t st = check_linear(d);
+    if (st != RE_OK) return st;
+    if (slope && d->act == RE_ACT_NONE) return RE_ERR_INVALID_ARG;
+    const uintptr_t size = static_cast<uintptr_t>(dtype_size(d->dtype));
+    if (!aligned(y, size) || !aligned(slope, size)) return RE_ERR_INVALID_ARG;
+    if (d->rows == 0) return RE_OK;
+    if (!y) return RE_ERR_INVALID_ARG;
+    Product g;
+    plan_product(g, matrix(d->weight, d->outs, d->ins, d->weight_stride), false,
+                 matrix(d->x, d->rows, d->ins, d->x_stride), false, d->dtype);
+    if ((st = check_workspace(workspace, workspace_bytes, g.bytes)) != RE_OK) return st;
+    g.a.bias = d->bias;
+    g.a.bias_bf16 = d->bias_dtype == RE_DTYPE_BF16;
+    g.a.residual = d->residual;
+    g.a.ldr = d->rows > 1 ? d->residual_stride : 0;
+    g.a.slope = slope;
+    g.a.act = d->act;
+    return run_product(g, y, workspace, d->dtype, static_cast<hipStream_t>(stream));
+}
+
+re_status_t linear_act_bwd(const linear_act_t *d, const void *grad_y, const void *slope, const void *y,
+                           void *grad_x, void *grad_weight, void *grad_bias, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    re_status_t st = check_linear(d);
+    if (st != RE_OK) return st;
+    const int64_t size = dtype_size(d->dtype);
+    for (const void *p : {grad_y, slope, y, static_cast<const void *>(grad_x), static_cast<const void *>(grad_weight)})
+        if (!aligned(p, static_cast<uintptr_t>(size))) return RE_ERR_INVALID_ARG;
+    if (grad_bias && (!d->bias || !aligned(grad_bias, static_cast<uintptr_t>(dtype_size(d->bias_dtype)))))
+        return RE_ERR_INVALID_ARG;
+    if (d->act == RE_ACT_NONE ? (slope || y) : (slope && y)) return RE_ERR_INVALID_ARG;
+    if (y && d->act != RE_ACT_RELU) return RE_ERR_INVALID_ARG;
+    if (d->rows > 0 && (!grad_y || (d->act != RE_ACT_NONE && !slope && !y))) return RE_ERR_INVALID_ARG;
+    Backward b;
+    plan_backward(d, d->act == RE_ACT_NONE ? grad_y : nullptr, b);
+    if ((st = check_workspace(workspace, workspace_bytes, b.bytes)) != RE_OK) return st;
+    char *ws = static_cast<char *>(workspace);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+
+    const void *g = grad_y;
+    SlopeArgs &sl = b.slope;
+    const bool times = d->act != RE_ACT_NONE && (grad_x || grad_weight);
+    sl.gy = grad_y;
+    sl.saved = d->act == RE_ACT_NONE ? nullptr : slope ? slope : y;
+    sl.relu = y != nullptr;
+    if (d->act != RE_ACT_NONE) g = sl.g = ws;
+    sl.part = grad_bias ? reinterpret_cast<float *>(ws + b.g_bytes) : nullptr;
+    sl.gbias = grad_bias;
+    sl.bias_bf16 = d->bias_dtype == RE_DTYPE_BF16;
+    sl.vec = d->outs * size % 16 == 0 && aligned(grad_y, 16) && aligned(sl.saved, 16);
+    if ((times && d->rows > 0) || grad_bias)
+        if ((st = from_hip(launch_slope(sl, d->dtype, s))) != RE_OK) return st;
+    void *part = ws + b.g_bytes + b.part_bytes;
+    if (grad_x && d->rows > 0) {
+        b.x.a.q = g;
+        if ((st = run_product(b.x, grad_x, part, d->dtype, s)) != RE_OK) return st;
+    }
+    if (grad_weight) {
+        if (d->rows == 0) return from_hip(launch_clear(grad_weight, d->outs * d->ins * size, s));
+        b.weight.a.q = g;
+        if ((st = run_product(b.weight, grad_weight, part, d->dtype, s)) != RE_OK) return st;
+    }
+    return RE_OK;
+}
+
+}  // extern "C"

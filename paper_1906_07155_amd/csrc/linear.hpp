@@ -1,0 +1,197 @@
+// linear.hpp -- argument blocks and launchers of the dense layers' kernels, and what their
+// epilogues compute.
+#pragma once
+
+#include "attn.hpp"
+
+namespace rex {
+
+enum : int { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+
+// One product: out[m][n] = sum_k Q(m, k) P(n, k), both operands with k adjacent in memory
+// ([row][k]) or, transposed, with their rows adjacent ([k][row]).
+struct GemmArgs {
+    const void *p, *q;
+    int64_t ldp, ldq;               // bytes from row to row, or from k to k
+    void *out;                      // [M][N], ldo elements from row to row
+    int64_t ldo;
+    int32_t M, N, K;
+    int32_t tiles_m, tiles_n;
+    int32_t split, steps;           // parts of k, and the steps of each
+    float *part;                    // split > 1: [split][M][N]
+    // epilogue
+    const void *bias;               // [N] or null
+    const void *residual;           // [M][N], ldr elements from row to row, or null
+    int64_t ldr;
+    void *slope;                    // [M][N] dense or null
+    int32_t bias_bf16, act;
+    int32_t vec;                    // four adjacent results can be written (and residuals read) at once
+};
+
+// How a product is cut up.
+enum : int { kTileLarge = 0, kTileMiddle = 1, kTileSmall = 2 };
+struct GemmPlan {
+    int tile, bm, bn;               // a workgroup's rows and columns
+    int split, steps;
+    bool whole;                     // operands can be read 16 bytes at a time
+};
+
+hipError_t launch_gemm_bf16(const GemmArgs &a, const GemmPlan &p, bool tp, bool tq, hipStream_t s);
+hipError_t launch_gemm_f32(const GemmArgs &a, const GemmPlan &p, bool tp, bool tq, hipStream_t s);
+hipError_t launch_gemm_join(const GemmArgs &a, int dtype, hipStream_t s);
+// A few rows against [N][K]: the weights go from memory straight to the products.
+constexpr int kSkinnyRows = 64;
+hipError_t launch_skinny(const GemmArgs &a, int dtype, hipStream_t s);
+
+struct SlopeArgs {
+    const void *gy, *saved;         // [M][N] dense; saved null: slope 1
+    void *g;                        // gy * slope, or null
+    float *part;                    // [blocks][N]: column sums of runs of rows, or null
+    void *gbias;                    // [N]
+    int32_t bias_bf16;
+    int32_t relu;                   // `saved` is the layer's result, not the slope
+    int32_t N;
+    int64_t M;
+    int32_t blocks, run;            // runs of `run` rows
+    int32_t vec;
+};
+hipError_t launch_slope(const SlopeArgs &a, int dtype, hipStream_t s);
+hipError_t launch_clear(void *p, int64_t bytes, hipStream_t s);      // an even number of them
+
+// ---------------------------------------------------------------------------
+// Activations
+// ---------------------------------------------------------------------------
+
+// erfc(z) = t R(t) exp(-z^2) for z >= 0, t = 1 / (1 + 0.45 z), R the polynomial of degree nine with
+// the least largest relative error over all z (3.2e-8; 3.7e-7 as evaluated here), found by
+// reweighted least squares at Chebyshev points.  A relative error, so that the left tail of the
+// normal distribution is as exact as the rest.
+__device__ __forceinline__ float erfc_over_exp(float z) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.45f, z, 1.0f));
+    float r = -0.041390951722860336f;
+    r = fmaf(r, t, 0.19068720936775208f);
+    r = fmaf(r, t, -0.30058127641677856f);
+    r = fmaf(r, t, 0.14239980280399323f);
+    r = fmaf(r, t, -0.022357303649187088f);
+    r = fmaf(r, t, 0.11995022743940353f);
+    r = fmaf(r, t, 0.17525216937065125f);
+    r = fmaf(r, t, 0.22827163338661194f);
+    r = fmaf(r, t, 0.25388315320014954f);
+    return t * fmaf(r, t, 0.25388532876968384f);
+}
+
+// act(x) and its slope at x.
+template <bool SLOPE>
+__device__ __forceinline__ float activate(int act, float x, float &slope) {
+    switch (act) {
+    case kActRelu:                      // NaN stays, and lets the gradient through
+        slope = x <= 0.0f ? 0.0f : 1.0f;
+        return x <= 0.0f ? 0.0f : x;
+    case kActGelu: {                    // x Phi(x), Phi + x phi(x)
+        const float e = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
+        const float tail = 0.5f * e * erfc_over_exp(fabsf(x) * 0.70710678118654752f);
+        const float phi = x < 0.0f ? tail : 1.0f - tail;
+        if (SLOPE) slope = fmaf(x * 0.39894228040143268f, e, phi);
+        return x * phi;
+    }
+    case kActSilu: {                    // x s, s (1 + x (1 - s))
+        const float e = __builtin_amdgcn_exp2f(-kLog2e * x), s = 1.0f / (1.0f + e);
+        if (SLOPE) slope = s * fmaf(x, 1.0f - s, 1.0f);
+        return x * s;
+    }
+    default:
+        slope = 1.0f;
+        return x;
+    }
+}
+
+// The slope kept for the backward: binary32 beside binary32 data, and beside bf16 data 16 bits in
+// steps of 2^-15 from -1/4 on (slopes lie in [-0.13, 1.13]; 0 and 1 are exact, the rest is off by
+// 2^-16 at most, 128 times less than the gradient's own rounding), 65535 for NaN: half the bytes,
+// and nothing to evaluate in the backward.
+template <typename T> struct Slope;
+template <> struct Slope<float> {
+    using Type = float;
+    static __device__ __forceinline__ float pack(float x) { return x; }
+    static __device__ __forceinline__ float unpack(float x) { return x; }
+};
+template <> struct Slope<uint16_t> {
+    using Type = uint16_t;
+    static __device__ __forceinline__ uint16_t pack(float x) {
+        const int c = static_cast<int>(rintf(fmaf(x, 32768.0f, 8192.0f)));
+        return x != x ? 65535u : static_cast<uint16_t>(min(max(c, 0), 65534));
+    }
+    static __device__ __forceinline__ float unpack(uint16_t c) {
+        return c == 65535u ? __builtin_nanf("") : fmaf(static_cast<float>(c), 0x1p-15f, -0.25f);
+    }
+};
+
+template <typename T> __device__ __forceinline__ void load4(const void *p, int64_t at, float (&x)[4]);
+template <> __device__ __forceinline__ void load4<float>(const void *p, int64_t at, float (&x)[4]) {
+    const f32x4 v = *(const REX_GLOBAL f32x4 *)(static_cast<const float *>(p) + at);
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
+}
+template <> __device__ __forceinline__ void load4<uint16_t>(const void *p, int64_t at, float (&x)[4]) {
+    const u32x2 v = *(const REX_GLOBAL u32x2 *)(static_cast<const uint16_t *>(p) + at);
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+}
+
+__device__ __forceinline__ float load_bias(const GemmArgs &a, int n) {
+    return a.bias_bf16 ? bf16_to_f32(as_global<uint16_t>(a.bias)[n]) : as_global<float>(a.bias)[n];
+}
+
+// Four adjacent results of row m from column n on (n < N): bias, activation, residual, stores.
+template <typename T>
+__device__ __forceinline__ void finish4(const GemmArgs &a, int m, int n, f32x4 x) {
+    const int64_t at = static_cast<int64_t>(m) * a.ldo + n, dense = static_cast<int64_t>(m) * a.N + n;
+    const int64_t rat = static_cast<int64_t>(m) * a.ldr + n;
+    float y[4], s[4], r[4] = {};
+    const int left = a.N - n;
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) x[i] += load_bias(a, n + i);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = x[i];
+    if (a.act != kActNone) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = activate<true>(a.act, x[i], s[i]);
+    }
+    if (a.vec) {                        // (then N is a multiple of 4)
+        if (a.residual) {
+            load4<T>(a.residual, rat, r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += r[i];
+        }
+        Num<T>::store4(reinterpret_cast<char *>(static_cast<T *>(a.out) + at), f32x4{y[0], y[1], y[2], y[3]});
+        if (a.slope) {
+            using S = typename Slope<T>::Type;
+            using S4 = S __attribute__((ext_vector_type(4)));
+            *(REX_GLOBAL S4 *)(static_cast<S *>(a.slope) + dense) =
+                S4{Slope<T>::pack(s[0]), Slope<T>::pack(s[1]), Slope<T>::pack(s[2]), Slope<T>::pack(s[3])};
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= left) break;
+        if (a.residual) y[i] += load_f32<T>(as_global<T>(a.residual) + rat + i);
+        store_f32<T>(as_global_mut<T>(a.out) + at + i, y[i]);
+        if (a.slope) as_global_mut<typename Slope<T>::Type>(a.slope)[dense + i] = Slope<T>::pack(s[i]);
+    }
+}
+
+// Four adjacent sums of one part of k.
+__device__ __forceinline__ void store_part(const GemmArgs &a, int part, int m, int n, f32x4 x) {
+    float *to = a.part + (static_cast<int64_t>(part) * a.M + m) * a.N + n;
+    if (a.N % 4 == 0) {
+        *(REX_GLOBAL f32x4 *)(to) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < a.N) as_global_mut<float>(to)[i] = x[i];
+    }
+}
+
+}  // namespace rex

@@ -1,0 +1,180 @@
+"""Thin ctypes binding of include/box_head.h (argument marshalling only): dense layers with
+their epilogue, and the log probabilities of classes.
+
+As in `relation`, every operation runs in the library's HIP kernels on torch's current stream
+(or `stream`), and nothing falls back; descriptors are packed in one go into bytes.
+
+Paper anchors (MMDetection, arXiv 1906.07155): §3.1 RoIHead, §3.2 losses.
+"""
+from __future__ import annotations
+
+import ctypes
+import os
+import re
+import struct
+from typing import List
+
+from . import binding
+from .binding import _dtype_code, _need_cuda, _torch, check
+from .relation import _Call, _dense, _ptr, _same_device, _size
+
+HEADER = os.path.join(os.path.dirname(binding.HERE), "include", "box_head.h")
+
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}      # RE_ACT_*
+
+_VP, _I32, _SZ, _D = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_char_p
+_SZP = ctypes.POINTER(_SZ)
+
+SIGNATURES = {
+    "linear_act_workspace_size": [_D, _I32, _SZP],
+    "linear_act_fwd": [_D, _VP, _VP, _VP, _SZ, _VP],
+    "linear_act_bwd": [_D, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP],
+}
+
+# linear_act_t
+_LINEAR = struct.Struct("@4P6q3i4x")
+
+_lib = None
+
+
+def header_functions() -> List[str]:
+    """Names of the functions include/box_head.h declares."""
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    return re.findall(r"^\s*re_status_t\s+(\w+)\s*\(", text, flags=re.M)
+
+
+def lib():
+    """libroi_extract.so with this header's signatures (raises if it has not been built)."""
+    global _lib
+    if _lib is None:
+        L = binding.lib()
+        for name, argtypes in SIGNATURES.items():
+            fn = getattr(L, name)
+            fn.argtypes = argtypes
+            fn.restype = ctypes.c_int
+        _lib = L
+    return _lib
+
+
+# ---------------------------------------------------------------------------
+# Dense layers
+# ---------------------------------------------------------------------------
+
+def _matrix(t, shape, name: str, dtype):
+    """The row stride of a 2-D tensor with adjacent columns."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError("%s must be a %s tensor of shape %s (got %s %s)"
+                         % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    row, column = t.stride()
+    if column != 1 and shape[1] > 1 and shape[0] > 0:
+        raise ValueError("the columns of %s must be adjacent" % name)
+    return row
+
+
+def _linear_descriptor(x, weight, bias, act, residual):
+    torch = _torch()
+    if act not in ACTS:
+        raise ValueError("act must be one of %s (got %r)" % (sorted(ACTS), act))
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x must be 2-D [rows, ins] and weight 2-D [outs, ins] (got %s, %s)"
+                         % (tuple(x.shape), tuple(weight.shape)))
+    m, k = x.shape
+    n = weight.shape[0]
+    dtype = x.dtype
+    code = _dtype_code(x)
+    xs, ws, rs = _matrix(x, (m, k), "x", dtype), _matrix(weight, (n, k), "weight", dtype), 0
+    bias_code = 0
+    if bias is not None:
+        if bias.dtype != dtype:
+            _dense(bias, (n,), "bias", torch.float32)
+        else:
+            _dense(bias, (n,), "bias", dtype)
+            bias_code = code
+    if residual is not None:
+        rs = _matrix(residual, (m, n), "residual", dtype)
+    _need_cuda(x, "x")
+    _same_device(x, "weight bias residual", (weight, bias, residual))
+    return _LINEAR.pack(x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(residual), xs, ws, rs, m, k, n,
+                        code, bias_code, ACTS[act])
+
+
+def linear_act_workspace_size(x, weight, bias=None, backward: bool = False, *, act: str = "none") -> int:
+    """Workspace bytes of linear_act_fwd (or of linear_act_bwd where `backward`) for these tensors."""
+    d = _linear_descriptor(x, weight, bias, act, None)
+    return _size(lib().linear_act_workspace_size, "linear_act_workspace_size", d, int(backward))
+
+
+def _slope_dtype(x):
+    torch = _torch()
+    return torch.int16 if x.dtype == torch.bfloat16 else torch.float32
+
+
+def linear_act_fwd(x, weight, bias=None, *, act: str = "none", residual=None, save: bool = False, out=None,
+                   workspace=None, stream=None):
+    """y = act(x weight^T + bias) + residual of x [rows, ins] and weight [outs, ins] (one dtype, rows
+    may be strided), bias [outs] of that dtype or float32, act "none", "relu", "gelu" or "silu",
+    residual [rows, outs].  Returns (y, saved): saved, made where `save` is true, is what the
+    backward takes: None without an activation, y itself for relu without a residual, else the
+    activation's slopes."""
+    d = _linear_descriptor(x, weight, bias, act, residual)
+    shape = (x.shape[0], weight.shape[0])
+    if out is not None:
+        _dense(out, shape, "out", x.dtype)
+        _same_device(x, "out", (out,))
+    if workspace is not None:
+        binding._workspace(workspace, x)
+        _same_device(x, "workspace", (workspace,))
+    L = lib()
+    with _Call(x, stream) as c:
+        if out is None:
+            out = c.empty(shape, x.dtype)
+        saved = slope = None
+        if save and act != "none":
+            if act == "relu" and residual is None:
+                saved = out
+            else:
+                saved = slope = c.empty(shape, _slope_dtype(x))
+        need = 0
+        if workspace is None:
+            need = _size(L.linear_act_workspace_size, "linear_act_workspace_size", d, 0)
+        ws, wsb, _keep = c.workspace(workspace, need)
+        check(L.linear_act_fwd(d, out.data_ptr(), _ptr(slope), ws, wsb, c.stream), "linear_act_fwd")
+    return out, saved
+
+
+def linear_act_bwd(grad_y, x, weight, saved=None, *, bias=None, act: str = "none", want_x: bool = True,
+                   want_weight: bool = True, want_bias: bool = True, workspace=None, stream=None):
+    """Gradients of linear_act_fwd for upstream grad_y (contiguous [rows, outs]); saved as it
+    returned it.  Returns (grad_x, grad_weight, grad_bias), None for what is not wanted or (bias)
+    was not given; the residual's gradient is grad_y."""
+    torch = _torch()
+    d = _linear_descriptor(x, weight, bias, act, None)
+    shape = (x.shape[0], weight.shape[0])
+    _dense(grad_y, shape, "grad_y", x.dtype)
+    slope = y = None
+    if act == "none":
+        if saved is not None:
+            raise ValueError("saved without an activation")
+    else:
+        if saved is None:
+            raise ValueError("%s needs what the forward saved" % act)
+        if act == "relu" and saved.dtype == x.dtype:
+            y = _dense(saved, shape, "saved", x.dtype)
+        else:
+            slope = _dense(saved, shape, "saved", _slope_dtype(x))
+    _same_device(x, "grad_y saved", (grad_y, saved))
+    if workspace is not None:
+        binding._workspace(workspace, x)
+        _same_device(x, "workspace", (workspace,))
+    L = lib()
+    with _Call(x, stream) as c:
+        gx = c.empty(x.shape, x.dtype) if want_x else None
+        gw = c.empty(weight.shape, x.dtype) if want_weight else None
+        gb = c.empty(bias.shape, bias.dtype) if want_bias and bias is not None else None
+        need = 0
+        if workspace is None:
+            need = _size(L.linear_act_workspace_size, "linear_act_workspace_size", d, 1)
+        ws, wsb, _keep = c.workspace(workspace, need)
+        check(L.linear_act_bwd(d, grad_y.data_ptr(), _ptr(slope), _ptr(y), _ptr(gx), _ptr(gw), _ptr(gb), ws, wsb,
+                               c.stream), "linear_act_bwd")
+    return gx, gw, gb
