@@ -69,6 +69,44 @@ re_status_t linear_act_bwd(const linear_act_t *a, const void *grad_y, const void
                            void *grad_x, void *grad_weight, void *grad_bias, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* Log probabilities over a row's classes.  With x = scale * logits, per row:
+ *   lse = log sum_c exp(x_c),  p_c = exp(x_c - lse),
+ *   logp = x_label - lse,  entropy = -sum_c p_c log p_c,
+ * and the `top` classes of the largest logits, the lower class first among equal ones.  A label
+ * outside [0, classes) is not counted: its logp is 0 and has no gradient.  A class whose logit is
+ * -inf has p = 0; a row with no other has lse = -inf, logp = -inf, entropy 0 and no gradient.  NaN and
+ * +inf make their row's lse, logp and entropy NaN; among the top classes NaN comes first.  A row all of
+ * whose logits are at -1e9 has the probabilities that it has with all of them at 0. */
+#define RE_LOGPROB_MAX_CLASSES (1 << 24)
+#define RE_LOGPROB_MAX_ROWS (1 << 23)     /* divided by a row's parts, of 4096 classes each (RE_ERR_UNSUPPORTED) */
+#define RE_LOGPROB_MAX_TOP 16
+typedef struct {
+    const void *logits;       /* [rows][classes], row stride stride (elements) */
+    const int64_t *labels;    /* [rows] dense */
+    int64_t stride;
+    int64_t rows;             /* may be 0 */
+    int64_t classes;          /* at least 1 */
+    int32_t dtype;
+    int32_t top;              /* in [0, min(classes, RE_LOGPROB_MAX_TOP)] */
+    float scale;              /* finite, above 0 */
+} class_logprob_t;
+
+/* Device workspace of class_logprob_fwd: the parts of long rows.  Host-only. */
+re_status_t class_logprob_workspace_size(const class_logprob_t *a, size_t *bytes);
+
+/* logp, entropy: float[rows]; stats: float[rows][2], the largest x and log sum_c exp(x_c - that), whose
+ * sum is lse (-inf and 0 in a row without a class), 8-byte aligned; top_logp: float[rows][top],
+ * top_index: int64[rows][top], both dense, not used where top is 0. */
+re_status_t class_logprob_fwd(const class_logprob_t *a, float *logp, float *entropy, float *stats,
+                              float *top_logp, int64_t *top_index, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Gradient of the logits ([rows][classes] dense of dtype) for upstream grad_logp and grad_entropy
+ * (float[rows], either may be NULL: zero); stats and entropy as class_logprob_fwd wrote them:
+ *   grad_c = scale * (grad_logp ([c = label] - p_c) - grad_entropy p_c (log p_c + entropy)). */
+re_status_t class_logprob_bwd(const class_logprob_t *a, const float *grad_logp, const float *grad_entropy,
+                              const float *stats, const float *entropy, void *grad_logits, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

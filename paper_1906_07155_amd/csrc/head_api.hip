@@ -8,6 +8,7 @@
 
 #include "box_head.h"
 #include "linear.hpp"
+#include "logprob.hpp"
 
 using namespace rex;
 
@@ -174,6 +175,37 @@ void plan_backward(const linear_act_t *d, const void *grad_y, Backward &b) {
     b.bytes = b.g_bytes + b.part_bytes + std::max(b.x.bytes, b.weight.bytes);
 }
 
+re_status_t logprob_args(const class_logprob_t *d, LogprobArgs *a) {
+    *a = LogprobArgs{};
+    if (!d || !valid_dtype(d->dtype)) return RE_ERR_INVALID_ARG;
+    if (d->rows < 0 || d->classes < 1) return RE_ERR_INVALID_ARG;
+    if (d->top < 0 || d->top > RE_LOGPROB_MAX_TOP || d->top > d->classes) return RE_ERR_INVALID_ARG;
+    if (!std::isfinite(d->scale) || !(d->scale > 0.0f)) return RE_ERR_INVALID_ARG;
+    if (d->rows > 0 && (!d->logits || !d->labels)) return RE_ERR_INVALID_ARG;
+    if (!aligned(d->logits, static_cast<uintptr_t>(dtype_size(d->dtype))) || !aligned(d->labels, 8))
+        return RE_ERR_INVALID_ARG;
+    if (d->rows > 1 && (d->stride < 0 || d->stride > (int64_t(1) << 40))) return RE_ERR_INVALID_ARG;
+    if (d->classes > RE_LOGPROB_MAX_CLASSES) return RE_ERR_UNSUPPORTED;
+    a->logits = d->logits;
+    a->labels = d->labels;
+    a->stride = d->rows > 1 ? d->stride : 0;
+    a->rows = d->rows;
+    a->C = static_cast<int32_t>(d->classes);
+    a->top = d->top;
+    a->scale = d->scale;
+    a->parts = static_cast<int32_t>((d->classes + kLogprobSpan - 1) / kLogprobSpan);
+    a->each = static_cast<int32_t>(((d->classes + a->parts - 1) / a->parts + 7) / 8 * 8);
+    // a row or part may be a workgroup's work, and a launch has fewer than 2^32 threads
+    if (d->rows > RE_LOGPROB_MAX_ROWS / a->parts) return RE_ERR_UNSUPPORTED;
+    return RE_OK;
+}
+size_t logprob_part_bytes(const LogprobArgs &a) {
+    return a.parts > 1 ? align256(static_cast<size_t>(a.rows) * a.parts * sizeof(LogPart)) : 0;
+}
+size_t logprob_bytes(const LogprobArgs &a) {
+    return a.parts > 1 ? logprob_part_bytes(a) + align256(static_cast<size_t>(a.rows) * a.parts * a.top * 8) : 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -265,6 +297,55 @@ re_status_t linear_act_bwd(const linear_act_t *d, const void *grad_y, const void
         if ((st = run_product(b.weight, grad_weight, part, d->dtype, s)) != RE_OK) return st;
     }
     return RE_OK;
+}
+
+re_status_t class_logprob_workspace_size(const class_logprob_t *d, size_t *bytes) {
+    if (!bytes) return RE_ERR_INVALID_ARG;
+    LogprobArgs a;
+    const re_status_t st = logprob_args(d, &a);
+    if (st != RE_OK) return st;
+    *bytes = logprob_bytes(a);
+    return RE_OK;
+}
+
+re_status_t class_logprob_fwd(const class_logprob_t *d, float *logp, float *entropy, float *stats,
+                              float *top_logp, int64_t *top_index, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    LogprobArgs a;
+    re_status_t st = logprob_args(d, &a);
+    if (st != RE_OK) return st;
+    if (!aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 8)) return RE_ERR_INVALID_ARG;
+    if (a.rows > 0 && (!logp || !entropy || !stats)) return RE_ERR_INVALID_ARG;
+    if (a.top > 0 && (!aligned(top_logp, 4) || !aligned(top_index, 8) || (a.rows > 0 && (!top_logp || !top_index))))
+        return RE_ERR_INVALID_ARG;
+    if (a.rows == 0) return RE_OK;
+    if ((st = check_workspace(workspace, workspace_bytes, logprob_bytes(a))) != RE_OK) return st;
+    a.logp = logp;
+    a.entropy = entropy;
+    a.stats = stats;
+    a.top_logp = top_logp;
+    a.top_index = top_index;
+    a.part = static_cast<LogPart *>(workspace);
+    a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + logprob_part_bytes(a));
+    return from_hip(launch_logprob_fwd(a, d->dtype, static_cast<hipStream_t>(stream)));
+}
+
+re_status_t class_logprob_bwd(const class_logprob_t *d, const float *grad_logp, const float *grad_entropy,
+                              const float *stats, const float *entropy, void *grad_logits, void *stream) {
+    LogprobArgs a;
+    const re_status_t st = logprob_args(d, &a);
+    if (st != RE_OK) return st;
+    if (!aligned(grad_logp, 4) || !aligned(grad_entropy, 4) || !aligned(stats, 8) || !aligned(entropy, 4))
+        return RE_ERR_INVALID_ARG;
+    if (!aligned(grad_logits, static_cast<uintptr_t>(dtype_size(d->dtype)))) return RE_ERR_INVALID_ARG;
+    if (a.rows == 0) return RE_OK;
+    if (!stats || !entropy || !grad_logits) return RE_ERR_INVALID_ARG;
+    a.glogp = grad_logp;
+    a.gentropy = grad_entropy;
+    a.stats = const_cast<float *>(stats);
+    a.entropy = const_cast<float *>(entropy);
+    a.grad = grad_logits;
+    return from_hip(launch_logprob_bwd(a, d->dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

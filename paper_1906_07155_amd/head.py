@@ -29,10 +29,16 @@ SIGNATURES = {
     "linear_act_workspace_size": [_D, _I32, _SZP],
     "linear_act_fwd": [_D, _VP, _VP, _VP, _SZ, _VP],
     "linear_act_bwd": [_D, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP],
+    "class_logprob_workspace_size": [_D, _SZP],
+    "class_logprob_fwd": [_D, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP],
+    "class_logprob_bwd": [_D, _VP, _VP, _VP, _VP, _VP, _VP],
 }
 
-# linear_act_t
+# linear_act_t, class_logprob_t
 _LINEAR = struct.Struct("@4P6q3i4x")
+_LOGPROB = struct.Struct("@2P3q2if4x")
+MAX_TOP = 16                        # RE_LOGPROB_MAX_TOP
+LOGPROB_SPAN = 4096                 # rows of more classes come in parts, which need a workspace
 
 _lib = None
 
@@ -178,3 +184,69 @@ def linear_act_bwd(grad_y, x, weight, saved=None, *, bias=None, act: str = "none
         check(L.linear_act_bwd(d, grad_y.data_ptr(), _ptr(slope), _ptr(y), _ptr(gx), _ptr(gw), _ptr(gb), ws, wsb,
                                c.stream), "linear_act_bwd")
     return gx, gw, gb
+
+
+# ---------------------------------------------------------------------------
+# Log probabilities of classes
+# ---------------------------------------------------------------------------
+
+def _logprob_descriptor(logits, labels, scale, top):
+    torch = _torch()
+    if logits.dim() != 2 or logits.shape[1] < 1:
+        raise ValueError("logits must be 2-D [rows, classes] (got %s)" % (tuple(logits.shape),))
+    m, c = logits.shape
+    code = _dtype_code(logits)
+    stride, column = logits.stride()
+    if column != 1 and c > 1 and m > 0:
+        raise ValueError("the classes of logits must be adjacent")
+    if not 0 <= top <= min(c, MAX_TOP):
+        raise ValueError("top must be in [0, %d] (got %d)" % (min(c, MAX_TOP), top))
+    _dense(labels, (m,), "labels", torch.int64)
+    _need_cuda(logits, "logits")
+    _same_device(logits, "labels", (labels,))
+    return _LOGPROB.pack(logits.data_ptr(), labels.data_ptr(), stride, m, c, code, top, scale)
+
+
+def class_logprob_fwd(logits, labels, *, scale: float = 1.0, top: int = 0, workspace=None, stream=None):
+    """Log probabilities over logits [rows, classes] times `scale`: returns (logp, entropy,
+    stats, top_logp, top_index): float32 [rows] of the labels (int64 [rows]; one outside the classes is
+    not counted: 0) and of the entropy; stats float32 [rows, 2], which the backward takes, the
+    largest of a row and the log sum relative to it; float32 and int64 [rows, top] of the `top` classes
+    with the largest logits, the lower class first among equals (None where top is 0)."""
+    torch = _torch()
+    d = _logprob_descriptor(logits, labels, scale, top)
+    if workspace is not None:
+        binding._workspace(workspace, logits)
+        _same_device(logits, "workspace", (workspace,))
+    m, c = logits.shape
+    L = lib()
+    with _Call(logits, stream) as call:
+        logp, entropy, stats = call.empty((m,), torch.float32), call.empty((m,), torch.float32), call.empty((m, 2), torch.float32)
+        top_logp = top_index = None
+        if top:
+            top_logp, top_index = call.empty((m, top), torch.float32), call.empty((m, top), torch.int64)
+        need = 0
+        if workspace is None and c > LOGPROB_SPAN:
+            need = _size(L.class_logprob_workspace_size, "class_logprob_workspace_size", d)
+        ws, wsb, _keep = call.workspace(workspace, need)
+        check(L.class_logprob_fwd(d, logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(), _ptr(top_logp),
+                                  _ptr(top_index), ws, wsb, call.stream), "class_logprob_fwd")
+    return logp, entropy, stats, top_logp, top_index
+
+
+def class_logprob_bwd(grad_logp, grad_entropy, logits, labels, stats, entropy, *, scale: float = 1.0, stream=None):
+    """Gradient of the logits ([rows, classes] of their dtype) for upstream grad_logp and grad_entropy
+    (float32 [rows], either may be None); stats and entropy as class_logprob_fwd returned them."""
+    torch = _torch()
+    d = _logprob_descriptor(logits, labels, scale, 0)
+    m, c = logits.shape
+    _dense(stats, (m, 2), "stats", torch.float32)
+    for t, name in ((grad_logp, "grad_logp"), (grad_entropy, "grad_entropy"), (entropy, "entropy")):
+        if t is not None:
+            _dense(t, (m,), name, torch.float32)
+    _same_device(logits, "grad_logp grad_entropy stats entropy", (grad_logp, grad_entropy, stats, entropy))
+    with _Call(logits, stream) as call:
+        grad = call.empty((m, c), logits.dtype)
+        check(lib().class_logprob_bwd(d, _ptr(grad_logp), _ptr(grad_entropy), stats.data_ptr(), entropy.data_ptr(),
+                                      grad.data_ptr(), call.stream), "class_logprob_bwd")
+    return grad
