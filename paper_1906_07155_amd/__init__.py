@@ -12,6 +12,7 @@ from .binding import (RoIExtractError, box_nms, box_nms_batched, deform_roi_pool
 from .relation import (box_attn_bwd, box_attn_fwd, box_attn_workspace_size, box_memory,
                        box_memory_append, box_memory_attn_fwd, box_memory_read, gated_norm_bwd,
                        gated_norm_fwd)
+from .evict import box_memory_evict, box_memory_weigh
 from .head import class_logprob_bwd, class_logprob_fwd, linear_act_bwd, linear_act_fwd, linear_act_workspace_size
 
 __all__ = ["RoIExtractError", "box_nms", "box_nms_batched", "deform_roi_pool_bwd", "deform_roi_pool_fwd", "fpn_level_map", "lib", "plan", "plan_offsets", "plan_perm",
@@ -20,7 +21,7 @@ __all__ = ["RoIExtractError", "box_nms", "box_nms_batched", "deform_roi_pool_bwd
            "RoIAlignFunction", "box_attn_bwd", "box_attn_fwd", "box_attn_workspace_size",
            "box_memory", "box_memory_append", "box_memory_attn_fwd", "box_memory_read",
            "gated_norm_bwd", "gated_norm_fwd",
-           "class_logprob_bwd", "class_logprob_fwd", "linear_act_bwd", "linear_act_fwd", "linear_act_workspace_size",
+           "box_memory_evict", "box_memory_weigh", "class_logprob_bwd", "class_logprob_fwd", "linear_act_bwd", "linear_act_fwd", "linear_act_workspace_size",
            "BoxMemory", "RelationHead", "box_attention", "gated_norm"]
 
 

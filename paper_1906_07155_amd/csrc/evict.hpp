@@ -1,0 +1,30 @@
+// evict.hpp -- argument blocks and launchers of what the memory of boxes forgets.
+#pragma once
+
+#include "relation.hpp"
+
+namespace rex {
+
+struct WeighArgs {
+    AttnArgs a;                     // the recall's
+    const float *lse, *weight;      // weight may be null
+    float *out;
+    float decay;
+};
+constexpr int kFewQueries = 16;     // of a stream: one column tile of the products
+hipError_t launch_weigh(const WeighArgs &w, int dtype, hipStream_t s);
+
+struct EvictArgs {
+    int8_t *k, *v;
+    float *ks, *vs, *boxes;
+    int64_t num_pages;
+    int32_t Hkv, D, B, max_pages;
+    const int32_t *pages, *lengths, *keep;
+    const float *weight;
+    int32_t *lengths_out, *origin;  // origin may be null
+    float *weight_out;
+    int32_t *freed, *to;            // [B][places]: free places in order; where a place's box goes, or -1
+};
+hipError_t launch_evict(const EvictArgs &e, hipStream_t s);
+
+}  // namespace rex
