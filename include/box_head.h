@@ -54,8 +54,9 @@ typedef struct {
 re_status_t linear_act_workspace_size(const linear_act_t *a, int32_t backward, size_t *bytes);
 
 /* y: [rows][outs] dense.  slope: the activation's slope at every t, [rows][outs] dense, which the
- * backward takes, or NULL: binary32 with binary32 data; with bf16 data 16 bits each, c for
- * c * 2^-15 - 1/4 (65535: NaN).  It has to be NULL for RE_ACT_NONE. */
+ * backward takes, or NULL: binary32 with binary32 data; with bf16 data 3 * rows * outs bytes, for
+ * numbers c of 24 bits that stand for c * 2^-23 - 1/4 (all ones: NaN), the upper 16 bits of all and then
+ * the lower 8 of all, 16-byte aligned.  It has to be NULL for RE_ACT_NONE. */
 re_status_t linear_act_fwd(const linear_act_t *a, void *y, void *slope, void *workspace,
                            size_t workspace_bytes, void *stream);
 

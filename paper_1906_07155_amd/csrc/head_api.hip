@@ -238,7 +238,7 @@ re_status_t linear_act_fwd(const linear_act_t *d, void *y, void *slope, void *wo
     if (st != RE_OK) return st;
     if (slope && d->act == RE_ACT_NONE) return RE_ERR_INVALID_ARG;
     const uintptr_t size = static_cast<uintptr_t>(dtype_size(d->dtype));
-    if (!aligned(y, size) || !aligned(slope, size)) return RE_ERR_INVALID_ARG;
+    if (!aligned(y, size) || !aligned(slope, d->dtype == RE_DTYPE_BF16 ? 16 : 4)) return RE_ERR_INVALID_ARG;
     if (d->rows == 0) return RE_OK;
     if (!y) return RE_ERR_INVALID_ARG;
     Product g;
@@ -260,7 +260,8 @@ re_status_t linear_act_bwd(const linear_act_t *d, const void *grad_y, const void
     re_status_t st = check_linear(d);
     if (st != RE_OK) return st;
     const int64_t size = dtype_size(d->dtype);
-    for (const void *p : {grad_y, slope, y, static_cast<const void *>(grad_x), static_cast<const void *>(grad_weight)})
+    if (!aligned(slope, d->dtype == RE_DTYPE_BF16 ? 16 : 4)) return RE_ERR_INVALID_ARG;
+    for (const void *p : {grad_y, y, static_cast<const void *>(grad_x), static_cast<const void *>(grad_weight)})
         if (!aligned(p, static_cast<uintptr_t>(size))) return RE_ERR_INVALID_ARG;
     if (grad_bias && (!d->bias || !aligned(grad_bias, static_cast<uintptr_t>(dtype_size(d->bias_dtype)))))
         return RE_ERR_INVALID_ARG;

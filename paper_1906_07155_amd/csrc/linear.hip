@@ -115,9 +115,19 @@ hipError_t launch_gemm_join(const GemmArgs &a, int dtype, hipStream_t s) {
 // before the product is rounded.  `lanes` (a power of two) lanes take a row, so that narrow layers
 // use whole waves too.
 
+// 16 bytes of them
+template <typename T, int V> __device__ __forceinline__ void load_run(const T *p, float *x) {
+    using Chunk = T __attribute__((ext_vector_type(V)));
+    const Chunk c = *(const REX_GLOBAL Chunk *)(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if constexpr (sizeof(T) == 2) x[i] = bf16_to_f32(c[i]);
+        else x[i] = c[i];
+    }
+}
+
 template <typename T, int V, bool SLOPE, bool RELU>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, int lanes, int strips) {
-    using S = typename Slope<T>::Type;
     __shared__ float sums[256 * V];
     const int strip = blockIdx.x % strips, block = blockIdx.x / strips;
     const int slot = threadIdx.x / lanes, slots = 256 / lanes;
@@ -131,26 +141,12 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, int lanes, int 
             float g[V], f[V];
             if constexpr (V == 1) {
                 g[0] = load_f32<T>(as_global<T>(a.gy) + at);
-                if (SLOPE) f[0] = RELU ? load_f32<T>(as_global<T>(a.saved) + at) : Slope<T>::unpack(as_global<S>(a.saved)[at]);
+                if (SLOPE && RELU) f[0] = load_f32<T>(as_global<T>(a.saved) + at);
             } else {
-                using Chunk = T __attribute__((ext_vector_type(V)));
-                using SChunk = S __attribute__((ext_vector_type(V)));
-                const Chunk c = *(const REX_GLOBAL Chunk *)(static_cast<const T *>(a.gy) + at);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    if constexpr (sizeof(T) == 2) g[i] = bf16_to_f32(c[i]);
-                    else g[i] = c[i];
-                }
-                if (SLOPE) {
-                    const SChunk d = *(const REX_GLOBAL SChunk *)(static_cast<const S *>(a.saved) + at);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        if constexpr (RELU && sizeof(T) == 2) f[i] = bf16_to_f32(d[i]);
-                        else if constexpr (RELU) f[i] = d[i];
-                        else f[i] = Slope<T>::unpack(d[i]);
-                    }
-                }
+                load_run<T, V>(static_cast<const T *>(a.gy) + at, g);
+                if (SLOPE && RELU) load_run<T, V>(static_cast<const T *>(a.saved) + at, f);
             }
+            if (SLOPE && !RELU) Slope<T>::template load<V>(a.saved, a.M * a.N, at, f);
             if (SLOPE) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) g[i] = RELU ? (f[i] <= 0.0f ? 0.0f : g[i]) : g[i] * f[i];

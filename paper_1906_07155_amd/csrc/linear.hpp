@@ -105,24 +105,54 @@ __device__ __forceinline__ float activate(int act, float x, float &slope) {
     }
 }
 
-// The slope kept for the backward: binary32 beside binary32 data, and beside bf16 data 16 bits in
-// steps of 2^-15 from -1/4 on (slopes lie in [-0.13, 1.13]; 0 and 1 are exact, the rest is off by
-// 2^-16 at most, 128 times less than the gradient's own rounding), 65535 for NaN: half the bytes,
-// and nothing to evaluate in the backward.
+// The slope kept for the backward: binary32 beside binary32 data, and beside bf16 data 24 bits in
+// steps of 2^-23 from -1/4 on (slopes lie in [-0.13, 1.13]; 0 and 1 are exact), all ones for NaN: the
+// upper 16 of all slopes, then the lower 8 of all.  (16 bits would do for the products, whose operands
+// are bf16, but the bias gradient, a binary32 sum over all rows, would be 1.3e-5 of itself off; binary32
+// would be a quarter more bytes than 24 bits, and there is nothing to evaluate in the backward.)
 template <typename T> struct Slope;
 template <> struct Slope<float> {
-    using Type = float;
-    static __device__ __forceinline__ float pack(float x) { return x; }
-    static __device__ __forceinline__ float unpack(float x) { return x; }
+    template <int V> static __device__ __forceinline__ void store(void *p, int64_t, int64_t at, const float *x) {
+        using W = float __attribute__((ext_vector_type(V), aligned(4)));
+        W w;
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = x[i];
+        *(REX_GLOBAL W *)(static_cast<float *>(p) + at) = w;
+    }
+    template <int V> static __device__ __forceinline__ void load(const void *p, int64_t, int64_t at, float *x) {
+        using W = float __attribute__((ext_vector_type(V), aligned(4)));
+        const W w = *(const REX_GLOBAL W *)(static_cast<const float *>(p) + at);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = w[i];
+    }
 };
 template <> struct Slope<uint16_t> {
-    using Type = uint16_t;
-    static __device__ __forceinline__ uint16_t pack(float x) {
-        const int c = static_cast<int>(rintf(fmaf(x, 32768.0f, 8192.0f)));
-        return x != x ? 65535u : static_cast<uint16_t>(min(max(c, 0), 65534));
+    // slopes `at` .. at + V - 1 of `all`; V > 1: at and all are multiples of V
+    template <int V> static __device__ __forceinline__ void store(void *p, int64_t all, int64_t at, const float *x) {
+        using H = uint16_t __attribute__((ext_vector_type(V)));
+        using L = uint8_t __attribute__((ext_vector_type(V)));
+        H h;
+        L l;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = min(max(static_cast<int>(rintf(fmaf(x[i], 0x1p23f, 0x1p21f))), 0), 0xfffffe);
+            const uint32_t u = x[i] != x[i] ? 0xffffffu : static_cast<uint32_t>(c);
+            h[i] = static_cast<uint16_t>(u >> 8);
+            l[i] = static_cast<uint8_t>(u);
+        }
+        *(REX_GLOBAL H *)(static_cast<uint16_t *>(p) + at) = h;
+        *(REX_GLOBAL L *)(static_cast<uint8_t *>(p) + 2 * all + at) = l;
     }
-    static __device__ __forceinline__ float unpack(uint16_t c) {
-        return c == 65535u ? __builtin_nanf("") : fmaf(static_cast<float>(c), 0x1p-15f, -0.25f);
+    template <int V> static __device__ __forceinline__ void load(const void *p, int64_t all, int64_t at, float *x) {
+        using H = uint16_t __attribute__((ext_vector_type(V)));
+        using L = uint8_t __attribute__((ext_vector_type(V)));
+        const H h = *(const REX_GLOBAL H *)(static_cast<const uint16_t *>(p) + at);
+        const L l = *(const REX_GLOBAL L *)(static_cast<const uint8_t *>(p) + 2 * all + at);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const uint32_t u = static_cast<uint32_t>(h[i]) << 8 | l[i];
+            x[i] = u == 0xffffffu ? __builtin_nanf("") : fmaf(static_cast<float>(u), 0x1p-23f, -0.25f);
+        }
     }
 };
 
@@ -165,12 +195,7 @@ __device__ __forceinline__ void finish4(const GemmArgs &a, int m, int n, f32x4 x
             for (int i = 0; i < 4; ++i) y[i] += r[i];
         }
         Num<T>::store4(reinterpret_cast<char *>(static_cast<T *>(a.out) + at), f32x4{y[0], y[1], y[2], y[3]});
-        if (a.slope) {
-            using S = typename Slope<T>::Type;
-            using S4 = S __attribute__((ext_vector_type(4)));
-            *(REX_GLOBAL S4 *)(static_cast<S *>(a.slope) + dense) =
-                S4{Slope<T>::pack(s[0]), Slope<T>::pack(s[1]), Slope<T>::pack(s[2]), Slope<T>::pack(s[3])};
-        }
+        if (a.slope) Slope<T>::template store<4>(a.slope, static_cast<int64_t>(a.M) * a.N, dense, s);
         return;
     }
 #pragma unroll
@@ -178,7 +203,7 @@ __device__ __forceinline__ void finish4(const GemmArgs &a, int m, int n, f32x4 x
         if (i >= left) break;
         if (a.residual) y[i] += load_f32<T>(as_global<T>(a.residual) + rat + i);
         store_f32<T>(as_global_mut<T>(a.out) + at + i, y[i]);
-        if (a.slope) as_global_mut<typename Slope<T>::Type>(a.slope)[dense + i] = Slope<T>::pack(s[i]);
+        if (a.slope) Slope<T>::template store<1>(a.slope, static_cast<int64_t>(a.M) * a.N, dense + i, s + i);
     }
 }
 

@@ -110,9 +110,12 @@ def linear_act_workspace_size(x, weight, bias=None, backward: bool = False, *, a
     return _size(lib().linear_act_workspace_size, "linear_act_workspace_size", d, int(backward))
 
 
-def _slope_dtype(x):
+def _slope(x, shape):
+    """Shape and type of a layer's slopes: 24 bits each beside bf16 data."""
     torch = _torch()
-    return torch.int16 if x.dtype == torch.bfloat16 else torch.float32
+    if x.dtype == torch.bfloat16:
+        return (3 * shape[0] * shape[1],), torch.uint8
+    return shape, torch.float32
 
 
 def linear_act_fwd(x, weight, bias=None, *, act: str = "none", residual=None, save: bool = False, out=None,
@@ -139,7 +142,7 @@ def linear_act_fwd(x, weight, bias=None, *, act: str = "none", residual=None, sa
             if act == "relu" and residual is None:
                 saved = out
             else:
-                saved = slope = c.empty(shape, _slope_dtype(x))
+                saved = slope = c.empty(*_slope(x, shape))
         need = 0
         if workspace is None:
             need = _size(L.linear_act_workspace_size, "linear_act_workspace_size", d, 0)
@@ -167,7 +170,8 @@ def linear_act_bwd(grad_y, x, weight, saved=None, *, bias=None, act: str = "none
         if act == "relu" and saved.dtype == x.dtype:
             y = _dense(saved, shape, "saved", x.dtype)
         else:
-            slope = _dense(saved, shape, "saved", _slope_dtype(x))
+            like, dtype = _slope(x, shape)
+            slope = _dense(saved, like, "saved", dtype)
     _same_device(x, "grad_y saved", (grad_y, saved))
     if workspace is not None:
         binding._workspace(workspace, x)

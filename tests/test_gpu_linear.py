@@ -5,7 +5,7 @@ the sum S of the products' magnitudes (each of n roundings is off by at most 2^-
 sum, signs are random, and 4 deviations of that walk stay below it; 8 for short sums).  The activations
 change such an error by a factor of at most 1.13, and are off by 2^-17 of their value at most (of
 that x^2 / 2 * 2^-23 for |x| <= 8 from the exponent's argument).  A result is off by half a step of
-its type more.  The gradient g = grad_y * slope of bf16 data has slopes off by 2^-16 and, where the
+its type more.  The gradient g = grad_y * slope of bf16 data has slopes off by 2^-23 and, where the
 slope is not 0 or 1, is rounded to bf16 (2^-8): both enter the products with the other operand's
 magnitude.
 """
@@ -61,6 +61,14 @@ def within(got, want, tolerance, what):
         what, int(bad.sum()), bad.numel(), float((err / tolerance).max()))
 
 
+def kept(saved, dtype, m, n):
+    """What the backward takes the slopes (or relu's result) from, as numbers."""
+    if dtype == torch.float32 or saved.dtype == dtype:
+        return saved.double()
+    upper = saved[:2 * m * n].view(torch.int16).int() & 0xffff
+    return ((upper << 8 | saved[2 * m * n:].int()).double() * 2.0 ** -23 - 0.25).view(m, n)
+
+
 def check(seed, m, n, k, dtype, act="none", bias=torch.float32, residual=False, wide=0, backward=True):
     x, w, b, r, gy = make(seed, m, n, k, dtype, bias, residual, wide)
     y, saved = rex.linear_act_fwd(x, w, b, act=act, residual=r, save=True)
@@ -75,17 +83,21 @@ def check(seed, m, n, k, dtype, act="none", bias=torch.float32, residual=False, 
     assert (saved is None) == (act == "none")
     if not backward:
         return
+    if act in ("gelu", "silu"):
+        slope = slope64(act, t)
+        err = (kept(saved, dtype, m, n) - slope).abs()
+        assert bool((err <= 0.8 * tol_t + 2.0 ** -17 * slope.abs() + 2.0 ** -22).all())
     grads = rex.linear_act_bwd(gy, x, w, saved, bias=b, act=act)
     g64 = gy.double()
     if act == "relu":           # (a sum next to 0 may fall to either side)
-        on = (saved.double() > 0) if saved.dtype == dtype else (saved != 8192)
+        on = kept(saved, dtype, m, n) > 0
         assert bool((on == (t > 0))[t.abs() > tol_t].all())
         g, g_tol = g64 * on, torch.zeros_like(g64)
     else:
         g = g64 * slope64(act, t)
         # (the second derivatives are below 0.8)
         g_tol = g64.abs() * (0.8 * tol_t + 2.0 ** -17) if act != "none" else torch.zeros_like(g64)
-    col_tol = g_tol + (g64.abs() * 2.0 ** -16 if dtype == torch.bfloat16 and act in ("gelu", "silu") else 0)
+    col_tol = g_tol + (g64.abs() * 2.0 ** -23 if dtype == torch.bfloat16 and act in ("gelu", "silu") else 0)
     if dtype == torch.bfloat16 and act in ("gelu", "silu"):
         g_tol = col_tol + 2.0 ** -8 * g.abs()
     within(grads[0], g @ wd, short(n) * (g.abs() @ wd.abs()) + g_tol @ wd.abs(), "grad_x")
