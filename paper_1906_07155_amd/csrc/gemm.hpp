@@ -28,13 +28,32 @@ namespace rex {
 #define REX_LDS_LOAD(r, to, off) (void)0
 #endif
 
-// One operand's tile of ROWS rows.
+// The products of a type: 16 x 16 results, rows 4g .. 4g + 3 (g = l / 16) of column l % 16 in lane l.
+// (32x32x16 products of bf16 read half as many operands' registers, and yet 8192^3 took 1030 us with
+// them where it took 935 on the same card.)
+template <typename T> struct Shape;
+template <> struct Shape<uint16_t> {
+    using Frag = bf16x8;
+    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Shape<float> {
+    using Frag = f32x4;
+    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// One operand's tile of ROWS rows, 128 bytes of k each.
 template <typename T, bool TR, int ROWS, int WAVES, bool WHOLE>
 struct Side {
-    static constexpr int kSize = sizeof(T), kChunk = 16 / kSize, kStep = 8 * kChunk;   // elements
-    static constexpr int kBytes = ROWS * 128, kLoads = ROWS / (8 * WAVES);             // of a wave
-    static constexpr int kPitch = TR ? ROWS * kSize : 128, kPieces = kPitch / 16;      // of a line
-    using Frag = std::conditional_t<kSize == 2, bf16x8, f32x4>;
+    static constexpr int kSize = sizeof(T), kChunk = 16 / kSize, kStep = 128 / kSize;   // elements
+    static constexpr int kBytes = ROWS * 128, kLoads = kBytes / (1024 * WAVES);         // of a wave
+    static constexpr int kPitch = TR ? ROWS * kSize : 128, kPieces = kPitch / 16;       // of a line
+    using Frag = typename Shape<T>::Frag;
     using Place = REX_LDS char *;
 
     // what the loads need: the lane's offsets, and the k and first row of its chunks in a step
@@ -45,8 +64,11 @@ struct Side {
     int left_k, left_rows;
     u32x4 held[WHOLE ? 1 : kLoads];
 
+    // What spreads a line's chunks over the banks for the lanes that read together: eight lanes with a
+    // chunk of eight rows each (k adjacent); 32 lanes with 32 bytes of eight lines (transposed bf16: lines
+    // 0-3 and 8-11 of 16), 64 with 64 bytes of every fourth line (transposed binary32).
     static __device__ __forceinline__ int turn(int line) {
-        if (!TR) return (line & 3) | (line >> 1 & 4);
+        if (!TR) return line & 7;
         if (kSize == 4) return 4 * (line >> 2 & 3);
         return 2 * (((line & 3) | (line >> 1 & 4)) >> (ROWS == 64 ? 1 : 0));
     }
@@ -106,37 +128,36 @@ struct Side {
         }
     }
 
-    // Operands of the half s of a step, product t of the wave whose first row is `base`.
+    // Operands of half s of a step, product t of the wave whose first row is `base`.
     struct Reader {
-        int at[TR ? 1 : 2], row, n, g;
+        int at[TR ? 1 : 2], tile, g;
         __device__ __forceinline__ Reader(int base, int lane) {
-            n = lane & 15;
-            g = lane >> 4;
-            row = base / 16;
+            const int n = lane & 15;              // row or column of a product
+            g = lane >> 4;                        // which chunk of k
+            tile = base / 16;
             if constexpr (!TR) {
-                const int line = base + 8 * (n >> 2) + (n & 3);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) at[s] = line * 128 + ((4 * s + g) ^ (n & 7)) * 16;
-            } else if constexpr (kSize == 2) {
+                for (int s = 0; s < 2; ++s) at[s] = (base + n) * 128 + ((4 * s + g) ^ turn(base + n)) * 16;
+            } else if constexpr (kSize == 2) {    // sixteen lanes transpose four lines
                 at[0] = (8 * g + (n >> 2)) * kPitch + (n >> 1 & 1) * 16 + (n & 1) * 8;
+                g = turn(8 * g + (n >> 2)) / 2;
             } else {
                 at[0] = 4 * g * kPitch + n * 4;
             }
         }
-        __device__ __forceinline__ Frag get(const char *tile, int t, int s) const {
-            Place p = (Place)(const_cast<char *>(tile));
+        __device__ __forceinline__ Frag get(const char *data, int t, int s) const {
+            Place p = (Place)(const_cast<char *>(data));
             if constexpr (!TR) {
-                return *(const REX_LDS Frag *)(p + at[s] + (t >> 1) * 4096 + (t & 1) * 512);
+                return *(const REX_LDS Frag *)(p + at[s] + t * 2048);
             } else if constexpr (kSize == 2) {
 #ifdef __HIP_DEVICE_COMPILE__
                 using s16x4 = short __attribute__((ext_vector_type(4)));
                 using s16x8 = short __attribute__((ext_vector_type(8)));
-                const int chunk = 2 * (row + t) ^ turn(8 * g + (n >> 2));
                 s16x4 x[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (REX_LDS s16x4 *)(p + at[0] + chunk * 16 + (32 * s + 4 * e) * kPitch));
+                        (REX_LDS s16x4 *)(p + at[0] + ((tile + t) ^ g) * 32 + (32 * s + 4 * e) * kPitch));
                 return __builtin_bit_cast(Frag, s16x8{x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]});
 #else
                 return Frag{};
@@ -145,57 +166,43 @@ struct Side {
                 Frag f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    f[j] = *(const REX_LDS float *)(p + at[0] + ((row + t) ^ g) * 64 + (16 * s + j) * kPitch);
+                    f[j] = *(const REX_LDS float *)(p + at[0] + ((tile + t) ^ g) * 64 + (16 * s + j) * kPitch);
                 return f;
             }
-        }
-        // the first of the four rows that a lane's results of product t are (P side), or the row
-        // of its column (Q side)
-        __device__ __forceinline__ int result_row(int t) const {
-            return 16 * row + (TR ? 16 * t + 4 * g : 32 * (t >> 1) + 8 * g + 4 * (t & 1));
-        }
-        __device__ __forceinline__ int result_column(int t) const {
-            return 16 * row + (TR ? 16 * t + n : 32 * (t >> 1) + 8 * (n >> 2) + 4 * (t & 1) + (n & 3));
         }
     };
 };
 
-__device__ __forceinline__ f32x4 gemm_mma(bf16x8 a, bf16x8 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 gemm_mma(f32x4 a, f32x4 b, f32x4 c) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
-    return c;
-}
-
 // WM x WN waves of MT x NT products each.
 template <typename T, bool TP, bool TQ, int MT, int NT, int WM, int WN, bool WHOLE, int OCC>
 __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
-    constexpr int kWaves = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN;
+    constexpr int kWaves = WM * WN, kRows = 16 * MT, kCols = 16 * NT, BM = kRows * WM, BN = kCols * WN;
     using P = Side<T, TP, BN, kWaves, WHOLE>;
     using Q = Side<T, TQ, BM, kWaves, WHOLE>;
     using Frag = typename P::Frag;
     __shared__ __attribute__((aligned(16))) char smem[2][P::kBytes + Q::kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups go to the eight XCDs in turn: each takes a run of neighbouring tiles, in groups of
-    // eight rows of tiles, whose operands its L2 then holds.
-    const int tiles = a.tiles_m * a.tiles_n, all = tiles * a.split;
-    int id = (blockIdx.x & 7) * ((all + 7) >> 3) + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= ((all + 7) >> 3) || id >= all) return;
-    const int part = id / tiles;
-    id -= part * tiles;
-    const int band = id / (8 * a.tiles_n), rows = min(8, a.tiles_m - 8 * band);
+    // First the tiles that are made whole, then the parts of the others.  Workgroups go to the eight XCDs
+    // in turn: each takes a run of neighbouring tiles, in groups of eight rows of tiles, whose operands
+    // its L2 then holds.
+    const bool parted = static_cast<int>(blockIdx.x) >= a.grid_whole;
+    const int block = blockIdx.x - (parted ? a.grid_whole : 0), some = parted ? a.parted * a.split : a.whole;
+    int id = (block & 7) * ((some + 7) >> 3) + (block >> 3);
+    if ((block >> 3) >= ((some + 7) >> 3) || id >= some) return;
+    const int part = parted ? id / a.parted : 0, rest = parted ? id % a.parted : 0;
+    if (parted) id = a.whole + rest;
+    const int band = id / (8 * a.tiles_n), rows_of = min(8, a.tiles_m - 8 * band);
     id -= band * 8 * a.tiles_n;
-    const int m0 = (8 * band + id % rows) * BM, n0 = id / rows * BN;
+    const int m0 = (8 * band + id % rows_of) * BM, n0 = id / rows_of * BN;
 
-    const int k0 = part * a.steps * P::kStep;
-    const int steps = min(a.steps, (a.K - k0 + P::kStep - 1) / P::kStep);
+    const int k_steps = (a.K + P::kStep - 1) / P::kStep;
+    const int first = parted ? part * a.steps : 0, steps = parted ? min(a.steps, k_steps - first) : k_steps;
+    const int k0 = first * P::kStep;
     P p(a.p, a.ldp, n0, a.N, k0, a.K, wave, lane);
     Q q(a.q, a.ldq, m0, a.M, k0, a.K, wave, lane);
     const int wn = wave % WN, wm = wave / WN;
-    const typename P::Reader pr(wn * 16 * NT, lane);
-    const typename Q::Reader qr(wm * 16 * MT, lane);
+    const typename P::Reader pr(wn * kCols, lane);
+    const typename Q::Reader qr(wm * kRows, lane);
 
     f32x4 acc[MT][NT] = {};
     p.load(smem[0], wave);
@@ -208,6 +215,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        // (all of a step's reads before the next step's loads: the compiler takes those for writes to
+        // what is read, and would wait)
         Frag pf[2][NT], qf[2][MT];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -225,7 +234,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = gemm_mma(pf[s][j], qf[s][i], acc[i][j]);
+                for (int j = 0; j < NT; ++j) acc[i][j] = Shape<T>::mma(pf[s][j], qf[s][i], acc[i][j]);
     }
     // (the compiler leaves out the wait states between products and a use behind a branch)
     asm volatile("s_nop 15" ::: "memory");
@@ -233,31 +242,37 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
     // Results go through LDS, each wave's to a place of its own, so that a row's are written by
     // neighbouring lanes and the epilogue is there once.  16-byte chunks are spread over the banks by
     // their row.
-    constexpr int kRound = MT > 4 ? 4 : MT, kQuads = 4 * NT;        // products' rows at a time
-    static_assert(kRound * NT * 1024 * kWaves <= static_cast<int>(sizeof(smem)), "results of a round");
+    // A lane's columns are the same in every row that it writes.
+    constexpr int kFit = static_cast<int>(sizeof(smem)) / (16 * kCols * 4 * kWaves);
+    constexpr int kRound = MT <= kFit ? MT : MT / 2, kQuads = kCols / 4, kStride = 64 / kQuads;
+    static_assert(kRound <= kFit && MT % kRound == 0, "results of a round");
     __builtin_amdgcn_s_barrier();
-    f32x4 *stage = reinterpret_cast<f32x4 *>(&smem[0][0]) + wave * kRound * NT * 64;
-    const int wave_m = m0 + wm * 16 * MT, wave_n = n0 + wn * 16 * NT;
+    f32x4 *stage = reinterpret_cast<f32x4 *>(&smem[0][0]) + wave * kRound * 16 * kQuads;
+    const int quad = lane % kQuads, n = n0 + wn * kCols + 4 * quad, left = a.N - n;
+    const int wave_m = wm * kRows + lane / kQuads;
+    const f32x4 bias = parted ? f32x4{} : load_bias(a, min(n, a.N - 1));
+    f32x4 *sums = reinterpret_cast<f32x4 *>(a.part) + (static_cast<int64_t>(part) * a.parted + rest) * (BM * BN / 4) +
+                  (wn * kCols >> 2) + quad;
 #pragma unroll
     for (int r = 0; r < MT; r += kRound) {
 #pragma unroll
         for (int i = 0; i < kRound; ++i) {
-            const int row = qr.result_column(r + i) - wm * 16 * MT - 16 * r;
+            const int row = 16 * i + (lane & 15);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int quad = (pr.result_row(j) - wn * 16 * NT) >> 2;
-                stage[row * kQuads + (quad ^ (row & (kQuads - 1)))] = acc[r + i][j];
-            }
+            for (int j = 0; j < NT; ++j)
+                stage[row * kQuads + ((4 * j + (lane >> 4)) ^ (row & (kQuads - 1)))] = acc[r + i][j];
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 2
-        for (int i = lane; i < kRound * NT * 64; i += 64) {
-            const int row = i / kQuads, quad = i % kQuads;
-            const f32x4 x = stage[row * kQuads + (quad ^ (row & (kQuads - 1)))];
-            const int m = wave_m + 16 * r + row, n = wave_n + 4 * quad;
-            if (m >= a.M || n >= a.N) continue;
-            if (a.split > 1) store_part(a, part, m, n, x);
-            else finish4<T>(a, m, n, x);
+        const int m = m0 + wave_m + 16 * r, rows = left > 0 ? a.M - m : 0;
+        int64_t at = static_cast<int64_t>(m) * a.N + n, rat = m * a.ldr + n;
+#pragma unroll 4
+        for (int i = 0; i < 16 * kRound; i += kStride) {
+            const int row = i + lane / kQuads;
+            const f32x4 x = stage[row * kQuads + (quad ^ (row & (kQuads - 1)))] + bias;
+            if (parted) as_global_mut<f32x4>(sums)[(wave_m + 16 * r + i) * (BN / 4)] = x;
+            else if (i < rows) finish4<T>(a, left, at, rat, x);
+            at += static_cast<int64_t>(kStride) * a.N;
+            rat += kStride * a.ldr;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -265,8 +280,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
 
 template <typename T, bool TP, bool TQ, int MT, int NT, int WM, int WN, bool WHOLE, int OCC>
 hipError_t run_gemm(const GemmArgs &a, hipStream_t s) {
-    const int64_t all = static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.split;
-    gemm_kernel<T, TP, TQ, MT, NT, WM, WN, WHOLE, OCC><<<static_cast<uint32_t>((all + 7) / 8 * 8), 64 * WM * WN, 0, s>>>(a);
+    const uint32_t grid = a.grid_whole + (a.parted * a.split + 7) / 8 * 8;
+    gemm_kernel<T, TP, TQ, MT, NT, WM, WN, WHOLE, OCC><<<grid, 64 * WM * WN, 0, s>>>(a);
     return hipGetLastError();
 }
 

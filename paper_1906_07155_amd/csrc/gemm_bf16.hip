@@ -5,9 +5,9 @@ namespace rex {
 
 template <bool TP, bool TQ>
 static hipError_t run(const GemmArgs &a, const GemmPlan &p, hipStream_t s) {
-    if (!p.whole) return run_gemm<uint16_t, TP, TQ, 2, 2, 2, 2, false, 2>(a, s);
+    if (!p.chunks) return run_gemm<uint16_t, TP, TQ, 2, 2, 2, 2, false, 2>(a, s);
     if (p.tile == kTileLarge) return run_gemm<uint16_t, TP, TQ, 8, 4, 2, 4, true, 2>(a, s);
-    if (p.tile == kTileMiddle) return run_gemm<uint16_t, TP, TQ, 4, 4, 2, 2, true, 2>(a, s);
+    if (p.tile == kTileMiddle) return run_gemm<uint16_t, TP, TQ, 4, 2, 2, 4, true, 4>(a, s);
     return run_gemm<uint16_t, TP, TQ, 2, 2, 2, 2, true, 2>(a, s);
 }
 

@@ -32,7 +32,7 @@ struct Matrix {
     int64_t rows, cols, stride;
 };
 // 16-byte chunks of rows and nothing else: what the fast kernels read.
-bool whole(const Matrix &x, int64_t size) {
+bool chunks(const Matrix &x, int64_t size) {
     return aligned(x.p, 16) && x.cols * size % 16 == 0 && x.stride * size % 16 == 0;
 }
 
@@ -45,10 +45,22 @@ struct Product {
 
 // out[M][N] = q p^T, with q [M][K], or transposed [K][M], and p [N][K] or [K][N].
 //
-// A tile's rate is that of 256 workgroups of its kind at work; the last round of them is as long as
-// a full one, and parts of k fill the GPU where tiles do not, for one more pass over the results.
-// (Rates measured at 16000 x 2048 x 1024 in bf16 and 1024 x 12544 x 1024 in binary32.)
-void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq, int32_t dtype) {
+// What a cut takes is estimated from what its kind of tile took here, in us: a step of k where the CUs are
+// full (8192^3 in bf16: 256 x 256 results 875 us, 128 x 128 1045, 64 x 64 1590; 4096^3 in binary32: 128 x 128
+// 1000 us) and of a workgroup that is alone on its CU, and what precedes and follows the steps (half of
+// it is hidden behind the products of other workgroups of the CU, which 256 x 256 has none of).  Tiles
+// that would start another round on the GPU's 256 CUs are cut along k until they fill it, or all are; the
+// parts are written and read again at some 6 TB/s, and joined by a launch more.
+struct TileCost {
+    int kind, bm, bn;
+    double step, alone, around;
+};
+const TileCost kTilesBf16[] = {{kTileLarge, 256, 256, 1.71, 1.71, 12.0}, {kTileMiddle, 128, 128, 0.51, 0.85, 3.0},
+                               {kTileSmall, 64, 64, 0.20, 0.45, 1.0}};
+const TileCost kTilesF32[] = {{kTileMiddle, 128, 128, 1.95, 2.3, 4.0}, {kTileSmall, 64, 64, 0.51, 0.8, 1.0}};
+constexpr int64_t kCus = 256;
+
+void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq, int32_t dtype, bool smooth) {
     const int64_t size = dtype_size(dtype), step = 128 / size;
     g = Product{};
     GemmArgs &a = g.a;
@@ -59,47 +71,59 @@ void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq
     a.N = static_cast<int32_t>(tp ? p.cols : p.rows);
     a.M = static_cast<int32_t>(tq ? q.cols : q.rows);
     a.K = static_cast<int32_t>(tp ? p.rows : p.cols);
-    a.ldo = a.N;
     a.split = 1;
     g.tp = tp;
     g.tq = tq;
-    g.plan.whole = whole(p, size) && whole(q, size);
+    g.plan.chunks = chunks(p, size) && chunks(q, size);
     const int64_t M = a.M, N = a.N, K = a.K;
-    if (!tp && !tq && M <= kSkinnyRows && g.plan.whole && K % 8 == 0) {
+    if (!tp && !tq && M <= kSkinnyRows && g.plan.chunks && K % 8 == 0) {
         g.skinny = true;
         const int64_t groups = (N + 15) / 16, steps = (K + 31) / 32;
         a.split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(128 / groups, steps / 64)));
         a.steps = static_cast<int32_t>((steps + a.split - 1) / a.split);
         a.split = static_cast<int32_t>((steps + a.steps - 1) / a.steps);
-    } else {
-        struct Tile { int kind, bm, bn; double us; };       // us: of one step of k
-        static const Tile kBf16[] = {{kTileLarge, 256, 256, 2.2}, {kTileMiddle, 128, 128, 0.7}, {kTileSmall, 64, 64, 0.3}};
-        static const Tile kF32[] = {{kTileMiddle, 128, 128, 2.0}, {kTileSmall, 64, 64, 0.55}};
-        const bool bf16 = dtype == RE_DTYPE_BF16;
-        const Tile *all = bf16 ? kBf16 : kF32;
-        const int count = bf16 ? 3 : 2;
-        const int64_t steps = std::max<int64_t>(1, (K + step - 1) / step);
-        double best = 0;
-        for (int i = g.plan.whole ? 0 : count - 1; i < count; ++i) {
-            const int64_t tm = (M + all[i].bm - 1) / all[i].bm, tn = (N + all[i].bn - 1) / all[i].bn;
-            for (int64_t split = 1; split <= 64 && (split == 1 || (steps / split >= 4 && tm * tn * split <= 1024)); ++split) {
+        g.bytes = a.split > 1 ? align256(static_cast<size_t>(a.split) * M * N * 4) : 0;
+        return;
+    }
+    const bool bf16 = dtype == RE_DTYPE_BF16;
+    const TileCost *all = bf16 ? kTilesBf16 : kTilesF32;
+    const int count = bf16 ? 3 : 2;
+    const int64_t steps = (K + step - 1) / step;
+    double best = -1;
+    for (int i = g.plan.chunks ? 0 : count - 1; i < count; ++i) {
+        const TileCost &t = all[i];
+        const int64_t tm = (M + t.bm - 1) / t.bm, tn = (N + t.bn - 1) / t.bn, tiles = tm * tn;
+        if (tiles > (int64_t(1) << 28) && i + 1 < (g.plan.chunks ? count : 0)) continue;
+        // us of n workgroups of k steps each
+        const auto run = [&](int64_t n, int64_t k) {
+            const double rounds = double((n + kCus - 1) / kCus);
+            return double(k) * std::max(n > 0 ? t.alone : 0.0, rounds * t.step) + rounds * t.around * (smooth ? 1.8 : 1.0);
+        };
+        for (int some = 0; some < 2; ++some) {       // parts of all tiles, or of those past full rounds
+            const int64_t whole = some ? tiles / kCus * kCus : 0, parted = tiles - whole;
+            if (some && (whole == 0 || parted == 0)) continue;
+            for (int64_t split = 1; split <= 64; ++split) {
+                if (split > 1 && (steps / split < 4 || parted * split > 8 * kCus)) break;
                 const int64_t each = (steps + split - 1) / split;
-                if (split > 1 && (steps + each - 1) / each != split) continue;
-                const double rounds = double((tm * tn * split + 255) / 256);
-                const double us = rounds * (double(each) * all[i].us + 2.0) +
-                                  (split > 1 ? 4.0 + 8e-6 * double(split) * double(M) * double(N) / 4.0 : 0.0);
-                if (best == 0 || us < best) {
-                    best = us;
-                    g.plan.tile = all[i].kind;
-                    a.tiles_m = static_cast<int32_t>(tm);
-                    a.tiles_n = static_cast<int32_t>(tn);
-                    a.split = static_cast<int32_t>(split);
-                    a.steps = static_cast<int32_t>(each);
-                }
+                if ((steps + each - 1) / each != split || (some && split == 1)) continue;
+                double us = run(whole, steps) + run(parted * split, each);
+                if (split > 1) us += 3.0 + 8e-6 / 6.0 * double(split * parted) * t.bm * t.bn;
+                if (best >= 0 && us >= best) continue;
+                best = us;
+                g.plan.tile = t.kind;
+                g.plan.bm = t.bm;
+                g.plan.bn = t.bn;
+                a.tiles_m = static_cast<int32_t>(tm);
+                a.tiles_n = static_cast<int32_t>(tn);
+                a.whole = static_cast<int32_t>(split == 1 ? tiles : whole);
+                a.parted = static_cast<int32_t>(split == 1 ? 0 : parted);
+                a.split = static_cast<int32_t>(split);
+                a.steps = static_cast<int32_t>(each);
             }
         }
     }
-    g.bytes = a.split > 1 ? align256(static_cast<size_t>(a.split) * M * N * 4) : 0;
+    a.grid_whole = (a.whole + 7) / 8 * 8;
+    g.bytes = align256(static_cast<size_t>(a.split) * a.parted * g.plan.bm * g.plan.bn * 4);
 }
 
 re_status_t run_product(Product &g, void *out, void *ws, int32_t dtype, hipStream_t s) {
@@ -107,13 +131,13 @@ re_status_t run_product(Product &g, void *out, void *ws, int32_t dtype, hipStrea
     a.out = out;
     a.part = static_cast<float *>(ws);
     const int64_t size = dtype_size(dtype);
-    a.vec = a.N % 4 == 0 && a.ldo % 4 == 0 && aligned(out, 4 * size) &&
+    a.vec = a.N % 4 == 0 && aligned(out, 4 * size) &&
             (!a.residual || (a.ldr % 4 == 0 && aligned(a.residual, 4 * size))) && aligned(a.slope, 4 * size);
     hipError_t e;
     if (g.skinny) e = launch_skinny(a, dtype, s);
     else if (dtype == RE_DTYPE_BF16) e = launch_gemm_bf16(a, g.plan, g.tp, g.tq, s);
     else e = launch_gemm_f32(a, g.plan, g.tp, g.tq, s);
-    if (e == hipSuccess && a.split > 1) e = launch_gemm_join(a, dtype, s);
+    if (e == hipSuccess && a.split > 1) e = g.skinny ? launch_skinny_join(a, dtype, s) : launch_gemm_join(a, g.plan, dtype, s);
     return from_hip(e);
 }
 
@@ -167,8 +191,8 @@ void plan_backward(const linear_act_t *d, const void *grad_y, Backward &b) {
     const Matrix w = matrix(d->weight, d->outs, d->ins, d->weight_stride);
     const Matrix x = matrix(d->x, d->rows, d->ins, d->x_stride);
     if (d->rows > 0) {
-        plan_product(b.x, w, true, g, false, d->dtype);
-        plan_product(b.weight, x, true, g, true, d->dtype);
+        plan_product(b.x, w, true, g, false, d->dtype, false);
+        plan_product(b.weight, x, true, g, true, d->dtype, false);
     }
     b.g_bytes = d->act == RE_ACT_NONE ? 0 : align256(static_cast<size_t>(d->rows) * d->outs * size);
     b.part_bytes = d->bias ? align256(static_cast<size_t>(b.slope.blocks) * d->outs * 4) : 0;
@@ -225,7 +249,7 @@ re_status_t linear_act_workspace_size(const linear_act_t *d, int32_t backward, s
         if (d->rows > 0) {
             Product g;
             plan_product(g, matrix(d->weight, d->outs, d->ins, d->weight_stride), false,
-                         matrix(d->x, d->rows, d->ins, d->x_stride), false, d->dtype);
+                         matrix(d->x, d->rows, d->ins, d->x_stride), false, d->dtype, d->act >= RE_ACT_GELU);
             *bytes = g.bytes;
         }
     }
@@ -243,7 +267,7 @@ re_status_t linear_act_fwd(const linear_act_t *d, void *y, void *slope, void *wo
     if (!y) return RE_ERR_INVALID_ARG;
     Product g;
     plan_product(g, matrix(d->weight, d->outs, d->ins, d->weight_stride), false,
-                 matrix(d->x, d->rows, d->ins, d->x_stride), false, d->dtype);
+                 matrix(d->x, d->rows, d->ins, d->x_stride), false, d->dtype, d->act >= RE_ACT_GELU);
     if ((st = check_workspace(workspace, workspace_bytes, g.bytes)) != RE_OK) return st;
     g.a.bias = d->bias;
     g.a.bias_bf16 = d->bias_dtype == RE_DTYPE_BF16;

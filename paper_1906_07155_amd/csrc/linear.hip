@@ -57,8 +57,13 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(GemmArgs a) {
     for (int w = 1; w < kSkinnyWaves; ++w) x += sums[w][wave][lane];
     const int m = 16 * wave + n, to = n0 + 4 * g;
     if (m >= a.M || to >= a.N) return;
-    if (a.split > 1) store_part(a, part, m, to, x);
-    else finish4<T>(a, m, to, x);
+    const int64_t at = static_cast<int64_t>(m) * a.N + to;
+    if (a.split > 1) {
+        float *sums = a.part + static_cast<int64_t>(part) * a.M * a.N + at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (to + i < a.N) as_global_mut<float>(sums)[i] = x[i];
+    } else finish4<T>(a, a.N - to, at, m * a.ldr + to, x + load_bias(a, to));
 }
 
 template <typename T>
@@ -79,32 +84,46 @@ hipError_t launch_skinny(const GemmArgs &a, int dtype, hipStream_t s) {
 // Parts of k
 // ---------------------------------------------------------------------------
 
+// A thread for four adjacent results of a tile that was made in parts.
 template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(GemmArgs a) {
-    const int quads = (a.N + 3) / 4;
-    const int64_t at = blockIdx.x * int64_t(256) + threadIdx.x;
-    const int m = static_cast<int>(at / quads), n = static_cast<int>(at % quads) * 4;
-    if (m >= a.M) return;
-    const int64_t size = static_cast<int64_t>(a.M) * a.N;
-    const float *from = a.part + static_cast<int64_t>(m) * a.N + n;
+__global__ __launch_bounds__(256) void join_kernel(GemmArgs a, int bm, int bn) {
+    const int quads = bm * bn / 4, tile = blockIdx.x / (quads / 256), at = blockIdx.x % (quads / 256) * 256 + threadIdx.x;
+    int id = a.whole + tile;
+    const int band = id / (8 * a.tiles_n), rows_of = min(8, a.tiles_m - 8 * band);
+    id -= band * 8 * a.tiles_n;
+    const int m = (8 * band + id % rows_of) * bm + at / (bn / 4), n = id / rows_of * bn + at % (bn / 4) * 4;
+    if (m >= a.M || n >= a.N) return;
+    const f32x4 *from = reinterpret_cast<const f32x4 *>(a.part) + static_cast<int64_t>(tile) * quads + at;
     f32x4 x = {};
-    if (a.N % 4 == 0) {
-#pragma unroll 4
-        for (int i = 0; i < a.split; ++i) x += *(const REX_GLOBAL f32x4 *)(from + i * size);
-    } else {
-        for (int i = 0; i < a.split; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < a.N) x[e] += as_global<float>(from + i * size)[e];
-    }
-    finish4<T>(a, m, n, x);
+#pragma unroll 8
+    for (int i = 0; i < a.split; ++i) x += as_global<f32x4>(from)[static_cast<int64_t>(i) * a.parted * quads];
+    finish4<T>(a, a.N - n, static_cast<int64_t>(m) * a.N + n, m * a.ldr + n, x + load_bias(a, n));
 }
 
-hipError_t launch_gemm_join(const GemmArgs &a, int dtype, hipStream_t s) {
-    const int64_t threads = static_cast<int64_t>(a.M) * ((a.N + 3) / 4);
-    const uint32_t grid = static_cast<uint32_t>((threads + 255) / 256);
-    if (dtype == kBF16) join_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
-    else join_kernel<float><<<grid, 256, 0, s>>>(a);
+hipError_t launch_gemm_join(const GemmArgs &a, const GemmPlan &p, int dtype, hipStream_t s) {
+    const uint32_t grid = static_cast<uint32_t>(a.parted) * (p.bm * p.bn / 1024);
+    if (dtype == kBF16) join_kernel<uint16_t><<<grid, 256, 0, s>>>(a, p.bm, p.bn);
+    else join_kernel<float><<<grid, 256, 0, s>>>(a, p.bm, p.bn);
+    return hipGetLastError();
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void skinny_join_kernel(GemmArgs a) {
+    const int quads = (a.N + 3) / 4, at = blockIdx.x * 256 + threadIdx.x, m = at / quads, n = at % quads * 4;
+    if (m >= a.M) return;
+    const int64_t size = static_cast<int64_t>(a.M) * a.N, to = static_cast<int64_t>(m) * a.N + n;
+    f32x4 x = {};
+    for (int i = 0; i < a.split; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < a.N) x[e] += as_global<float>(a.part)[i * size + to + e];
+    finish4<T>(a, a.N - n, to, m * a.ldr + n, x + load_bias(a, n));
+}
+
+hipError_t launch_skinny_join(const GemmArgs &a, int dtype, hipStream_t s) {
+    const uint32_t grid = (static_cast<uint32_t>(a.M) * ((a.N + 3) / 4) + 255) / 256;
+    if (dtype == kBF16) skinny_join_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
+    else skinny_join_kernel<float><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -13,12 +13,13 @@ enum : int { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
 struct GemmArgs {
     const void *p, *q;
     int64_t ldp, ldq;               // bytes from row to row, or from k to k
-    void *out;                      // [M][N], ldo elements from row to row
-    int64_t ldo;
+    void *out;                      // [M][N] dense
     int32_t M, N, K;
-    int32_t tiles_m, tiles_n;
-    int32_t split, steps;           // parts of k, and the steps of each
-    float *part;                    // split > 1: [split][M][N]
+    int32_t tiles_m, tiles_n;       // tiles, of which the first `whole` are made by one workgroup each
+    int32_t whole, grid_whole;      // (rounded up to a multiple of 8 for them)
+    int32_t parted;                 // the others in `split` parts of k, of `steps` steps each
+    int32_t split, steps;
+    float *part;                    // [split][parted][rows and columns of a tile]; few rows: [split][M][N]
     // epilogue
     const void *bias;               // [N] or null
     const void *residual;           // [M][N], ldr elements from row to row, or null
@@ -32,13 +33,13 @@ struct GemmArgs {
 enum : int { kTileLarge = 0, kTileMiddle = 1, kTileSmall = 2 };
 struct GemmPlan {
     int tile, bm, bn;               // a workgroup's rows and columns
-    int split, steps;
-    bool whole;                     // operands can be read 16 bytes at a time
+    bool chunks;                    // operands can be read 16 bytes at a time
 };
 
 hipError_t launch_gemm_bf16(const GemmArgs &a, const GemmPlan &p, bool tp, bool tq, hipStream_t s);
 hipError_t launch_gemm_f32(const GemmArgs &a, const GemmPlan &p, bool tp, bool tq, hipStream_t s);
-hipError_t launch_gemm_join(const GemmArgs &a, int dtype, hipStream_t s);
+hipError_t launch_gemm_join(const GemmArgs &a, const GemmPlan &p, int dtype, hipStream_t s);
+hipError_t launch_skinny_join(const GemmArgs &a, int dtype, hipStream_t s);
 // A few rows against [N][K]: the weights go from memory straight to the products.
 constexpr int kSkinnyRows = 64;
 hipError_t launch_skinny(const GemmArgs &a, int dtype, hipStream_t s);
@@ -80,28 +81,31 @@ __device__ __forceinline__ float erfc_over_exp(float z) {
     return t * fmaf(r, t, 0.25388532876968384f);
 }
 
-// act(x) and its slope at x.
+// act(x), and its slope at x where SLOPE, of four.
 template <bool SLOPE>
-__device__ __forceinline__ float activate(int act, float x, float &slope) {
-    switch (act) {
-    case kActRelu:                      // NaN stays, and lets the gradient through
-        slope = x <= 0.0f ? 0.0f : 1.0f;
-        return x <= 0.0f ? 0.0f : x;
-    case kActGelu: {                    // x Phi(x), Phi + x phi(x)
-        const float e = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
-        const float tail = 0.5f * e * erfc_over_exp(fabsf(x) * 0.70710678118654752f);
-        const float phi = x < 0.0f ? tail : 1.0f - tail;
-        if (SLOPE) slope = fmaf(x * 0.39894228040143268f, e, phi);
-        return x * phi;
-    }
-    case kActSilu: {                    // x s, s (1 + x (1 - s))
-        const float e = __builtin_amdgcn_exp2f(-kLog2e * x), s = 1.0f / (1.0f + e);
-        if (SLOPE) slope = s * fmaf(x, 1.0f - s, 1.0f);
-        return x * s;
-    }
-    default:
-        slope = 1.0f;
-        return x;
+__device__ __forceinline__ void activate(int act, f32x4 &x, float (&slope)[4]) {
+    if (act == kActRelu) {                      // NaN stays, and lets the gradient through
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            slope[i] = x[i] <= 0.0f ? 0.0f : 1.0f;
+            x[i] = x[i] <= 0.0f ? 0.0f : x[i];
+        }
+    } else if (act == kActGelu) {               // x Phi(x), Phi + x phi(x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f(x[i] * x[i] * (-0.5f * kLog2e));
+            const float tail = 0.5f * e * erfc_over_exp(fabsf(x[i]) * 0.70710678118654752f);
+            const float phi = x[i] < 0.0f ? tail : 1.0f - tail;
+            if (SLOPE) slope[i] = fmaf(x[i] * 0.39894228040143268f, e, phi);
+            x[i] *= phi;
+        }
+    } else if (act == kActSilu) {               // x s, s (1 + x (1 - s))
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x[i]));
+            if (SLOPE) slope[i] = s * fmaf(x[i], 1.0f - s, 1.0f);
+            x[i] *= s;
+        }
     }
 }
 
@@ -135,8 +139,8 @@ template <> struct Slope<uint16_t> {
         L l;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int c = min(max(static_cast<int>(rintf(fmaf(x[i], 0x1p23f, 0x1p21f))), 0), 0xfffffe);
-            const uint32_t u = x[i] != x[i] ? 0xffffffu : static_cast<uint32_t>(c);
+            const uint32_t c = static_cast<uint32_t>(fmaf(x[i], 0x1p23f, 0x1p21f + 0.5f));
+            const uint32_t u = x[i] != x[i] ? 0xffffffu : c;
             h[i] = static_cast<uint16_t>(u >> 8);
             l[i] = static_cast<uint8_t>(u);
         }
@@ -166,56 +170,41 @@ template <> __device__ __forceinline__ void load4<uint16_t>(const void *p, int64
     for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
 }
 
-__device__ __forceinline__ float load_bias(const GemmArgs &a, int n) {
-    return a.bias_bf16 ? bf16_to_f32(as_global<uint16_t>(a.bias)[n]) : as_global<float>(a.bias)[n];
+// The biases of columns n .. n + 3 (0 where there is none).
+__device__ __forceinline__ f32x4 load_bias(const GemmArgs &a, int n) {
+    f32x4 x = {};
+    if (!a.bias) return x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int at = min(n + i, a.N - 1);
+        x[i] = a.bias_bf16 ? bf16_to_f32(as_global<uint16_t>(a.bias)[at]) : as_global<float>(a.bias)[at];
+    }
+    return x;
 }
 
-// Four adjacent results of row m from column n on (n < N): bias, activation, residual, stores.
+// Four adjacent results (`left` of them, if there are fewer) at element `at` of the dense results,
+// whose sums are x: activation, residual (at element `rat`), stores.
 template <typename T>
-__device__ __forceinline__ void finish4(const GemmArgs &a, int m, int n, f32x4 x) {
-    const int64_t at = static_cast<int64_t>(m) * a.ldo + n, dense = static_cast<int64_t>(m) * a.N + n;
-    const int64_t rat = static_cast<int64_t>(m) * a.ldr + n;
-    float y[4], s[4], r[4] = {};
-    const int left = a.N - n;
-    if (a.bias) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < left) x[i] += load_bias(a, n + i);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = x[i];
-    if (a.act != kActNone) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = activate<true>(a.act, x[i], s[i]);
-    }
+__device__ __forceinline__ void finish4(const GemmArgs &a, int left, int64_t at, int64_t rat, f32x4 x) {
+    float s[4], r[4] = {};
     if (a.vec) {                        // (then N is a multiple of 4)
+        if (a.residual) load4<T>(a.residual, rat, r);
+        if (a.act != kActNone) activate<true>(a.act, x, s);
         if (a.residual) {
-            load4<T>(a.residual, rat, r);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += r[i];
+            for (int i = 0; i < 4; ++i) x[i] += r[i];
         }
-        Num<T>::store4(reinterpret_cast<char *>(static_cast<T *>(a.out) + at), f32x4{y[0], y[1], y[2], y[3]});
-        if (a.slope) Slope<T>::template store<4>(a.slope, static_cast<int64_t>(a.M) * a.N, dense, s);
+        Num<T>::store4(reinterpret_cast<char *>(static_cast<T *>(a.out) + at), x);
+        if (a.slope) Slope<T>::template store<4>(a.slope, static_cast<int64_t>(a.M) * a.N, at, s);
         return;
     }
+    if (a.act != kActNone) activate<true>(a.act, x, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (i >= left) break;
-        if (a.residual) y[i] += load_f32<T>(as_global<T>(a.residual) + rat + i);
-        store_f32<T>(as_global_mut<T>(a.out) + at + i, y[i]);
-        if (a.slope) Slope<T>::template store<1>(a.slope, static_cast<int64_t>(a.M) * a.N, dense + i, s + i);
-    }
-}
-
-// Four adjacent sums of one part of k.
-__device__ __forceinline__ void store_part(const GemmArgs &a, int part, int m, int n, f32x4 x) {
-    float *to = a.part + (static_cast<int64_t>(part) * a.M + m) * a.N + n;
-    if (a.N % 4 == 0) {
-        *(REX_GLOBAL f32x4 *)(to) = x;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < a.N) as_global_mut<float>(to)[i] = x[i];
+        if (a.residual) x[i] += load_f32<T>(as_global<T>(a.residual) + rat + i);
+        store_f32<T>(as_global_mut<T>(a.out) + at + i, x[i]);
+        if (a.slope) Slope<T>::template store<1>(a.slope, static_cast<int64_t>(a.M) * a.N, at + i, s + i);
     }
 }
 
