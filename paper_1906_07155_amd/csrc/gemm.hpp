@@ -34,16 +34,16 @@ namespace rex {
 template <typename T> struct Shape;
 template <> struct Shape<uint16_t> {
     using Frag = bf16x8;
-    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+    static constexpr int kParts = 1;
+    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c, int) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
 };
 template <> struct Shape<float> {
     using Frag = f32x4;
-    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
-        return c;
+    static constexpr int kParts = 4;         // of an operand's registers, one product each
+    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c, int part) {
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(a[part], b[part], c, 0, 0, 0);
     }
 };
 
@@ -232,9 +232,11 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int e = 0; e < Shape<T>::kParts; ++e)      // (no product needs the one before it)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = Shape<T>::mma(pf[s][j], qf[s][i], acc[i][j]);
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = Shape<T>::mma(pf[s][j], qf[s][i], acc[i][j], e);
     }
     // (the compiler leaves out the wait states between products and a use behind a branch)
     asm volatile("s_nop 15" ::: "memory");

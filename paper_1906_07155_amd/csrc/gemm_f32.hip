@@ -6,7 +6,7 @@ namespace rex {
 template <bool TP, bool TQ>
 static hipError_t run(const GemmArgs &a, const GemmPlan &p, hipStream_t s) {
     if (!p.chunks) return run_gemm<float, TP, TQ, 2, 2, 2, 2, false, 2>(a, s);
-    if (p.tile == kTileMiddle) return run_gemm<float, TP, TQ, 4, 4, 2, 2, true, 2>(a, s);
+    if (p.tile == kTileMiddle) return run_gemm<float, TP, TQ, 4, 2, 2, 2, true, 3>(a, s);
     return run_gemm<float, TP, TQ, 2, 2, 2, 2, true, 2>(a, s);
 }
 

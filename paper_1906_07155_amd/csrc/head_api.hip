@@ -46,8 +46,8 @@ struct Product {
 // out[M][N] = q p^T, with q [M][K], or transposed [K][M], and p [N][K] or [K][N].
 //
 // What a cut takes is estimated from what its kind of tile took here, in us: a step of k where the CUs are
-// full (8192^3 in bf16: 256 x 256 results 875 us, 128 x 128 1045, 64 x 64 1590; 4096^3 in binary32: 128 x 128
-// 1000 us) and of a workgroup that is alone on its CU, and what precedes and follows the steps (half of
+// full (8192^3 in bf16: 256 x 256 results 875 us, 128 x 128 1045, 64 x 64 1590; 4096^3 in binary32: 128 x 64
+// 1020 us, 64 x 64 1040) and of a workgroup that is alone on its CU, and what precedes and follows the steps (half of
 // it is hidden behind the products of other workgroups of the CU, which 256 x 256 has none of).  Tiles
 // that would start another round on the GPU's 256 CUs are cut along k until they fill it, or all are; the
 // parts are written and read again at some 6 TB/s, and joined by a launch more.
@@ -57,7 +57,7 @@ struct TileCost {
 };
 const TileCost kTilesBf16[] = {{kTileLarge, 256, 256, 1.71, 1.71, 12.0}, {kTileMiddle, 128, 128, 0.51, 0.85, 3.0},
                                {kTileSmall, 64, 64, 0.20, 0.45, 1.0}};
-const TileCost kTilesF32[] = {{kTileMiddle, 128, 128, 1.95, 2.3, 4.0}, {kTileSmall, 64, 64, 0.51, 0.8, 1.0}};
+const TileCost kTilesF32[] = {{kTileMiddle, 128, 64, 0.98, 1.4, 2.0}, {kTileSmall, 64, 64, 0.51, 0.8, 1.0}};
 constexpr int64_t kCus = 256;
 
 void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq, int32_t dtype, bool smooth) {
