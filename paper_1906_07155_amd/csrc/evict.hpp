@@ -21,9 +21,11 @@ struct EvictArgs {
     int32_t Hkv, D, B, max_pages;
     const int32_t *pages, *lengths, *keep;
     const float *weight;
-    int32_t *lengths_out, *origin;  // origin may be null
+    int32_t *lengths_out;
     float *weight_out;
-    int32_t *freed, *to;            // [B][places]: free places in order; where a place's box goes, or -1
+    int32_t *from;                  // [B][places]: the place that a place's box was in, or -1
+    int32_t *source;                // [B][places]: the page of that place, where a box moves, else -1
+    int32_t *freed, *late;          // [B][places]: of long streams, free places and the boxes that fill them
 };
 hipError_t launch_evict(const EvictArgs &e, hipStream_t s);
 

@@ -652,7 +652,7 @@ re_status_t box_memory_evict_workspace_size(const box_memory_t *m, const box_evi
     EvictArgs e;
     const re_status_t st = evict_args(m, d, &e);
     if (st != RE_OK) return st;
-    *bytes = 2 * evict_part_bytes(e);
+    *bytes = 4 * evict_part_bytes(e);
     return RE_OK;
 }
 
@@ -666,12 +666,14 @@ re_status_t box_memory_evict(const box_memory_t *m, const box_evict_t *d, int32_
     if (e.B == 0) return RE_OK;
     if (!lengths_out || (e.max_pages > 0 && !weight_out)) return RE_ERR_INVALID_ARG;
     if (weight_out && weight_out == d->weight) return RE_ERR_INVALID_ARG;
-    if ((st = check_workspace(workspace, workspace_bytes, 2 * evict_part_bytes(e))) != RE_OK) return st;
+    if ((st = check_workspace(workspace, workspace_bytes, 4 * evict_part_bytes(e))) != RE_OK) return st;
     e.lengths_out = lengths_out;
     e.weight_out = weight_out;
-    e.origin = origin;
-    e.freed = static_cast<int32_t *>(workspace);
-    e.to = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + evict_part_bytes(e));
+    char *ws = static_cast<char *>(workspace);
+    e.freed = reinterpret_cast<int32_t *>(ws);
+    e.late = reinterpret_cast<int32_t *>(ws + evict_part_bytes(e));
+    e.source = reinterpret_cast<int32_t *>(ws + 2 * evict_part_bytes(e));
+    e.from = origin ? origin : reinterpret_cast<int32_t *>(ws + 3 * evict_part_bytes(e));
     return from_hip(launch_evict(e, static_cast<hipStream_t>(stream)));
 }
 
