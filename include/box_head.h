@@ -79,7 +79,7 @@ re_status_t linear_act_bwd(const linear_act_t *a, const void *grad_y, const void
  * +inf make their row's lse, logp and entropy NaN; among the top classes NaN comes first.  A row all of
  * whose logits are at -1e9 has the probabilities that it has with all of them at 0. */
 #define RE_LOGPROB_MAX_CLASSES (1 << 24)
-#define RE_LOGPROB_MAX_ROWS (1 << 23)     /* divided by a row's parts, of 4096 classes each (RE_ERR_UNSUPPORTED) */
+#define RE_LOGPROB_MAX_ROWS (1 << 23)     /* divided by a row's parts, of 4088 classes each (RE_ERR_UNSUPPORTED) */
 #define RE_LOGPROB_MAX_TOP 16
 typedef struct {
     const void *logits;       /* [rows][classes], row stride stride (elements) */

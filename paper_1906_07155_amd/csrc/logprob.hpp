@@ -26,8 +26,9 @@ struct LogprobArgs {
     void *grad;
 };
 
-// Classes that one workgroup holds in registers: longer rows come in parts.
-constexpr int kLogprobSpan = 4096;
+// What a workgroup holds in registers, and the classes of a part of a longer row: a chunk of 16 bytes
+// fewer, since a row may begin inside one.
+constexpr int kLogprobRegisters = 4096, kLogprobSpan = kLogprobRegisters - 8;
 hipError_t launch_logprob_fwd(const LogprobArgs &a, int dtype, hipStream_t s);
 hipError_t launch_logprob_bwd(const LogprobArgs &a, int dtype, hipStream_t s);
 

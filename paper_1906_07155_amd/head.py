@@ -38,7 +38,7 @@ SIGNATURES = {
 _LINEAR = struct.Struct("@4P6q3i4x")
 _LOGPROB = struct.Struct("@2P3q2if4x")
 MAX_TOP = 16                        # RE_LOGPROB_MAX_TOP
-LOGPROB_SPAN = 4096                 # rows of more classes come in parts, which need a workspace
+LOGPROB_SPAN = 4088                 # rows of more classes come in parts, which need a workspace
 
 _lib = None
 
