@@ -62,7 +62,7 @@ struct Side {
     uint32_t off[kLoads];
     int k[kLoads], e[WHOLE ? 1 : kLoads];
     int left_k, left_rows;
-    u32x4 held[WHOLE ? 1 : kLoads];
+    u32x4 held[2][WHOLE ? 1 : kLoads];        // of this step and the next
 
     // What spreads a line's chunks over the banks for the lanes that read together: eight lanes with a
     // chunk of eight rows each (k adjacent); 32 lanes with 32 bytes of eight lines (transposed bf16: lines
@@ -86,15 +86,15 @@ struct Side {
             off[i] = static_cast<uint32_t>(line * ld) + chunk * 16;
             k[i] = TR ? line : chunk * kChunk;
             const int row = TR ? chunk * kChunk : line;
-            if (row >= left_rows) off[i] = kBufOOB;
+            if (WHOLE && row >= left_rows) off[i] = kBufOOB;
             if (!WHOLE) e[i] = row;
         }
     }
 
-    // the next step's tile on its way to `to` (WHOLE), or to registers
-    __device__ __forceinline__ void load(char *to, int wave) {
-        const auto r = make_rsrc(origin, kBufMaxBytes - 1);
+    // the next tile on its way to `to` (WHOLE), or to registers
+    __device__ __forceinline__ void load(char *to, int wave, int which = 0) {
         if constexpr (WHOLE) {
+            const auto r = make_rsrc(origin, kBufMaxBytes - 1);
             const bool all = left_k >= kStep;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
@@ -102,29 +102,34 @@ struct Side {
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                uint32_t x[kChunk];
+                // a chunk at any address where all of it is there, else its elements
+                const int there = TR ? left_rows - e[i] : left_k - k[i];
+                const bool line = TR ? k[i] < left_k : e[i] < left_rows;
+                held[which][i] = u32x4{};
+                if (line && there >= kChunk) {
+                    using Any = uint32_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+                    held[which][i] = *(const REX_GLOBAL Any *)(origin + off[i]);
+                } else if (line && there > 0) {
+                    using Bits = std::conditional_t<kSize == 2, uint16_t, uint32_t>;
+                    uint32_t x[kChunk];
 #pragma unroll
-                for (int c = 0; c < kChunk; ++c) {
-                    const bool in = (TR ? k[i] : k[i] + c) < left_k && (TR ? e[i] + c : e[i]) < left_rows;
-                    const uint32_t at = in ? off[i] + c * kSize : kBufOOB;
-                    if constexpr (kSize == 2) x[c] = __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
-                    else x[c] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
-                }
+                    for (int c = 0; c < kChunk; ++c) x[c] = c < there ? as_global<Bits>(origin + off[i])[c] : Bits(0);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if constexpr (kSize == 2) held[i][c] = x[2 * c] | x[2 * c + 1] << 16;
-                    else held[i][c] = x[c];
+                    for (int c = 0; c < 4; ++c) {
+                        if constexpr (kSize == 2) held[which][i][c] = x[2 * c] | x[2 * c + 1] << 16;
+                        else held[which][i][c] = x[c];
+                    }
                 }
             }
         }
         origin += step_bytes;
         left_k -= kStep;
     }
-    __device__ __forceinline__ void put(char *to, int wave, int lane) const {
+    __device__ __forceinline__ void put(char *to, int wave, int lane, int which) const {
         if constexpr (!WHOLE) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                *reinterpret_cast<u32x4 *>(to + ((i * WAVES + wave) * 64 + lane) * 16) = held[i];
+                *reinterpret_cast<u32x4 *>(to + ((i * WAVES + wave) * 64 + lane) * 16) = held[which][i];
         }
     }
 
@@ -207,12 +212,19 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
     f32x4 acc[MT][NT] = {};
     p.load(smem[0], wave);
     q.load(smem[0] + P::kBytes, wave);
-    for (int step = 0; step < steps; ++step) {
-        char *now = smem[step & 1], *then = smem[step & 1 ^ 1];
-        p.put(now, wave, lane);
-        q.put(now + P::kBytes, wave, lane);
+    if (!WHOLE && steps > 1) {
+        p.load(nullptr, wave, 1);
+        q.load(nullptr, wave, 1);
+    }
+    // One step, of buffer `which`.  Operands that are not whole chunks come through registers, two steps
+    // ahead; the others straight to LDS, one step ahead.
+    const auto run = [&](int step, int which) {
+        char *now = smem[which], *then = smem[which ^ 1];
+        p.put(now, wave, lane, which);
+        q.put(now + P::kBytes, wave, lane, which);
         // what this wave loaded is there, and what it read of the other buffer is back
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (WHOLE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         // (all of a step's reads before the next step's loads: the compiler takes those for writes to
@@ -225,9 +237,9 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) qf[s][t] = qr.get(now + P::kBytes, t, s);
         }
-        if (step + 1 < steps) {
-            p.load(then, wave);
-            q.load(then + P::kBytes, wave);
+        if (step + (WHOLE ? 1 : 2) < steps) {
+            p.load(then, wave, which);
+            q.load(then + P::kBytes, wave, which);
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -237,6 +249,14 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int j = 0; j < NT; ++j) acc[i][j] = Shape<T>::mma(pf[s][j], qf[s][i], acc[i][j], e);
+    };
+    if constexpr (WHOLE) {
+        for (int step = 0; step < steps; ++step) run(step, step & 1);
+    } else {
+        for (int step = 0; step < steps; step += 2) {
+            run(step, 0);
+            if (step + 1 < steps) run(step + 1, 1);
+        }
     }
     // (the compiler leaves out the wait states between products and a use behind a branch)
     asm volatile("s_nop 15" ::: "memory");

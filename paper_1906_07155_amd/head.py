@@ -15,7 +15,7 @@ import struct
 from typing import List
 
 from . import binding
-from .binding import _dtype_code, _need_cuda, _torch, check
+from .binding import RE_ERR_WORKSPACE, _dtype_code, _need_cuda, _torch, check
 from .relation import _Call, _dense, _ptr, _same_device, _size
 
 HEADER = os.path.join(os.path.dirname(binding.HERE), "include", "box_head.h")
@@ -143,11 +143,13 @@ def linear_act_fwd(x, weight, bias=None, *, act: str = "none", residual=None, sa
                 saved = out
             else:
                 saved = slope = c.empty(*_slope(x, shape))
-        need = 0
-        if workspace is None:
+        ws, wsb, _keep = c.workspace(workspace, 0)
+        status = L.linear_act_fwd(d, out.data_ptr(), _ptr(slope), ws, wsb, c.stream)
+        if status == RE_ERR_WORKSPACE and workspace is None:       # (most calls need none: not asked first)
             need = _size(L.linear_act_workspace_size, "linear_act_workspace_size", d, 0)
-        ws, wsb, _keep = c.workspace(workspace, need)
-        check(L.linear_act_fwd(d, out.data_ptr(), _ptr(slope), ws, wsb, c.stream), "linear_act_fwd")
+            ws, wsb, _keep = c.workspace(None, need)
+            status = L.linear_act_fwd(d, out.data_ptr(), _ptr(slope), ws, wsb, c.stream)
+        check(status, "linear_act_fwd")
     return out, saved
 
 
