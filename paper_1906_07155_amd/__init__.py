@@ -22,7 +22,8 @@ __all__ = ["RoIExtractError", "box_nms", "box_nms_batched", "deform_roi_pool_bwd
            "box_memory", "box_memory_append", "box_memory_attn_fwd", "box_memory_read",
            "gated_norm_bwd", "gated_norm_fwd",
            "box_memory_evict", "box_memory_weigh", "class_logprob_bwd", "class_logprob_fwd", "linear_act_bwd", "linear_act_fwd", "linear_act_workspace_size",
-           "BoxMemory", "RelationHead", "box_attention", "gated_norm"]
+           "BoxMemory", "RelationHead", "box_attention", "gated_norm",
+           "BoxHead", "class_logprob", "linear_act"]
 
 
 def __getattr__(name):
@@ -32,4 +33,7 @@ def __getattr__(name):
     if name in ("BoxMemory", "RelationHead", "box_attention", "gated_norm"):
         from . import relation_head
         return getattr(relation_head, name)
+    if name in ("BoxHead", "class_logprob", "linear_act"):
+        from . import box_head
+        return getattr(box_head, name)
     raise AttributeError(name)

@@ -17,7 +17,12 @@ from typing import List, Optional, Sequence
 import torch
 from torch import nn
 
-from . import relation
+from . import evict, relation
+
+
+def linear_act(*args, **kw):
+    from .box_head import linear_act as fused           # (which needs `once` of this module)
+    return fused(*args, **kw)
 
 
 class _Final(torch.autograd.Function):
@@ -122,18 +127,27 @@ def gated_norm(x, branch=None, *, gate=None, post_weight=None, post_bias=None, p
 class BoxMemory:
     """The 8-bit memories of a head's layers, which share one table of pages.
 
-    Streams take pages of 32 boxes from one pool; a stream with `max_pages` pages gives its
-    oldest page back for a new one, so it remembers at least 32 * (max_pages - 1) boxes.  The
+    Streams take pages of 32 boxes from one pool.  With evict "oldest" a stream with `max_pages`
+    pages gives its oldest page back for a new one, so it remembers at least 32 * (max_pages - 1)
+    boxes.  With evict "weight" a full stream loses the boxes that have received the least attention
+    (`weight`: of all heads, rows and layers, of earlier frames `decay` times as much with every
+    frame), as many as are needed for the new ones.  The
     order of places means nothing to the attention.  The table is kept on the host and copied to
     the device when it has changed."""
 
     def __init__(self, num_pages: int, streams: int, max_pages: int, kv_heads: int, dim: int,
-                 layers: int = 1, device="cuda"):
+                 layers: int = 1, device="cuda", evict: str = "oldest", decay: float = 0.9):
         if not 2 <= max_pages <= num_pages:
             raise ValueError("max_pages must be in [2, num_pages] (got %d of %d)" % (max_pages, num_pages))
         if streams < 1 or layers < 1:
             raise ValueError("a memory has at least one stream and one layer")
+        if evict not in ("oldest", "weight"):
+            raise ValueError("evict must be 'oldest' or 'weight' (got %r)" % (evict,))
         self.layers = [relation.box_memory(num_pages, kv_heads, dim, device) for _ in range(layers)]
+        self.decay = decay
+        self.weight = None                              # [streams, places] where it decides what leaves
+        if evict == "weight":
+            self.weight = torch.zeros((streams, max_pages * relation.MEMORY_PAGE), dtype=torch.float32, device=device)
         self.max_pages, self.device = max_pages, device
         self.free = list(range(num_pages - 1, -1, -1))
         self.table: List[List[int]] = [[] for _ in range(streams)]
@@ -149,6 +163,8 @@ class BoxMemory:
                              % (most, len(self.table)))
         need = 0
         for pages, used, c in zip(self.table, self.used, counts):
+            if self.weight is not None:                 # room is made for what does not fit
+                used = min(used, page * self.max_pages - c)
             total = (used + c + page - 1) // page
             need += min(total, self.max_pages) - len(pages) if total > len(pages) else 0
         if need > len(self.free):
@@ -158,6 +174,8 @@ class BoxMemory:
         """Places for counts[s] new boxes of each stream: int64 slots of all of them, stream
         after stream.  Raises (and takes nothing) where the pool has too few pages."""
         self.check(counts)
+        if self.weight is not None:
+            self._make_room(counts)
         page = relation.MEMORY_PAGE
         free, table, used = list(self.free), [list(p) for p in self.table], list(self.used)
         slots: List[int] = []
@@ -169,17 +187,31 @@ class BoxMemory:
                         free.append(pages.pop(0))
                         used[s] -= page
                     pages.append(free.pop())
-                at = used[s] % page
+                at, into = used[s] % page, pages[used[s] // page]
                 n = min(c, page - at)
-                slots.extend(range(pages[-1] * page + at, pages[-1] * page + at + n))
+                slots.extend(range(into * page + at, into * page + at + n))
                 used[s] += n
                 c -= n
         made = torch.tensor(slots, dtype=torch.int64, device=self.device)
         self.free, self.table, self.used, self._device_table = free, table, used, None
         return made
 
+    def _make_room(self, counts: Sequence[int]) -> None:
+        """The boxes of least weight leave the streams that counts[s] new ones do not fit into."""
+        most = relation.MEMORY_PAGE * self.max_pages
+        keep = [min(used, most - c) for used, c in zip(self.used, counts)]
+        if keep == self.used:
+            return
+        pages, lengths = self.pages_and_lengths()
+        kept = torch.tensor(keep, dtype=torch.int32, device=self.device)
+        for held in self.layers:                        # one decision, made for each of them
+            _, weight, _ = evict.box_memory_evict(held, pages, lengths, self.weight, kept)
+        self.weight, self.used, self._device_table = weight, keep, None
+
     def forget(self, stream: int) -> None:
         """The stream's pages go back to the pool."""
+        if self.weight is not None:
+            self.weight[stream] = 0
         self.free.extend(self.table[stream])
         self.table[stream], self.used[stream] = [], 0
         self._device_table = None
@@ -198,8 +230,9 @@ class RelationLayer(nn.Module):
     branch is normalised, gated for its image from the mean over its boxes, added to the features,
     and normalised for what follows, in one kernel."""
 
-    def __init__(self, channels: int, heads: int, kv_heads: int, buckets: int, norm: str):
+    def __init__(self, channels: int, heads: int, kv_heads: int, buckets: int, norm: str, fused: bool = False):
         super().__init__()
+        self.fused = fused
         self.heads, self.kv_heads, self.dim = heads, kv_heads, channels // heads
         self.norm = norm
         self.qkv = nn.Linear(channels, (heads + 2 * kv_heads) * self.dim)
@@ -224,18 +257,23 @@ class RelationLayer(nn.Module):
                 p.grad = None if grad is None else grad.to(device)
         return self
 
+    def _dense(self, layer, x, act: str = "none"):
+        if self.fused:
+            return linear_act(x, layer.weight, layer.bias, act=act)
+        return torch.relu(layer(x)) if act == "relu" else layer(x)
+
     def forward(self, x, u, gate, boxes, lengths, recall, last: bool, pre_next):
         """x [images, boxes, channels] and u, x normalised -> (x, u) for the next layer."""
         B, n, c = x.shape
         split = [self.heads, self.kv_heads, self.kv_heads]
-        q, k, v = self.qkv(u).view(B, n, sum(split), self.dim).split(split, 2)
+        q, k, v = self._dense(self.qkv, u).view(B, n, sum(split), self.dim).split(split, 2)
         geo = dict(bias=self.bias, q_boxes=boxes, k_boxes=boxes, q_len=lengths, k_len=lengths)
         out = box_attention(q, k, v, **geo)[0] if recall is None else recall(q, k, v, geo)
-        branch = self.proj(out.reshape(B * n, c))
-        gate = torch.sigmoid(self.gate(gate)).float()
+        branch = self._dense(self.proj, out.reshape(B * n, c))
+        gate = torch.sigmoid(self._dense(self.gate, gate)).float()
         x, u = gated_norm(x.reshape(B * n, c), branch, gate=gate, post_weight=self.post[0],
                           pre_weight=self.pre[1], norm=self.norm)
-        branch = self.fc2(torch.relu(self.fc1(u)))
+        branch = self._dense(self.fc2, self._dense(self.fc1, u, "relu"))
         x, u = gated_norm(x, branch, gate=gate, post_weight=self.post[1], pre_weight=pre_next,
                           norm=self.norm, second=not last)
         return x.view(B, n, c), None if u is None else u.view(B, n, c)
@@ -243,24 +281,26 @@ class RelationLayer(nn.Module):
 
 class RelationHead(nn.Module):
     """Layers of relations among the boxes of an image.  channels / heads channels a head, a
-    multiple of 8; kv_heads heads share keys in equal groups; buckets a side of the bias table."""
+    multiple of 8; kv_heads heads share keys in equal groups; buckets a side of the bias table;
+    fused: the dense layers run in linear_act's kernels, in torch's otherwise."""
 
     def __init__(self, channels: int, heads: int, kv_heads: Optional[int] = None, layers: int = 2,
-                 buckets: int = 15, norm: str = "rms"):
+                 buckets: int = 15, norm: str = "rms", fused: bool = False):
         super().__init__()
         kv_heads = kv_heads or heads
         if channels % heads or channels // heads % 8 or channels // heads > relation.MAX_DIM:
             raise ValueError("channels / heads must be a multiple of 8, at most %d" % relation.MAX_DIM)
         if heads % kv_heads:
             raise ValueError("kv_heads must divide heads")
-        self.layers = nn.ModuleList(RelationLayer(channels, heads, kv_heads, buckets, norm)
+        self.layers = nn.ModuleList(RelationLayer(channels, heads, kv_heads, buckets, norm, fused)
                                     for _ in range(layers))
 
-    def memory(self, num_pages: int, streams: int, max_pages: int) -> BoxMemory:
+    def memory(self, num_pages: int, streams: int, max_pages: int, evict: str = "oldest",
+               decay: float = 0.9) -> BoxMemory:
         """A memory for `streams` videos, one image of each to a call."""
         first = self.layers[0]
         return BoxMemory(num_pages, streams, max_pages, first.kv_heads, first.dim, len(self.layers),
-                         first.bias.device)
+                         first.bias.device, evict, decay)
 
     def forward(self, x, boxes, counts: Optional[Sequence[int]] = None, memory: Optional[BoxMemory] = None):
         """x [images, boxes, channels] float32 or bfloat16, boxes float32 [images, boxes, 4] (x1, y1,
@@ -291,6 +331,7 @@ class RelationHead(nn.Module):
 
         recalled = None
         fresh = []                              # what each layer is to remember
+        weight = None if memory is None else memory.weight
         if memory is not None:
             memory.check(host)
             first = self.layers[0]
@@ -304,11 +345,16 @@ class RelationHead(nn.Module):
         u = u.view(B, n, c)
         for i, layer in enumerate(self.layers):
             if memory is not None:
-                def recalled(q, k, v, geo, held=memory.layers[i]):
+                def recalled(q, k, v, geo, held=memory.layers[i], first_layer=i == 0):
+                    nonlocal weight
                     # both parts in binary32 (the memory's by binary32 queries), rounded when joined
                     out, lse, full = relation.box_attn_fwd(q, k, v, save=True, **geo)
                     far, far_lse = relation.box_memory_attn_fwd(q.float(), held, pages, remembered, q_boxes=boxes,
                                                                 bias=geo["bias"], q_len=lengths, save=True)
+                    if weight is not None:      # their share of the softmax over both
+                        weight = evict.box_memory_weigh(
+                            q.float(), held, pages, remembered, torch.logaddexp(lse, far_lse), weight=weight,
+                            decay=memory.decay if first_layer else 1.0, q_boxes=boxes, bias=geo["bias"], q_len=lengths)
                     fresh.append((held, *(t.reshape(B * n, *t.shape[2:])[rows] for t in (k, v))))
                     # one softmax over both: far's share is exp(far_lse) of the sum of both
                     share = torch.where(far_lse == -torch.inf, torch.zeros_like(lse),
@@ -319,6 +365,8 @@ class RelationHead(nn.Module):
                          None if last else self.layers[i + 1].pre[0])
         if memory is not None:                  # nothing is taken or written before all of it is there
             kept = boxes.reshape(B * n, 4)[rows].contiguous()
+            if weight is not None:
+                memory.weight = weight
             slots = memory.take(host)
             for held, k, v in fresh:
                 relation.box_memory_append(held, slots, k, v, kept)
