@@ -28,12 +28,14 @@ re_status_t box_memory_weigh(const box_memory_t *m, const box_recall_t *r, const
 /* Each stream keeps the min(keep[b], lengths[b]) boxes of the largest weight, of equal ones those in
  * lower places, NaN counting as larger than any number.  They end in its first places: those that were
  * there stay where they are, and those further on go, in the order of their places, to the places that
- * became free, in order; so nothing else in the memory is written.
+ * became free, in order; every other place holds what it held (pages that boxes come to are written
+ * whole, and nothing else may write to them meanwhile).
  *   lengths_out[b]: the boxes kept;  weight_out[b][t]: the weight of the box that is now in place t,
  *   0 from lengths_out[b] on;  origin[b][t]: the place that it was in, -1 from there on.
  * A stream that has a page number outside [0, num_pages) among the pages of its lengths[b] places
  * is left as it is (origin[b][t] = t).  lengths is clamped to [0, 32 * max_pages], keep to
- * [0, lengths[b]].  A page belongs to one stream and is named once in its row. */
+ * [0, lengths[b]].  A page belongs to one stream and is named once in its row.  At most 2^24 pages times
+ * (kv_heads + 3) / 4, and 2^21 streams (RE_ERR_UNSUPPORTED); box_memory_weigh takes up to 2^22 pages. */
 typedef struct {
     int64_t batch, max_pages;
     const int32_t *pages;     /* [batch][max_pages] */

@@ -46,8 +46,9 @@ typedef struct {
     int32_t act;
 } linear_act_t;
 /* Any alignment of the element's size.  Fastest where ins, outs and the strides are multiples of 16
- * bytes and the bases are aligned to that.  256 rows of any operand span less than 2^30 bytes, and
- * rows, ins and outs are at most 2^31 - 1 and RE_LINEAR_MAX_SIZE (RE_ERR_UNSUPPORTED). */
+ * bytes and the bases are aligned to that.  256 rows of any operand span less than 2^30 bytes, rows, ins
+ * and outs are at most 2^31 - 1 and RE_LINEAR_MAX_SIZE, and y, x and weight each have fewer than 2^24
+ * blocks of 64 x 64 elements (RE_ERR_UNSUPPORTED). */
 
 /* Device workspace of linear_act_fwd, or of linear_act_bwd where `backward`: partial sums where
  * few results have long sums; in the backward the gradient of t and partial column sums.  Host-only. */

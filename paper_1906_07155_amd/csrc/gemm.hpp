@@ -269,6 +269,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(GemmArgs a) {
     constexpr int kRound = MT <= kFit ? MT : MT / 2, kQuads = kCols / 4, kStride = 64 / kQuads;
     static_assert(kRound <= kFit && MT % kRound == 0, "results of a round");
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");      // (the barrier alone does not hold the stores back)
     f32x4 *stage = reinterpret_cast<f32x4 *>(&smem[0][0]) + wave * kRound * 16 * kQuads;
     const int quad = lane % kQuads, n = n0 + wn * kCols + 4 * quad, left = a.N - n;
     const int wave_m = wm * kRows + lane / kQuads;

@@ -638,8 +638,8 @@ re_status_t box_memory_weigh(const box_memory_t *m, const box_recall_t *r, const
     if (!aligned(lse, 4) || !aligned(weight, 4) || !aligned(weight_out, 4)) return RE_ERR_INVALID_ARG;
     if (w.a.B == 0 || w.a.max_pages == 0) return RE_OK;
     if (!weight_out || (w.a.Nq > 0 && !lse)) return RE_ERR_INVALID_ARG;
-    // a launch has fewer than 2^32 threads: a workgroup of 512 for every page
-    if (double(w.a.B) * double(w.a.max_pages) >= double(1 << 23)) return RE_ERR_UNSUPPORTED;
+    // a launch has fewer than 2^32 threads: a workgroup of 1024 for every page
+    if (double(w.a.B) * double(w.a.max_pages) >= double(1 << 22)) return RE_ERR_UNSUPPORTED;
     w.lse = lse;
     w.weight = weight;
     w.decay = decay;

@@ -65,6 +65,7 @@ BAD_LINEAR = [
     (dict(rows=1 << 31), UNSUPPORTED), (dict(ins=(1 << 24) + 1), UNSUPPORTED), (dict(outs=(1 << 24) + 1), UNSUPPORTED),
     (dict(x_stride=1 << 20), UNSUPPORTED), (dict(weight_stride=1 << 20), UNSUPPORTED),      # 256 rows past a buffer's reach
     (dict(ins=1 << 20, x_stride=1 << 20, weight_stride=1 << 20), UNSUPPORTED), (dict(outs=1 << 20), UNSUPPORTED),
+    (dict(rows=1 << 30, outs=64), UNSUPPORTED),                 # more workgroups than a launch has
 ]
 
 
