@@ -5,15 +5,18 @@
 //
 // One to four rows that share a key head's keys (queries times the heads of a group): a lane has a box,
 // half a wave a key head, and products are sums of its lane: of sixteen columns of a matrix product
-// fifteen would be empty, and what is done with its results as well (64 single queries against up to
-// 8192 boxes in 8 heads of 32: 89 us).
+// fifteen would be empty, and what is done with its results as well.  64 streams of 8192 boxes in 8 heads
+// of 32: one row 31 us (4.6 TB/s), as columns 91; four 53 and 98; 16 streams in 16 heads of 64: 45 and 56, 62
+// and 62.
 //
 // More: the logits are made as in the recall (attn_fwd.hpp), keys the rows of the products and queries
 // their columns, so a lane has eight keys of one query, and adds their weights up over heads and
 // queries in its registers; the sixteen lanes of a row meet at the end, once for a page.  Up to 16 queries
-// a wave takes a page and all of its heads, several heads' codes on their way at once.  Beyond, a
-// workgroup takes a page, its waves share heads and queries out, and the buckets of 256 queries against
-// the page's boxes are computed once for all heads into LDS; vector instructions bound it.
+// a wave takes a page and all of its heads, several heads' codes on their way at once: 16 rows of those 64
+// streams 107 us.  Beyond, a workgroup takes a page, its waves share heads and queries out, and the buckets
+// of 256 queries against the page's boxes are computed once for all heads into LDS: 17 rows 123 us (155 the
+// other way), 128 249 (617); 300 rows against 6000 boxes in 16 heads of 64, 31: vector instructions bound
+// it, half of the time of the 188 CUs that have a page.
 #include "attn.hpp"
 #include "evict.hpp"
 
@@ -393,6 +396,13 @@ template <typename T, int COMBOS> void run_lane(const WeighArgs &w, hipStream_t 
     else weigh_lane_kernel<T, COMBOS, false><<<grid, kLaneWaves * 64, lds, s>>>(w, blocks);
 }
 
+template <typename T, int DB, int WAVES> void run_many(const WeighArgs &w, hipStream_t s) {
+    const uint32_t grid = static_cast<uint32_t>(w.a.B) * w.a.max_pages;
+    const uint32_t lds = many_lds(w.a.rule.nb, w.a.bias != nullptr, WAVES).total;
+    if (w.a.bias) weigh_many_kernel<T, DB, true, WAVES><<<grid, WAVES * 64, lds, s>>>(w);
+    else weigh_many_kernel<T, DB, false, WAVES><<<grid, WAVES * 64, lds, s>>>(w);
+}
+
 template <typename T, int DB> void run(const WeighArgs &w, hipStream_t s) {
     const int64_t pages = static_cast<int64_t>(w.a.B) * w.a.max_pages;
     switch (lane_combos(w.a)) {
@@ -406,11 +416,12 @@ template <typename T, int DB> void run(const WeighArgs &w, hipStream_t s) {
         else weigh_few_kernel<T, DB, false><<<grid, kFewWaves * 64, 0, s>>>(w);
         return;
     }
-    // (the operands of wide binary32 heads need the registers of more than a sixteenth of a CU's waves)
-    constexpr int kWaves = DB == 4 && sizeof(T) == 4 ? 8 : 16;
-    const uint32_t grid = static_cast<uint32_t>(pages), lds = many_lds(w.a.rule.nb, w.a.bias != nullptr, kWaves).total;
-    if (w.a.bias) weigh_many_kernel<T, DB, true, kWaves><<<grid, kWaves * 64, lds, s>>>(w);
-    else weigh_many_kernel<T, DB, false, kWaves><<<grid, kWaves * 64, lds, s>>>(w);
+    // Four waves a page where pages fill the GPU several times over, sixteen where they do not (eight for
+    // wide binary32 heads, whose operands fill more registers).  16 streams of 8192 boxes in 16 heads of 64
+    // against 32 rows: 74 us with 4 waves, 86 with 8, 126 with 16; one of 6000 against 300: 50, 34 and 33.
+    constexpr int kWide = DB == 4 && sizeof(T) == 4 ? 8 : 16;
+    if (pages >= 512) run_many<T, DB, 4>(w, s);
+    else run_many<T, DB, kWide>(w, s);
 }
 template <typename T> void run_sized(const WeighArgs &w, hipStream_t s) {
     if (w.a.D <= 32) run<T, 1>(w, s);

@@ -99,6 +99,19 @@ def test_weigh(dtype, nq, heads, hkv, D, nb):
     check_weigh(nq + D, 2, nq, heads, hkv, D, dtype, 4, [128, 70], nb)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("nq,heads,hkv", [(2, 3, 3), (3, 2, 2), (4, 2, 2), (1, 4, 2), (2, 4, 2), (1, 8, 2), (2, 6, 2)])
+def test_weigh_rows_that_share_keys(dtype, nq, heads, hkv):
+    check_weigh(nq * heads, 3, nq, heads, hkv, 40, dtype, 9, [288, 150, 31], 15, q_len=[nq, nq - 1, nq])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_weigh_many_pages(dtype, D):
+    """So many of them that a workgroup has fewer waves."""
+    check_weigh(D, 3, 20, 4, 2, D, dtype, 200, [6400, 5000, 33], 7)
+
+
 @pytest.mark.parametrize("nq", [3, 40])
 def test_weigh_lengths(nq):
     """No box, one, pages that end inside a tile, lengths and rows outside their range; in place."""
