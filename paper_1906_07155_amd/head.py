@@ -227,7 +227,9 @@ def class_logprob_fwd(logits, labels, *, scale: float = 1.0, top: int = 0, works
     m, c = logits.shape
     L = lib()
     with _Call(logits, stream) as call:
-        logp, entropy, stats = call.empty((m,), torch.float32), call.empty((m,), torch.float32), call.empty((m, 2), torch.float32)
+        # (parts of one buffer: an allocation costs more than a view)
+        logp, entropy, stats = call.empty((4 * m,), torch.float32).split_with_sizes((m, m, 2 * m))
+        stats = stats.view(m, 2)
         top_logp = top_index = None
         if top:
             top_logp, top_index = call.empty((m, top), torch.float32), call.empty((m, top), torch.int64)
