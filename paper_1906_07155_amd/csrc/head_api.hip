@@ -39,7 +39,7 @@ bool chunks(const Matrix &x, int64_t size) {
 struct Product {
     GemmArgs a;
     GemmPlan plan;
-    bool tp, tq, skinny;
+    bool tp, tq, skinny, turned;
     size_t bytes;               // of partial sums
 };
 
@@ -60,6 +60,16 @@ const TileCost kTilesBf16[] = {{kTileLarge, 256, 256, 1.71, 1.71, 12.0}, {kTileM
 const TileCost kTilesF32[] = {{kTileMiddle, 128, 64, 0.98, 1.4, 2.0}, {kTileSmall, 64, 64, 0.51, 0.8, 1.0}};
 constexpr int64_t kCus = 256;
 
+// Few rows, or few outputs, go from memory to the products (launch_skinny): up to 16 of them, whose sums
+// may be cut into parts where they are long, or up to 64 whose sums are short enough for one launch.
+// One of 1024 x 12544 in bf16 15 us that way, 17 in tiles; 16 of 2048 x 1024 9 and 15; 64 of 4096 x 1024 9 and
+// 15, of 1024 x 12544 22 and 17; 6 outputs of 7397 rows x 2624 13 and 17, 16 of 16000 x 1024 14 and 12.
+bool few_rows(int64_t M, int64_t N, int64_t K, int64_t size) {
+    const int64_t few = std::min(M, N), groups = (std::max(M, N) + 15) / 16, steps = (K + 31) / 32;
+    if (few <= 16) return groups <= 2 * kCus || steps >= 64;
+    return few <= kSkinnyRows && groups <= 2 * kCus && few * steps * size <= 8192;
+}
+
 void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq, int32_t dtype, bool smooth) {
     const int64_t size = dtype_size(dtype), step = 128 / size;
     g = Product{};
@@ -76,10 +86,11 @@ void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq
     g.tq = tq;
     g.plan.chunks = chunks(p, size) && chunks(q, size);
     const int64_t M = a.M, N = a.N, K = a.K;
-    if (!tp && !tq && M <= kSkinnyRows && g.plan.chunks && K % 8 == 0) {
+    if (few_rows(M, N, K, size) && !tp && !tq && g.plan.chunks && K % 8 == 0) {
         g.skinny = true;
-        const int64_t groups = (N + 15) / 16, steps = (K + 31) / 32;
-        a.split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(128 / groups, steps / 64)));
+        g.turned = N < M;
+        const int64_t groups = (std::max(M, N) + 15) / 16, steps = (K + 31) / 32;
+        if (steps >= 128) a.split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(kCus / groups, steps / 32)));
         a.steps = static_cast<int32_t>((steps + a.split - 1) / a.split);
         a.split = static_cast<int32_t>((steps + a.steps - 1) / a.steps);
         g.bytes = a.split > 1 ? align256(static_cast<size_t>(a.split) * M * N * 4) : 0;
@@ -131,10 +142,10 @@ re_status_t run_product(Product &g, void *out, void *ws, int32_t dtype, hipStrea
     a.out = out;
     a.part = static_cast<float *>(ws);
     const int64_t size = dtype_size(dtype);
-    a.vec = a.N % 4 == 0 && aligned(out, 4 * size) &&
+    a.vec = !g.turned && a.N % 4 == 0 && aligned(out, 4 * size) &&
             (!a.residual || (a.ldr % 4 == 0 && aligned(a.residual, 4 * size))) && aligned(a.slope, 4 * size);
     hipError_t e;
-    if (g.skinny) e = launch_skinny(a, dtype, s);
+    if (g.skinny) e = launch_skinny(a, dtype, g.turned, s);
     else if (dtype == RE_DTYPE_BF16) e = launch_gemm_bf16(a, g.plan, g.tp, g.tq, s);
     else e = launch_gemm_f32(a, g.plan, g.tp, g.tq, s);
     if (e == hipSuccess && a.split > 1) e = g.skinny ? launch_skinny_join(a, dtype, s) : launch_gemm_join(a, g.plan, dtype, s);

@@ -9,10 +9,11 @@ namespace rex {
 // ---------------------------------------------------------------------------
 // The weights are read once, by all of the GPU, and that is what bounds it: a workgroup takes 16
 // outputs, its waves every 16th step of 32 inputs, straight from memory into the products' operands.
-// The rows are the products' columns, so one to 64 of them cost the same weights.
+// The rows are the products' columns, so one to 64 of them cost the same weights.  Few outputs of many
+// rows are the same the other way round (TURNED): rows come from memory, weights are the columns.
 constexpr int kSkinnyWaves = 16;
 
-template <typename T, int NQ>
+template <typename T, int NQ, bool TURNED>
 __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(GemmArgs a) {
     using N = Num<T>;
     using Frag = typename N::Frag;
@@ -20,12 +21,15 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(GemmArgs a) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = blockIdx.x * 16, part = blockIdx.y;
-    const auto pr = make_rsrc(static_cast<const char *>(a.p) + n0 * a.ldp, kBufMaxBytes - 1);
-    const auto qr = make_rsrc(a.q, kBufMaxBytes - 1);
-    const uint32_t poff = n0 + n < a.N ? static_cast<uint32_t>(n * a.ldp) : kBufOOB;
+    // the many rows and the few
+    const int many = TURNED ? a.M : a.N, few = TURNED ? a.N : a.M;
+    const int64_t ldp = TURNED ? a.ldq : a.ldp, ldq = TURNED ? a.ldp : a.ldq;
+    const auto pr = make_rsrc(static_cast<const char *>(TURNED ? a.q : a.p) + n0 * ldp, kBufMaxBytes - 1);
+    const auto qr = make_rsrc(TURNED ? a.p : a.q, kBufMaxBytes - 1);
+    const uint32_t poff = n0 + n < many ? static_cast<uint32_t>(n * ldp) : kBufOOB;
     uint32_t qoff[NQ];
 #pragma unroll
-    for (int t = 0; t < NQ; ++t) qoff[t] = 16 * t + n < a.M ? static_cast<uint32_t>((16 * t + n) * a.ldq) : kBufOOB;
+    for (int t = 0; t < NQ; ++t) qoff[t] = 16 * t + n < few ? static_cast<uint32_t>((16 * t + n) * ldq) : kBufOOB;
 
     f32x4 acc[NQ] = {};
     const int all = (a.K + 31) / 32, first = part * a.steps, end = min(first + a.steps, all);
@@ -55,6 +59,20 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(GemmArgs a) {
     f32x4 x = sums[0][wave][lane];
 #pragma unroll
     for (int w = 1; w < kSkinnyWaves; ++w) x += sums[w][wave][lane];
+    if constexpr (TURNED) {             // four rows of one output
+        const int col = 16 * wave + n;
+        if (col >= a.N) return;
+        const float bias = a.bias && a.split == 1 ? load_bias(a, col)[0] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int m = n0 + 4 * g + i;
+            if (m >= a.M) return;
+            const int64_t at = static_cast<int64_t>(m) * a.N + col;
+            if (a.split > 1) as_global_mut<float>(a.part)[static_cast<int64_t>(part) * a.M * a.N + at] = x[i];
+            else finish4<T>(a, 1, at, m * a.ldr + col, f32x4{x[i] + bias, 0.0f, 0.0f, 0.0f});
+        }
+        return;
+    }
     const int m = 16 * wave + n, to = n0 + 4 * g;
     if (m >= a.M || to >= a.N) return;
     const int64_t at = static_cast<int64_t>(m) * a.N + to;
@@ -66,17 +84,18 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(GemmArgs a) {
     } else finish4<T>(a, a.N - to, at, m * a.ldr + to, x + load_bias(a, to));
 }
 
-template <typename T>
+template <typename T, bool TURNED>
 static void run_skinny(const GemmArgs &a, hipStream_t s) {
-    const dim3 grid((a.N + 15) / 16, a.split);
-    if (a.M <= 16) skinny_kernel<T, 1><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
-    else if (a.M <= 32) skinny_kernel<T, 2><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
-    else skinny_kernel<T, 4><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
+    const int few = TURNED ? a.N : a.M;
+    const dim3 grid(((TURNED ? a.M : a.N) + 15) / 16, a.split);
+    if (few <= 16) skinny_kernel<T, 1, TURNED><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
+    else if (few <= 32) skinny_kernel<T, 2, TURNED><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
+    else skinny_kernel<T, 4, TURNED><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
 }
 
-hipError_t launch_skinny(const GemmArgs &a, int dtype, hipStream_t s) {
-    if (dtype == kBF16) run_skinny<uint16_t>(a, s);
-    else run_skinny<float>(a, s);
+hipError_t launch_skinny(const GemmArgs &a, int dtype, bool turned, hipStream_t s) {
+    if (dtype == kBF16) turned ? run_skinny<uint16_t, true>(a, s) : run_skinny<uint16_t, false>(a, s);
+    else turned ? run_skinny<float, true>(a, s) : run_skinny<float, false>(a, s);
     return hipGetLastError();
 }
 

@@ -40,9 +40,10 @@ hipError_t launch_gemm_bf16(const GemmArgs &a, const GemmPlan &p, bool tp, bool 
 hipError_t launch_gemm_f32(const GemmArgs &a, const GemmPlan &p, bool tp, bool tq, hipStream_t s);
 hipError_t launch_gemm_join(const GemmArgs &a, const GemmPlan &p, int dtype, hipStream_t s);
 hipError_t launch_skinny_join(const GemmArgs &a, int dtype, hipStream_t s);
-// A few rows against [N][K]: the weights go from memory straight to the products.
+// A few rows against [N][K], or few outputs of many rows (turned): what there is much of goes from
+// memory straight to the products.
 constexpr int kSkinnyRows = 64;
-hipError_t launch_skinny(const GemmArgs &a, int dtype, hipStream_t s);
+hipError_t launch_skinny(const GemmArgs &a, int dtype, bool turned, hipStream_t s);
 
 struct SlopeArgs {
     const void *gy, *saved;         // [M][N] dense; saved null: slope 1

@@ -129,6 +129,14 @@ def test_sizes(dtype, m, n, k):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(16, 40, 8192), (17, 40, 1024), (64, 300, 512), (300, 16, 4104), (1001, 5, 264), (400, 33, 256),
+                                   (2000, 1, 8192), (9000, 16, 2048), (9000, 12, 64), (130, 64, 512), (15, 15, 15 * 8)])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_few_rows_or_outputs(dtype, m, n, k, act):
+    check(m + n + k, m, n, k, dtype, act, residual=act == "gelu")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m,n,k", [(1000, 1024, 2048), (2048, 1536, 512), (4000, 520, 264), (256, 256, 8200)])
 def test_large(dtype, m, n, k):
     check(3, m, n, k, dtype, "relu")
