@@ -20,7 +20,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIBRARY = os.path.join(HERE, "libroi_extract.so")
 SOURCES = ["api.hip", "plan.hip", "fwd.hip", "bwd.hip", "adaptive.hip", "pool.hip", "deform.hip", "nms.hip", "select.hip",
            "relation_api.hip", "attn_dense.hip", "attn_recall.hip", "attn_bwd.hip", "memory.hip", "norm.hip",
-           "head_api.hip", "gemm_bf16.hip", "gemm_f32.hip", "linear.hip", "logprob.hip", "weigh.hip", "evict.hip"]
+           "head_api.hip", "gemm_bf16.hip", "gemm_f32.hip", "linear.hip", "logprob.hip", "evict_api.hip", "weigh.hip",
+           "evict.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

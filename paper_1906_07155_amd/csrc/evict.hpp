@@ -1,9 +1,14 @@
 // evict.hpp -- argument blocks and launchers of what the memory of boxes forgets.
 #pragma once
 
+#include "box_evict.h"
 #include "relation.hpp"
 
 namespace rex {
+
+// Of the memory and of a call that reads it (relation_api.hip).
+re_status_t check_memory(const box_memory_t *m);
+re_status_t recall_args(const box_memory_t *m, const box_recall_t *r, AttnArgs *a);
 
 struct WeighArgs {
     AttnArgs a;                     // the recall's

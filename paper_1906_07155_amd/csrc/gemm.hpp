@@ -18,7 +18,7 @@
 // step, are given an offset that the range check answers with 0.
 #pragma once
 
-#include "linear.hpp"
+#include "epilogue.hpp"
 
 namespace rex {
 

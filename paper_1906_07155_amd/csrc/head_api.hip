@@ -170,10 +170,10 @@ re_status_t check_linear(const linear_act_t *d) {
     if (d->rows > INT32_MAX || d->ins > RE_LINEAR_MAX_SIZE || d->outs > RE_LINEAR_MAX_SIZE) return RE_ERR_UNSUPPORTED;
     for (int64_t v : {xs, ws, d->ins, d->outs})
         if (256 * v * static_cast<int64_t>(size) >= kBufMaxBytes) return RE_ERR_UNSUPPORTED;
-    // a launch has fewer than 2^32 threads: 256 for every 64 x 64 results at most
+    // a launch has fewer than 2^32 threads: 256 for every 64 x 64 results at most, and for some tiles more
     const auto tiles = [](int64_t m, int64_t n) { return double((m + 63) / 64) * double((n + 63) / 64); };
     for (double t : {tiles(d->rows, d->outs), tiles(d->rows, d->ins), tiles(d->outs, d->ins)})
-        if (t >= double(1 << 24)) return RE_ERR_UNSUPPORTED;
+        if (t > double((1 << 24) - 16)) return RE_ERR_UNSUPPORTED;
     return RE_OK;
 }
 

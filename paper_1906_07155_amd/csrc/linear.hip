@@ -1,6 +1,6 @@
 // linear.hip -- the dense layers' kernels beside the tiled products: few rows, the joining of
 // parts, the upstream gradient times the activation's slope.
-#include "linear.hpp"
+#include "epilogue.hpp"
 
 namespace rex {
 

@@ -197,6 +197,42 @@ def test_evict_refuses(L):
     assert call(e=eviction(batch=0), left=0, out=0, origin=0, ws=0, size=0) == OK
 
 
+@pytest.mark.skipif(not os.environ.get("REX_LIBRARY", "").endswith("_host.so"),
+                    reason="needs a build whose launchers do nothing")
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_valid_calls(L, dtype):
+    sizes = (1, 3, 16, 17, 63, 64, 65, 255, 256, 257, 1000, 4096, 12544, 16001)
+    shapes = [(m, n, k) for m in (0,) + sizes for n in sizes for k in sizes]
+    shapes += [(64 * ((1 << 24) - 16), 1, 8), ((1 << 24) - 16, 64, 64), ((1 << 25) - 64, 6, 2048),
+               (1 << 29, 16, 64), (1, 1 << 19, 2048), (1 << 20, 128, 256)]
+    for m, n, k in shapes:
+        for act, aligned in ((0, True), (1, True), (2, False)) if m < 300 else ((3, True), (0, False)):
+            stride = k if m < 1 << 24 else 0
+            d = linear(rows=m, outs=n, ins=k, dtype=dtype, bias_dtype=dtype, act=act, x=FAKE + (0 if aligned else 4),
+                       x_stride=stride, weight_stride=k, residual_stride=n, residual=FAKE if aligned else 0)
+            size = size_of(L.linear_act_workspace_size, d, 0)
+            assert L.linear_act_fwd(d, FAKE, FAKE if act else 0, FAKE if size else 0, size, 0) == OK, (m, n, k, act)
+            size = size_of(L.linear_act_workspace_size, d, 1)
+            y = FAKE if act == 1 else 0
+            gy = FAKE if aligned else FAKE + 4
+            for gx, gw, gb in ((FAKE, FAKE, FAKE), (FAKE, 0, 0), (0, FAKE, 0), (0, 0, FAKE), (0, 0, 0)):
+                assert L.linear_act_bwd(d, gy, 0 if act < 2 else FAKE, y, gx, gw, gb, FAKE, size, 0) == OK, (m, n, k, act)
+    for rows in (0, 1, 100, 1000):
+        for classes in (1, 7, 81, 4088, 4089, 8177, 100003, 1 << 24):
+            for top in (0, min(classes, 16)):
+                d = logprob(rows=rows, classes=classes, stride=classes, top=top, dtype=dtype)
+                size = size_of(L.class_logprob_workspace_size, d)
+                assert L.class_logprob_fwd(d, *[FAKE] * 5, FAKE, size, 0) == OK
+                assert L.class_logprob_bwd(d, *[FAKE] * 5, 0) == OK
+    for kw in (dict(), dict(batch=0), dict(num_q=0), dict(max_pages=0, pages=0), dict(batch=3, num_q=1, max_pages=1 << 19)):
+        assert L.box_memory_weigh(memory(), recall(dtype=dtype, **kw), FAKE, FAKE, 0.5, FAKE << 1, 0) == OK
+    for kw in (dict(), dict(batch=0), dict(max_pages=0, pages=0, weight=0), dict(batch=16, max_pages=1 << 18),
+               dict(batch=1 << 21, max_pages=1)):
+        size = size_of(L.box_memory_evict_workspace_size, memory(), eviction(**kw))
+        for origin in (0, FAKE):
+            assert L.box_memory_evict(memory(), eviction(**kw), FAKE, FAKE << 1, origin, FAKE, size, 0) == OK
+
+
 def test_headers_and_binding_agree(L, tmp_path):
     assert sorted(H.header_functions()) == sorted(H.SIGNATURES) and len(H.SIGNATURES) == 6
     assert sorted(E.header_functions()) == sorted(E.SIGNATURES) and len(E.SIGNATURES) == 3
