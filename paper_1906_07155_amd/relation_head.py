@@ -211,6 +211,7 @@ class BoxMemory:
     def forget(self, stream: int) -> None:
         """The stream's pages go back to the pool."""
         if self.weight is not None:
+            self.weight = self.weight.clone()           # (made in inference mode it takes no writes outside)
             self.weight[stream] = 0
         self.free.extend(self.table[stream])
         self.table[stream], self.used[stream] = [], 0

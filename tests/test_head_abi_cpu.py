@@ -331,3 +331,13 @@ def test_box_memory_by_weight(monkeypatch):
     memory.forget(0)
     assert memory.used == [0, 40] and not memory.weight[0].any() and len(memory.free) == 4
     assert len(memory.take([10, 0])) == 10
+
+
+def test_box_memory_forgets_outside_inference_mode():
+    from paper_1906_07155_amd import relation_head as RH
+    memory = RH.BoxMemory(6, 2, 3, 2, 32, device="cpu", evict="weight")
+    memory.take([10, 10])
+    with torch.inference_mode():                # as a frame does
+        memory.weight = memory.weight + 1
+    memory.forget(0)
+    assert memory.used == [0, 10] and not memory.weight[0].any() and (memory.weight[1] == 1).all()
