@@ -34,8 +34,9 @@ re_status_t box_memory_weigh(const box_memory_t *m, const box_recall_t *r, const
  *   0 from lengths_out[b] on;  origin[b][t]: the place that it was in, -1 from there on.
  * A stream that has a page number outside [0, num_pages) among the pages of its lengths[b] places
  * is left as it is (origin[b][t] = t).  lengths is clamped to [0, 32 * max_pages], keep to
- * [0, lengths[b]].  A page belongs to one stream and is named once in its row.  At most 2^24 pages times
- * (kv_heads + 3) / 4, and 2^21 streams (RE_ERR_UNSUPPORTED); box_memory_weigh takes up to 2^22 pages. */
+ * [0, lengths[b]].  A page belongs to one stream and is named once in its row.  Fewer than 2^24 pages
+ * times (kv_heads + 3) / 4, and at most 2^21 streams (RE_ERR_UNSUPPORTED); box_memory_weigh takes fewer than 2^22
+ * pages. */
 typedef struct {
     int64_t batch, max_pages;
     const int32_t *pages;     /* [batch][max_pages] */

@@ -64,6 +64,8 @@ re_status_t linear_act_fwd(const linear_act_t *a, void *y, void *slope, void *wo
 /* Gradients for upstream grad_y ([rows][outs] dense).  With g = grad_y * slope:
  *   grad_x = g weight [rows][ins], grad_weight = g^T x [outs][ins] (both dense),
  *   grad_bias[n] = sum over the rows of g, of bias_dtype, summed before g is rounded to the data's type;
+ * the products take g rounded to the data's type (exact for RE_ACT_NONE and RE_ACT_RELU), so that of bf16
+ * data grad_x and grad_weight carry one more rounding of each of their terms beside their own;
  * the residual's gradient is grad_y itself.  Each may be NULL (not wanted).  Exactly one of slope
  * (as linear_act_fwd wrote it) and y (RE_ACT_RELU without a residual: what linear_act_fwd wrote) is
  * given, neither with RE_ACT_NONE.  a->residual is not read. */

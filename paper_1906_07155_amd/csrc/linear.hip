@@ -11,6 +11,7 @@ namespace rex {
 // outputs, its waves every 16th step of 32 inputs, straight from memory into the products' operands.
 // The rows are the products' columns, so one to 64 of them cost the same weights.  Few outputs of many
 // rows are the same the other way round (TURNED): rows come from memory, weights are the columns.
+// A row of 1024 x 1024 in bf16 takes 4.6 us: a launch, two dependent loads and the meeting of 16 waves.
 constexpr int kSkinnyWaves = 16;
 
 template <typename T, int NQ, bool TURNED>
@@ -103,7 +104,9 @@ hipError_t launch_skinny(const GemmArgs &a, int dtype, bool turned, hipStream_t 
 // Parts of k
 // ---------------------------------------------------------------------------
 
-// A thread for four adjacent results of a tile that was made in parts.
+// A thread for four adjacent results of a tile that was made in parts, which it adds in order.  1000 x 1024
+// in eight parts 8 us (4.2 TB/s), two of them a launch.  (The last workgroup of a tile adding up its
+// parts would spare the launch, for a fence and a count in memory that the caller has to clear.)
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(GemmArgs a, int bm, int bn) {
     const int quads = bm * bn / 4, tile = blockIdx.x / (quads / 256), at = blockIdx.x % (quads / 256) * 256 + threadIdx.x;
@@ -151,7 +154,11 @@ hipError_t launch_skinny_join(const GemmArgs &a, int dtype, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // One pass over both, a lane 16 bytes of a row at a time; the sums over a run of rows are taken
 // before the product is rounded.  `lanes` (a power of two) lanes take a row, so that narrow layers
-// use whole waves too.
+// use whole waves too.  Bytes bound it: 16000 x 2048 in bf16 with slopes of 24 bits 38 us, 229 MB at 6 TB/s.
+//
+// g is rounded to bf16, where the data is, for the two products that follow: with an activation other than
+// max(t, 0) their results are then off by two roundings of 2^-9 in the mean, 2.3e-3 of their norm instead
+// of 1.7e-3.  In two parts it would be one, for twice the products (70 and 81 us more at that size).
 
 // 16 bytes of them
 template <typename T, int V> __device__ __forceinline__ void load_run(const T *p, float *x) {

@@ -9,7 +9,10 @@
 // Rows begin at any element: a lane's 16 bytes are at a multiple of 16 all the same, and what is not of the
 // row counts as -inf (from the row's first element on, 32768 rows of 1231 bf16 took 32 us instead of 26).
 // What bounds it is memory: the
-// gradient needs the sums of the whole row, so that training reads the logits twice.
+// gradient needs the sums of the whole row, so that training reads the logits twice.  4096 rows of 32000 in bf16
+// 74 us (3.5 TB/s) and 108 (4.9 TB/s), 8192 of 1231, which caches hold, 11 and 13.  Few rows are bound by their steps,
+// each of which needs the one before: 16 of 100003 in binary32, with their eight top classes, 12 us in 25 parts
+// each and 6 for the joining.
 #include "logprob.hpp"
 #include "attn.hpp"
 
