@@ -213,23 +213,30 @@ def _logprob_descriptor(logits, labels, scale, top):
     return _LOGPROB.pack(logits.data_ptr(), labels.data_ptr(), stride, m, c, code, top, scale)
 
 
-def class_logprob_fwd(logits, labels, *, scale: float = 1.0, top: int = 0, workspace=None, stream=None):
+def class_logprob_fwd(logits, labels, *, scale: float = 1.0, top: int = 0, out=None, workspace=None, stream=None):
     """Log probabilities over logits [rows, classes] times `scale`: returns (logp, entropy,
     stats, top_logp, top_index): float32 [rows] of the labels (int64 [rows]; one outside the classes is
     not counted: 0) and of the entropy; stats float32 [rows, 2], which the backward takes, the
     largest of a row and the log sum relative to it; float32 and int64 [rows, top] of the `top` classes
-    with the largest logits, the lower class first among equals (None where top is 0)."""
+    with the largest logits, the lower class first among equals (None where top is 0).  out: (logp,
+    entropy, stats) to write."""
     torch = _torch()
     d = _logprob_descriptor(logits, labels, scale, top)
     if workspace is not None:
         binding._workspace(workspace, logits)
         _same_device(logits, "workspace", (workspace,))
     m, c = logits.shape
+    if out is not None:
+        for t, shape, name in zip(out, ((m,), (m,), (m, 2)), ("logp", "entropy", "stats")):
+            _dense(t, shape, name, torch.float32)
+        _same_device(logits, "logp entropy stats", out)
     L = lib()
     with _Call(logits, stream) as call:
-        # (parts of one buffer: an allocation costs more than a view)
-        logp, entropy, stats = call.empty((4 * m,), torch.float32).split_with_sizes((m, m, 2 * m))
-        stats = stats.view(m, 2)
+        if out is None:                 # (parts of one buffer: an allocation costs more than a view)
+            all = call.empty((4 * m,), torch.float32)
+            logp, entropy, stats = all[:m], all[m:2 * m], all[2 * m:].view(m, 2)
+        else:
+            logp, entropy, stats = out
         top_logp = top_index = None
         if top:
             top_logp, top_index = call.empty((m, top), torch.float32), call.empty((m, top), torch.int64)

@@ -75,6 +75,31 @@ def test_gradients_against_differences():
         assert abs(slope - float((leaves[i].grad.double() * d.double()).sum())) <= tol
 
 
+def test_results_may_be_written_to():
+    x, labels = randn(1, 6, 9), torch.tensor([0, 8, 3, -1, 5, 2], device="cuda")
+    keep = torch.tensor([1, 0, 1, 1, 0, 1], device="cuda")
+    for grad in (True, False):
+        leaf = x.clone().requires_grad_(grad)
+        weight = torch.ones(6, device="cuda", requires_grad=True)
+        logp, entropy, _, _ = rex.class_logprob(leaf, labels)
+        logp.masked_fill_(keep == 0, 0.0)
+        logp *= weight
+        (logp.sum() + 0.5 * entropy.sum()).backward()
+        ref = x.double().requires_grad_(grad)
+        full = torch.log_softmax(ref, 1)
+        picked = full.gather(1, labels.clamp(min=0)[:, None])[:, 0] * ((labels >= 0) & (keep == 1))
+        near(weight.grad, picked.detach(), 1e-5, "weight")
+        if grad:
+            (picked.sum() - 0.5 * (full.exp() * full).sum()).backward()
+            near(leaf.grad, ref.grad, 1e-5, "grad")
+    out = (torch.empty(6, device="cuda"), torch.empty(6, device="cuda"), torch.empty(6, 2, device="cuda"))
+    want = rex.class_logprob_fwd(x, labels)
+    got = rex.class_logprob_fwd(x, labels, out=out)
+    assert all(a is b and torch.equal(a, w) for a, b, w in zip(got, out, want))
+    with pytest.raises(ValueError):
+        rex.class_logprob_fwd(x, labels, out=(out[0], out[1][:5], out[2]))
+
+
 def test_second_derivatives_are_refused():
     x, w = randn(1, 4, 8).requires_grad_(), randn(2, 6, 8).requires_grad_()
     g, = torch.autograd.grad(rex.linear_act(x, w, act="gelu").sum(), x, create_graph=True)
