@@ -13,7 +13,8 @@
 // 16 streams of 8192 boxes in 16 heads of 64 channels, a quarter evicted, 111 us: 21 for the choice, 16
 // workgroups of dependent steps, and 88 for the moves, 218 MB read and 138 MB written at 4.1 TB/s: a free
 // place in every page makes all tiles of values go both ways, and late boxes' tiles are fetched for each
-// page that takes from them, where 50 MB of codes move.  (Neighbouring pages on one XCD: 186 MB read, 87 us.)
+// page that takes from them, where 50 MB of codes move.  (Neighbouring pages on
+// one XCD: 186 MB read, 87 us; late boxes' tiles through LDS whole, instead of bytes of them: 87.)
 #include "attn.hpp"
 #include "evict.hpp"
 
