@@ -99,7 +99,7 @@ typedef struct {
 re_status_t class_logprob_workspace_size(const class_logprob_t *a, size_t *bytes);
 
 /* logp, entropy: float[rows]; stats: float[rows][2], the largest x and log sum_c exp(x_c - that), whose
- * sum is lse (-inf and 0 in a row without a class), 8-byte aligned; top_logp: float[rows][top],
+ * sum is lse (-inf and 0 in a row without a class, NaN in one with NaN or +inf), 8-byte aligned; top_logp: float[rows][top],
  * top_index: int64[rows][top], both dense, not used where top is 0. */
 re_status_t class_logprob_fwd(const class_logprob_t *a, float *logp, float *entropy, float *stats,
                               float *top_logp, int64_t *top_index, void *workspace,

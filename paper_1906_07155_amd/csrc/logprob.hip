@@ -143,7 +143,8 @@ __device__ __forceinline__ float log_prob(const RowStats &r, float x) {
 }
 __device__ __forceinline__ RowStats row_stats(const LogPart &p) {
     const bool none = p.sum == 0.0f;
-    return RowStats{none ? -kInf : p.top, none ? 0.0f : __builtin_amdgcn_logf(p.sum) * kLn2};
+    // (the largest of nothing but NaN, or NaN and -inf, is -inf: their sum tells)
+    return RowStats{none ? -kInf : p.sum != p.sum ? p.sum : p.top, none ? 0.0f : __builtin_amdgcn_logf(p.sum) * kLn2};
 }
 // The label's x, if it is counted.
 struct Label {

@@ -142,6 +142,23 @@ def test_masks(dtype, c):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("c", [1, 81, 1231, 9000])
+def test_rows_of_nothing_but_nan(dtype, c):
+    x, labels, gl, gh = make(c, 8, c, dtype)
+    x[0] = math.nan
+    x[1, :-1] = -math.inf                                   # and one NaN
+    x[1, -1] = math.nan
+    x[2] = math.inf
+    x[3, :-1] = -math.inf
+    x[3, -1] = math.inf
+    labels[4] = -1
+    x[4] = math.nan
+    check(x, labels, gl, gh, top=min(c, 5))
+    logp, entropy, stats, _, _ = rex.class_logprob_fwd(x, labels)
+    assert logp[:4].isnan().all() and float(logp[4]) == 0.0 and entropy[:5].isnan().all() and stats[:5].sum(1).isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_large_logits(dtype):
     for spread in (50.0, 1000.0, 1e30):
         x, labels, gl, gh = make(5, 30, 333, dtype, spread=spread)
