@@ -91,13 +91,13 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return x != x ? 0xffffffffu : b ^ (static_cast<int32_t>(b) < 0 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ uint64_t make_key(uint32_t value, int c) {
-    return static_cast<uint64_t>(value) << 32 | (0xffffffffu - static_cast<uint32_t>(c));
+    return static_cast<uint64_t>(value) << 32 | (0xfffffffeu - static_cast<uint32_t>(c));      // (never all ones)
 }
 __device__ __forceinline__ float key_value(uint64_t k) {
     const uint32_t b = static_cast<uint32_t>(k >> 32);
     return b == 0xffffffffu ? __builtin_nanf("") : __uint_as_float(b ^ (b >> 31 ? 0x80000000u : 0xffffffffu));
 }
-__device__ __forceinline__ int key_class(uint64_t k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
+__device__ __forceinline__ int key_class(uint64_t k) { return static_cast<int>(0xfffffffeu - static_cast<uint32_t>(k)); }
 
 // over the `LANES` lanes of a row
 template <int LANES> __device__ __forceinline__ float lanes_max(float x) {
