@@ -8,6 +8,9 @@ roi_extract gives for each RoI through two shared dense layers to class scores a
     scores, deltas = head(rois_features)            # [K, 81], [K, 320]
     loss = head.loss(scores, labels)                # mean of -log p over the labels that count
     logp, classes = head.best(scores, 5)            # per RoI: the five likeliest classes
+
+All of it can be captured into a HIP graph.  A captured `backward()` needs leaves of which no eager graph
+lives any more (torch accumulates their gradients on that graph's stream); torch.autograd.grad does not.
 """
 from __future__ import annotations
 

@@ -163,6 +163,34 @@ def test_box_head_and_its_gradients(dtype, tol):
     assert [tuple(t.shape) for t in empty] == [(0, 12), (0, 44)]
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_captured_training_step(dtype):
+    torch.manual_seed(3)
+    head = rex.BoxHead(64 * 9, classes=5, hidden=48).cuda().to(dtype)
+    weights = list(head.parameters())
+    x, labels = randn(1, 70, 64, 3, 3, dtype=dtype), torch.arange(70, device="cuda") % 8 - 1
+
+    def step():
+        scores, deltas = head(x)
+        loss = head.loss(scores, labels) + 0.1 * (deltas * deltas).sum(1).mean()
+        return (loss.detach(), *torch.autograd.grad(loss, weights))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(2, 6):
+        x.copy_(randn(seed, 70, 64, 3, 3, dtype=dtype))
+        graph.replay()
+        got = [t.clone() for t in held]
+        want = step()                                   # eager, between replays
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), seed
+
+
 def test_box_head_on_extracted_features():
     """roi_extract's results through the head: one path from a pyramid to scores."""
     torch.manual_seed(0)
