@@ -101,10 +101,9 @@ void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq
     const int count = bf16 ? 3 : 2;
     const int64_t steps = (K + step - 1) / step;
     double best = -1;
-    for (int i = g.plan.chunks ? 0 : count - 1; i < count; ++i) {
+    for (int i = g.plan.chunks ? 0 : 1; i < count; ++i) {       // (through registers: the second and third, gemm_*.hip)
         const TileCost &t = all[i];
         const int64_t tm = (M + t.bm - 1) / t.bm, tn = (N + t.bn - 1) / t.bn, tiles = tm * tn;
-        if (tiles > (int64_t(1) << 28) && i + 1 < (g.plan.chunks ? count : 0)) continue;
         // us of n workgroups of k steps each
         const auto run = [&](int64_t n, int64_t k) {
             const double rounds = double((n + kCus - 1) / kCus);

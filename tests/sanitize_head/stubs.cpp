@@ -22,7 +22,7 @@ static bool small(int64_t groups, int threads) { return groups >= 1 && groups * 
 static hipError_t tiles(const GemmArgs &a, const GemmPlan &p, bool f32) {
     need(a.p && a.q && a.out && a.M >= 1 && a.N >= 1 && a.K >= 1);
     need(p.tile == kTileSmall || p.tile == kTileMiddle || (p.tile == kTileLarge && !f32));
-    need(p.chunks || p.tile == kTileSmall);
+    need(p.chunks || (f32 ? p.tile == kTileSmall : p.tile != kTileLarge));
     need(p.tile == kTileSmall ? p.bm == 64 && p.bn == 64 : p.tile == kTileLarge ? p.bm == 256 && p.bn == 256
                                                                                  : p.bm == 128 && p.bn == (f32 ? 64 : 128));
     need(a.tiles_m == (a.M + p.bm - 1) / p.bm && a.tiles_n == (a.N + p.bn - 1) / p.bn);

@@ -144,6 +144,13 @@ def test_large(dtype, m, n, k):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(1000, 1001, 2049), (777, 401, 1027), (4001, 131, 513), (257, 255, 8199), (1500, 1300, 70)])
+def test_large_and_odd(dtype, m, n, k):
+    check(5, m, n, k, dtype, "none", bias=None)
+    check(6, m, n, k, dtype, "gelu", residual=True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("wide", [1, 4, 8, 24])
 @pytest.mark.parametrize("m", [5, 200])
 def test_strides(dtype, wide, m):
