@@ -50,7 +50,9 @@ struct Product {
 // 1020 us, 64 x 64 1040) and of a workgroup that is alone on its CU, and what precedes and follows the steps (half of
 // it is hidden behind the products of other workgroups of the CU, which 256 x 256 has none of).  Tiles
 // that would start another round on the GPU's 256 CUs are cut along k until they fill it, or all are; the
-// parts are written and read again at some 6 TB/s, and joined by a launch more.
+// parts are written and read again at some 6 TB/s, and joined by a launch more, which costs 6 (1000 x 1024 x 1024
+// in binary32 31 us in two parts, 26 in one; 300 x 256 x 1024 in bf16 15 and 9).  Steps through registers take
+// longer (4096 x 4097 x 4095 in bf16 1.4 times as long, with an operand transposed 2.2 times; in binary32 1.2 times).
 struct TileCost {
     int kind, bm, bn;
     double step, alone, around;
@@ -100,6 +102,7 @@ void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq
     const TileCost *all = bf16 ? kTilesBf16 : kTilesF32;
     const int count = bf16 ? 3 : 2;
     const int64_t steps = (K + step - 1) / step;
+    const double slow = g.plan.chunks ? 1.0 : !bf16 ? 1.2 : tp || tq ? 2.0 : 1.5;
     double best = -1;
     for (int i = g.plan.chunks ? 0 : 1; i < count; ++i) {       // (through registers: the second and third, gemm_*.hip)
         const TileCost &t = all[i];
@@ -107,7 +110,7 @@ void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq
         // us of n workgroups of k steps each
         const auto run = [&](int64_t n, int64_t k) {
             const double rounds = double((n + kCus - 1) / kCus);
-            return double(k) * std::max(n > 0 ? t.alone : 0.0, rounds * t.step) + rounds * t.around * (smooth ? 1.8 : 1.0);
+            return double(k) * slow * std::max(n > 0 ? t.alone : 0.0, rounds * t.step) + rounds * t.around * (smooth ? 1.8 : 1.0);
         };
         for (int some = 0; some < 2; ++some) {       // parts of all tiles, or of those past full rounds
             const int64_t whole = some ? tiles / kCus * kCus : 0, parted = tiles - whole;
@@ -117,7 +120,7 @@ void plan_product(Product &g, const Matrix &p, bool tp, const Matrix &q, bool tq
                 const int64_t each = (steps + split - 1) / split;
                 if ((steps + each - 1) / each != split || (some && split == 1)) continue;
                 double us = run(whole, steps) + run(parted * split, each);
-                if (split > 1) us += 3.0 + 8e-6 / 6.0 * double(split * parted) * t.bm * t.bn;
+                if (split > 1) us += 6.0 + 8e-6 / 6.0 * double(split * parted) * t.bm * t.bn;
                 if (best >= 0 && us >= best) continue;
                 best = us;
                 g.plan.tile = t.kind;
