@@ -50,10 +50,7 @@ class LinearActFunction(torch.autograd.Function):
 class ClassLogprobFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels, scale, top):
-        # (results with gradients may be written to, so they are no views)
-        m, like = logits.shape[0], dict(dtype=torch.float32, device=logits.device)
-        out = torch.empty(m, **like), torch.empty(m, **like), torch.empty(m, 2, **like)
-        logp, entropy, stats, top_logp, top_index = ops.class_logprob_fwd(logits, labels, scale=scale, top=top, out=out)
+        logp, entropy, stats, top_logp, top_index = ops.class_logprob_fwd(logits, labels, scale=scale, top=top)
         ctx.save_for_backward(logits, labels, stats, entropy)
         ctx.scale = scale
         ctx.set_materialize_grads(False)

@@ -232,9 +232,11 @@ def class_logprob_fwd(logits, labels, *, scale: float = 1.0, top: int = 0, out=N
         _same_device(logits, "logp entropy stats", out)
     L = lib()
     with _Call(logits, stream) as call:
-        if out is None:                 # (parts of one buffer: an allocation costs more than a view)
-            all = call.empty((4 * m,), torch.float32)
-            logp, entropy, stats = all[:m], all[m:2 * m], all[2 * m:].view(m, 2)
+        if out is None:
+            # (parts of one buffer, an allocation costs more than a part, and to autograd tensors of their
+            # own, which may be written to)
+            logp, entropy, stats = torch.unsafe_split_with_sizes(call.empty((4 * m,), torch.float32), (m, m, 2 * m))
+            stats = stats.view(m, 2)
         else:
             logp, entropy, stats = out
         top_logp = top_index = None
