@@ -109,6 +109,12 @@ struct Side {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
                 REX_LDS_LOAD(r, to + (i * WAVES + wave) * 1024, all || k[i] < left_k ? off[i] : kBufOOB);
+        } else if (kSize == 4 && left_k >= kStep && left_rows >= ROWS) {
+            // nothing of the tile is outside (4096 x 4097 x 4095: 1312 -> 1167 us; of bf16, whose eight elements
+            // beside it stay in the same loop, 237 -> 248)
+            using Any = uint32_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) held[which][i] = *(const REX_GLOBAL Any *)(origin + off[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {

@@ -52,7 +52,7 @@ struct Product {
 // that would start another round on the GPU's 256 CUs are cut along k until they fill it, or all are; the
 // parts are written and read again at some 6 TB/s, and joined by a launch more, which costs 6 (1000 x 1024 x 1024
 // in binary32 31 us in two parts, 26 in one; 300 x 256 x 1024 in bf16 15 and 9).  Steps through registers take
-// longer (4096 x 4097 x 4095 in bf16 1.4 times as long, with an operand transposed 2.2 times; in binary32 1.2 times).
+// longer (4096 x 4097 x 4095 in bf16 1.4 times as long, with an operand transposed 2.2 times; in binary32 1.1 times).
 struct TileCost {
     int kind, bm, bn;
     double step, alone, around;
