@@ -20,7 +20,8 @@ extern "C" {
  * 0 for every other place.  weight, weight_out: float[batch][32 * max_pages], which may be the same
  * buffer; weight may be NULL (zeros; decay is then not used).  lse: float[batch][heads][num_q], as
  * box_memory_attn_fwd wrote it, or the log sum of a softmax over more keys than these; a row whose
- * lse is not finite adds nothing.  exp(s - lse) is as exact as lse is: its relative error is up to
+ * lse is not finite adds nothing, whatever its query and biases hold, and a logit that is NaN in a row whose
+ * lse is finite adds nothing.  exp(s - lse) is as exact as lse is: its relative error is up to
  * 2^-23 |lse| more than that of the difference.  decay: finite. */
 re_status_t box_memory_weigh(const box_memory_t *m, const box_recall_t *r, const float *lse,
                              const float *weight, float decay, float *weight_out, void *stream);

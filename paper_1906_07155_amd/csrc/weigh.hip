@@ -55,8 +55,15 @@ __device__ __forceinline__ void widen_codes(const KeyCodes<DB> &x, typename Num<
         }
 }
 
+// exp2(min(d, 0)) of a logit less its row's log sum, in units of log 2, and 0 where d is NaN (the median of
+// three is their least where one of them is NaN; with -inf for the lowest the compiler would leave it out): a
+// NaN logit adds nothing, nor does any logit, NaN and +inf among them, less the +inf of a row that is none.
+__device__ __forceinline__ float weight_of(float d) {
+    return __builtin_amdgcn_exp2f(__builtin_amdgcn_fmed3f(d, 0.0f, -3e38f));
+}
+
 // Adds a column's weights of eight keys, in units of log 2: ks the codes' scales times that of the
-// logits, bias by key, lse +inf for a column that is none.
+// logits, bias by key, lse as row_reference has it.
 template <typename T, int DB>
 __device__ __forceinline__ void add_weights(const typename Num<T>::Frag (&kf)[2][DB], const f32x4 (&ks)[2],
                                             const typename Num<T>::Frag (&q)[DB], const f32x4 (&bias)[2], float lse,
@@ -67,21 +74,12 @@ __device__ __forceinline__ void add_weights(const typename Num<T>::Frag (&kf)[2]
 #pragma unroll
         for (int k = 0; k < DB; ++k) x[t] = Num<T>::mma(kf[t][k], q[k], x[t]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float s = fmaf(x[j >> 2][j & 3], ks[j >> 2][j & 3], bias[j >> 2][j & 3]);
-        sum[j] += __builtin_amdgcn_exp2f(fminf(s - lse, 0.0f));
-    }
+    for (int j = 0; j < 8; ++j)
+        sum[j] += weight_of(fmaf(x[j >> 2][j & 3], ks[j >> 2][j & 3], bias[j >> 2][j & 3]) - lse);
 }
-// A row's log sum in units of log 2, +inf where the row adds nothing; its query is then 0, whatever it
-// holds (a NaN among it would get past the difference).
-template <int DB, typename Frag>
-__device__ __forceinline__ float row_reference(float lse, bool in, Frag (&q)[DB]) {
-    const bool on = in && fabsf(lse) < kInf;
-    if (__any(in && !on)) {
-#pragma unroll
-        for (int k = 0; k < DB; ++k) q[k] = on ? q[k] : Frag{};
-    }
-    return on ? lse * kLog2e : kInf;
+// A row's log sum in units of log 2, +inf where the row adds nothing.
+__device__ __forceinline__ float row_reference(float lse, bool in) {
+    return in && fabsf(lse) < kInf ? lse * kLog2e : kInf;
 }
 // The scale of a lane's eight keys, of their logits in units of log 2.
 __device__ __forceinline__ void logit_scales(f32x4 (&s)[2], float scale) {
@@ -149,7 +147,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void weigh_few_kernel(WeighArgs w) 
 #pragma unroll
                     for (int k = 0; k < DB; ++k) q[i][k] = x[0][k];
                     lse[i] = as_global<float>(w.lse)[(static_cast<int64_t>(b) * a.H + h) * a.Nq + min(n, qlen - 1)];
-                    lse[i] = row_reference<DB>(lse[i], n < qlen && first + i < a.Hkv, q[i]);
+                    lse[i] = row_reference(lse[i], n < qlen && first + i < a.Hkv);
                     bias[i][0] = bias[i][1] = f32x4{};
                     if (BIAS && n < qlen) {
                         const float *table = a.bias + static_cast<int64_t>(h) * a.rule.nb * a.rule.nb;
@@ -198,14 +196,13 @@ __global__ __launch_bounds__(kLaneWaves * 64) void weigh_lane_kernel(WeighArgs w
             const int kh = i / COMBOS, c = i % COMBOS, of = c / nq, row = c % nq;
             const bool in = of < a.group && row < qlen;
             const float lse = in ? as_global<float>(w.lse)[(static_cast<int64_t>(b) * a.H + kh * a.group + of) * nq + row] : kInf;
-            refs[i] = fabsf(lse) < kInf ? lse * kLog2e : kInf;
+            refs[i] = row_reference(lse, in);
         }
         for (int i = tid; i < a.Hkv * a.D * COMBOS; i += kLaneWaves * 64) {
             const int e = i & 3, c = (i >> 2) % COMBOS, rest = (i >> 2) / COMBOS, kh = rest / (a.D / 4);
             const int ch = rest % (a.D / 4) * 4 + e, of = c / nq, row = c % nq, h = kh * a.group + of;
             float x = 0.0f;
-            if (of < a.group && row < qlen &&
-                fabsf(as_global<float>(w.lse)[(static_cast<int64_t>(b) * a.H + h) * nq + row]) < kInf)
+            if (of < a.group && row < qlen)
                 x = load_f32<T>(as_global<T>(static_cast<const char *>(a.q.p) + b * a.q.sb + static_cast<int64_t>(row) * a.q.sr +
                                              static_cast<int64_t>(h) * a.q.sh) + ch);
             queries[i] = x;
@@ -258,7 +255,7 @@ __global__ __launch_bounds__(kLaneWaves * 64) void weigh_lane_kernel(WeighArgs w
                 for (int c = 0; c < COMBOS; ++c) {
                     float bias = 0.0f;
                     if (BIAS) bias = wide_entry(a.bias + static_cast<int64_t>(kh) * a.group * nb2, 4 * at[c]) * kLog2e;
-                    sum += __builtin_amdgcn_exp2f(fminf(fmaf(dot[c], scale, bias) - refs[kh * COMBOS + c], 0.0f));
+                    sum += weight_of(fmaf(dot[c], scale, bias) - refs[kh * COMBOS + c]);
                 }
             }
             sum += __shfl_xor(sum, 32);
@@ -360,7 +357,7 @@ __global__ __launch_bounds__(WAVES * 64) void weigh_many_kernel(WeighArgs w) {
             Frag q[DB];
 #pragma unroll
             for (int k = 0; k < DB; ++k) q[k] = next[0][k];
-            const float lse = row_reference<DB>(next_lse, at + n < cols, q);
+            const float lse = row_reference(next_lse, at + n < cols);
             const int here = at;
             at += 16;
             if (at >= 16 * tiles) {
