@@ -9,6 +9,8 @@ roi_extract gives for each RoI through two shared dense layers to class scores a
     loss = head.loss(scores, labels)                # mean of -log p over the labels that count
     logp, classes = head.best(scores, 5)            # per RoI: the five likeliest classes
 
+There are no second and no forward-mode derivatives: they are refused.
+
 All of it can be captured into a HIP graph.  A captured `backward()` needs leaves of which no eager graph
 lives any more (torch accumulates their gradients on that graph's stream); torch.autograd.grad does not.
 """
@@ -18,7 +20,7 @@ import torch
 from torch import nn
 
 from . import head as ops
-from .relation_head import once
+from .relation_head import differentiated, once
 
 
 def _rows(x):
@@ -74,7 +76,7 @@ def linear_act(x, weight, bias=None, *, act: str = "none", residual=None):
         raise ValueError("residual must have shape %s (got %s)" % (shape, tuple(residual.shape)))
     rows, added = _rows(x), None if residual is None else _rows(residual)
     given = (rows, _rows(weight), None if bias is None else bias.contiguous(), added)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given):
+    if differentiated(*given):
         y = LinearActFunction.apply(*given, act)
     else:
         y = ops.linear_act_fwd(*given[:3], act=act, residual=added)[0]
@@ -85,7 +87,7 @@ def class_logprob(logits, labels, *, scale: float = 1.0, top: int = 0):
     """head.class_logprob_fwd with gradients of logp and entropy for the logits.  Returns (logp,
     entropy, top_logp, top_index); the last two have no gradient (None where top is 0)."""
     logits = _rows(logits)
-    if torch.is_grad_enabled() and logits.requires_grad:
+    if differentiated(logits):
         return ClassLogprobFunction.apply(logits, labels, scale, top)
     logp, entropy, _, top_logp, top_index = ops.class_logprob_fwd(logits, labels, scale=scale, top=top)
     return logp, entropy, top_logp, top_index
@@ -118,4 +120,4 @@ class BoxHead(nn.Module):
         """(log probabilities, classes) of each row's `top` likeliest classes, background among them."""
         labels = scores.new_full(scores.shape[:1], -1, dtype=torch.int64)
         with torch.no_grad():
-            return class_logprob(scores, labels, scale=scale, top=top)[2:]
+            return class_logprob(scores.detach(), labels, scale=scale, top=top)[2:]

@@ -16,6 +16,7 @@ from typing import List, Optional, Sequence
 
 import torch
 from torch import nn
+from torch.autograd import forward_ad
 
 from . import evict, relation
 
@@ -23,6 +24,16 @@ from . import evict, relation
 def linear_act(*args, **kw):
     from .box_head import linear_act as fused           # (which needs `once` of this module)
     return fused(*args, **kw)
+
+
+def differentiated(*tensors) -> bool:
+    """Whether a call on these (None skipped) goes through autograd: one of them wants a gradient, or has a
+    forward-mode tangent, which the functions here refuse (outside autograd it would be lost)."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        return True
+    # (0.05 us to see that there is no level, 0.3 to look at each tensor)
+    return forward_ad._current_level >= 0 and any(
+        t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 class _Final(torch.autograd.Function):
@@ -100,7 +111,7 @@ def box_attention(q, k, v, *, bias=None, q_boxes=None, k_boxes=None, q_len=None,
                   **cfg):
     """relation.box_attn_fwd with gradients for q, k, v and bias.  Returns (out, lse); lse has
     no gradient.  `cfg`: scale, first_exp, octave_steps."""
-    if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, bias))):
+    if not differentiated(q, k, v, bias):
         relation._rows4(q, "q")
         lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
         return relation.box_attn_fwd(q, k, v, bias=bias, q_boxes=q_boxes, k_boxes=k_boxes, q_len=q_len,
@@ -117,7 +128,7 @@ def gated_norm(x, branch=None, *, gate=None, post_weight=None, post_bias=None, p
         raise ValueError("neither a branch nor the second norm: nothing to do")
     cfg = dict(alpha=alpha, norm=norm, eps=eps)
     given = (x, branch, gate, post_weight, post_bias, pre_weight, pre_bias)
-    if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given)):
+    if not differentiated(*given):
         return relation.gated_norm_fwd(x, branch, gate=gate, post_weight=post_weight, post_bias=post_bias,
                                        pre_weight=pre_weight, pre_bias=pre_bias, second=second, **cfg)[:2]
     first, u = GatedNormFunction.apply(*given, cfg, second)
@@ -348,6 +359,8 @@ class RelationHead(nn.Module):
             if memory is not None:
                 def recalled(q, k, v, geo, held=memory.layers[i], first_layer=i == 0):
                     nonlocal weight
+                    if differentiated(q, k, v):
+                        raise RuntimeError("a memory is for inference: what it recalls has no forward-mode tangent")
                     # both parts in binary32 (the memory's by binary32 queries), rounded when joined
                     out, lse, full = relation.box_attn_fwd(q, k, v, save=True, **geo)
                     far, far_lse = relation.box_memory_attn_fwd(q.float(), held, pages, remembered, q_boxes=boxes,
