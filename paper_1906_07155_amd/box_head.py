@@ -38,7 +38,7 @@ class LinearActFunction(torch.autograd.Function):
         return y
 
     @staticmethod
-    @once
+    @once("linear_act")
     def backward(ctx, grad_y):
         x, weight, bias, saved = ctx.saved_tensors
         want = ctx.needs_input_grad
@@ -60,7 +60,7 @@ class ClassLogprobFunction(torch.autograd.Function):
         return logp, entropy, top_logp, top_index
 
     @staticmethod
-    @once
+    @once("class_logprob")
     def backward(ctx, grad_logp, grad_entropy, *_):
         logits, labels, stats, entropy = ctx.saved_tensors
         if grad_logp is None and grad_entropy is None:

@@ -37,29 +37,32 @@ def differentiated(*tensors) -> bool:
 
 
 class _Final(torch.autograd.Function):
-    """Gradients that have no gradient themselves."""
+    """Gradients of an operator that have no gradient themselves."""
 
     @staticmethod
-    def forward(ctx, _, *grads):
+    def forward(ctx, operator, _, *grads):
+        ctx.operator = operator
         return tuple(g.view_as(g) for g in grads)
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("box_attention and gated_norm are once_differentiable: their gradients have none")
+        raise RuntimeError("%s is once_differentiable: its gradients have none" % ctx.operator)
 
 
-def once(backward):
-    """A backward whose results, under create_graph, fail where they are differentiated again instead
-    of counting as constants (torch's once_differentiable does so only where the upstream gradient
+def once(operator):
+    """Of an operator's backward: its results, under create_graph, fail where they are differentiated again
+    instead of counting as constants (torch's once_differentiable does so only where the upstream gradient
     itself wants one)."""
-    def wrapped(ctx, *upstream):
-        with torch.no_grad():
-            found = backward(ctx, *upstream)
-        if not torch.is_grad_enabled():
-            return found
-        given = iter(_Final.apply(torch.empty(0, requires_grad=True), *(g for g in found if g is not None)))
-        return tuple(None if g is None else next(given) for g in found)
-    return wrapped
+    def wrap(backward):
+        def wrapped(ctx, *upstream):
+            with torch.no_grad():
+                found = backward(ctx, *upstream)
+            if not torch.is_grad_enabled():
+                return found
+            given = iter(_Final.apply(operator, torch.empty(0, requires_grad=True), *(g for g in found if g is not None)))
+            return tuple(None if g is None else next(given) for g in found)
+        return wrapped
+    return wrap
 
 
 class BoxAttnFunction(torch.autograd.Function):
@@ -73,7 +76,7 @@ class BoxAttnFunction(torch.autograd.Function):
         return out, lse
 
     @staticmethod
-    @once
+    @once("box_attention")
     def backward(ctx, grad_out, _):
         q, k, v, bias, q_boxes, k_boxes, q_len, k_len, k_mask, out, lse, out_f32 = ctx.saved_tensors
         grads = relation.box_attn_bwd(grad_out.contiguous(), q, k, v, out, lse, out_f32, bias=bias,
@@ -94,7 +97,7 @@ class GatedNormFunction(torch.autograd.Function):
         return (u if branch is None else y), (None if branch is None else u)
 
     @staticmethod
-    @once
+    @once("gated_norm")
     def backward(ctx, grad_y, grad_u):
         x, branch, gate, w1, c1, w2, c2, stats = ctx.saved_tensors
         if branch is None:                  # the one output is u
