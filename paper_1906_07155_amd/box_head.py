@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import torch
 from torch import nn
+from torch.nn.modules import module as modules
 
 from . import head as ops
 from .relation_head import differentiated, once
@@ -93,6 +94,22 @@ def class_logprob(logits, labels, *, scale: float = 1.0, top: int = 0):
     return logp, entropy, top_logp, top_index
 
 
+class Dense(nn.Linear):
+    """nn.Linear in linear_act's kernels."""
+
+    def forward(self, x, act: str = "none"):
+        return linear_act(x, self.weight, self.bias, act=act)
+
+
+def dense(layer, x, act: str = "none"):
+    """A layer, called as a module, and an activation ("none" or "relu").  A Dense has it in its kernel, where
+    no hook is there to see the result before it, as those of nn.Linear do."""
+    if act == "none":
+        return layer(x)
+    seen = layer._forward_hooks or layer._backward_hooks or layer._backward_pre_hooks or modules._has_any_global_hook()
+    return layer(x, act=act) if isinstance(layer, Dense) and not seen else torch.relu(layer(x))
+
+
 class BoxHead(nn.Module):
     """Two shared dense layers of `hidden` channels, then scores of `classes` classes and background
     (the last) and four deltas for each class."""
@@ -100,15 +117,15 @@ class BoxHead(nn.Module):
     def __init__(self, in_features: int, classes: int, hidden: int = 1024):
         super().__init__()
         self.classes = classes
-        self.fc1, self.fc2 = nn.Linear(in_features, hidden), nn.Linear(hidden, hidden)
-        self.score, self.delta = nn.Linear(hidden, classes + 1), nn.Linear(hidden, 4 * classes)
+        self.fc1, self.fc2 = Dense(in_features, hidden), Dense(hidden, hidden)
+        self.score, self.delta = Dense(hidden, classes + 1), Dense(hidden, 4 * classes)
 
     def forward(self, x):
         """x: [K, channels, height, width] (or [K, in_features]) of the parameters' type."""
         x = x.flatten(1)
         for fc in (self.fc1, self.fc2):
-            x = linear_act(x, fc.weight, fc.bias, act="relu")
-        return tuple(linear_act(x, fc.weight, fc.bias) for fc in (self.score, self.delta))
+            x = dense(fc, x, "relu")
+        return dense(self.score, x), dense(self.delta, x)
 
     def loss(self, scores, labels):
         """Mean of -log p over the labels in [0, classes]; others are not counted."""

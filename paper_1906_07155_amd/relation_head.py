@@ -21,9 +21,9 @@ from torch.autograd import forward_ad
 from . import evict, relation
 
 
-def linear_act(*args, **kw):
-    from .box_head import linear_act as fused           # (which needs `once` of this module)
-    return fused(*args, **kw)
+def box_head():
+    from . import box_head as module                    # (which needs `once` of this module)
+    return module
 
 
 def differentiated(*tensors) -> bool:
@@ -250,11 +250,12 @@ class RelationLayer(nn.Module):
         self.fused = fused
         self.heads, self.kv_heads, self.dim = heads, kv_heads, channels // heads
         self.norm = norm
-        self.qkv = nn.Linear(channels, (heads + 2 * kv_heads) * self.dim)
-        self.proj = nn.Linear(channels, channels)
-        self.fc1 = nn.Linear(channels, 2 * channels)
-        self.fc2 = nn.Linear(2 * channels, channels)
-        self.gate = nn.Linear(channels, channels)
+        linear = box_head().Dense if fused else nn.Linear
+        self.qkv = linear(channels, (heads + 2 * kv_heads) * self.dim)
+        self.proj = linear(channels, channels)
+        self.fc1 = linear(channels, 2 * channels)
+        self.fc2 = linear(2 * channels, channels)
+        self.gate = linear(channels, channels)
         # parameters of the kernels stay binary32 when the module's type is changed
         self.bias = nn.Parameter(torch.zeros(heads, buckets, buckets))
         self.post = nn.ParameterList([nn.Parameter(torch.ones(channels)) for _ in range(2)])
@@ -274,7 +275,7 @@ class RelationLayer(nn.Module):
 
     def _dense(self, layer, x, act: str = "none"):
         if self.fused:
-            return linear_act(x, layer.weight, layer.bias, act=act)
+            return box_head().dense(layer, x, act)
         return torch.relu(layer(x)) if act == "relu" else layer(x)
 
     def forward(self, x, u, gate, boxes, lengths, recall, last: bool, pre_next):
