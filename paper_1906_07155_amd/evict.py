@@ -113,17 +113,25 @@ def box_memory_weigh(q, memory: Sequence, pages, lengths, lse, *, weight=None, d
 def box_memory_evict(memory: Sequence, pages, lengths, weight, keep, *, workspace=None, stream=None):
     """Each stream keeps its keep[b] (int32 [B]) boxes of the largest weight (float32
     [B, 32 * max_pages]), of equal ones those in lower places, in its first places; only kept boxes
-    further on are moved.  pages (each named once) and lengths as for box_memory_attn_fwd.  Returns
+    further on are moved.  pages (each named once) and lengths as for box_memory_attn_fwd.  memory may
+    also be a list of memories with these pages (a head's layers), whose boxes are moved alike: where
+    the call raises for want of memory or for an argument, none of them has changed.  Returns
     (lengths, weight, origin): int32 [B], float32 [B, 32 * max_pages] of the boxes where they now are (0
     behind them), and int32 [B, 32 * max_pages], the place that each was in (-1 behind them)."""
     torch = _torch()
-    m, _, _ = _memory_descriptor(memory)
+    several = [memory] if len(memory) == 0 or torch.is_tensor(memory[0]) else list(memory)
+    held_by = [_memory_descriptor(m)[0] for m in several]
     B, p = _table(pages, lengths)
     shape = (B, p * MEMORY_PAGE)
     _dense(weight, shape, "weight", torch.float32)
     _dense(keep, (B,), "keep", torch.int32)
-    like = memory[0]
+    like = several[0][0]
+    for m in several[1:]:
+        if m[0].shape[0] != like.shape[0]:
+            raise ValueError("memories with one table must have as many pages (got %d and %d)"
+                             % (like.shape[0], m[0].shape[0]))
     _same_device(like, "pages lengths weight keep", (pages, lengths, weight, keep))
+    _same_device(like, " ".join(["memory"] * len(several)), [m[0] for m in several])
     if workspace is not None:
         binding._workspace(workspace, like)
         _same_device(like, "workspace", (workspace,))
@@ -132,9 +140,10 @@ def box_memory_evict(memory: Sequence, pages, lengths, weight, keep, *, workspac
     with _Call(like, stream) as c:
         left, held, origin = c.empty((B,), torch.int32), c.empty(shape, torch.float32), c.empty(shape, torch.int32)
         need = 0
-        if workspace is None:
-            need = _size(L.box_memory_evict_workspace_size, "box_memory_evict_workspace_size", m, d)
+        if workspace is None or len(several) > 1:       # (which looks at all that the call looks at)
+            need = max(_size(L.box_memory_evict_workspace_size, "box_memory_evict_workspace_size", m, d) for m in held_by)
         ws, wsb, _keep = c.workspace(workspace, need)
-        check(L.box_memory_evict(m, d, left.data_ptr(), held.data_ptr(), origin.data_ptr(), ws, wsb, c.stream),
-              "box_memory_evict")
+        for m in held_by:
+            check(L.box_memory_evict(m, d, left.data_ptr(), held.data_ptr(), origin.data_ptr(), ws, wsb, c.stream),
+                  "box_memory_evict")
     return left, held, origin

@@ -187,11 +187,16 @@ class BoxMemory:
     def take(self, counts: Sequence[int]):
         """Places for counts[s] new boxes of each stream: int64 slots of all of them, stream
         after stream.  Raises (and takes nothing) where the pool has too few pages."""
+        return self._take(counts, self.weight)
+
+    def _take(self, counts: Sequence[int], weight):
+        """take, by these weights, which are the memory's where it succeeds."""
         self.check(counts)
-        if self.weight is not None:
-            self._make_room(counts)
         page = relation.MEMORY_PAGE
         free, table, used = list(self.free), [list(p) for p in self.table], list(self.used)
+        if weight is not None:                          # the boxes of least weight leave, as many as have to
+            used = [min(u, page * self.max_pages - c) for u, c in zip(used, counts)]
+        keep = list(used)
         slots: List[int] = []
         for s, c in enumerate(counts):
             pages = table[s]
@@ -207,20 +212,12 @@ class BoxMemory:
                 used[s] += n
                 c -= n
         made = torch.tensor(slots, dtype=torch.int64, device=self.device)
-        self.free, self.table, self.used, self._device_table = free, table, used, None
+        if weight is not None and keep != self.used:    # (the last that may fail: it moves boxes)
+            held, lengths = self.pages_and_lengths()
+            kept = torch.tensor(keep, dtype=torch.int32, device=self.device)
+            _, weight, _ = evict.box_memory_evict(self.layers, held, lengths, weight, kept)
+        self.free, self.table, self.used, self.weight, self._device_table = free, table, used, weight, None
         return made
-
-    def _make_room(self, counts: Sequence[int]) -> None:
-        """The boxes of least weight leave the streams that counts[s] new ones do not fit into."""
-        most = relation.MEMORY_PAGE * self.max_pages
-        keep = [min(used, most - c) for used, c in zip(self.used, counts)]
-        if keep == self.used:
-            return
-        pages, lengths = self.pages_and_lengths()
-        kept = torch.tensor(keep, dtype=torch.int32, device=self.device)
-        for held in self.layers:                        # one decision, made for each of them
-            _, weight, _ = evict.box_memory_evict(held, pages, lengths, self.weight, kept)
-        self.weight, self.used, self._device_table = weight, keep, None
 
     def forget(self, stream: int) -> None:
         """The stream's pages go back to the pool."""
@@ -381,11 +378,11 @@ class RelationHead(nn.Module):
             last = i + 1 == len(self.layers)
             x, u = layer(x, u, gate, boxes, lengths, recalled, last,
                          None if last else self.layers[i + 1].pre[0])
+        if lengths is not None:
+            x = torch.where(valid, x, torch.zeros_like(x))
         if memory is not None:                  # nothing is taken or written before all of it is there
             kept = boxes.reshape(B * n, 4)[rows].contiguous()
-            if weight is not None:
-                memory.weight = weight
-            slots = memory.take(host)
+            slots = memory._take(host, weight)
             for held, k, v in fresh:
                 relation.box_memory_append(held, slots, k, v, kept)
-        return x if lengths is None else torch.where(valid, x, torch.zeros_like(x))
+        return x

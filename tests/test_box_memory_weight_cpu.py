@@ -1,0 +1,125 @@
+"""A memory that forgets by weight is taken from wholly or not at all, whatever fails on the way (host code;
+the kernel's part is played by a plain one)."""
+import pytest
+import torch
+
+from paper_1906_07155_amd import relation_head
+from paper_1906_07155_amd.relation_head import BoxMemory
+
+
+def state(m):
+    return list(m.free), [list(p) for p in m.table], list(m.used), m.weight.clone()
+
+
+def same(a, b):
+    return a[:3] == b[:3] and torch.equal(a[3], b[3])
+
+
+class Evictions:
+    """Stands for box_memory_evict: which memories were given, and what failed before any was changed."""
+
+    def __init__(self):
+        self.calls, self.fail = [], False
+
+    def __call__(self, memory, pages, lengths, weight, keep):
+        if self.fail:
+            raise MemoryError("no room")
+        self.calls.append((memory, pages.clone(), lengths.tolist(), weight.clone(), keep.tolist()))
+        held = torch.zeros_like(weight)
+        for s, k in enumerate(keep.tolist()):
+            held[s, :k] = weight[s, :int(lengths[s])].sort(descending=True)[0][:k]
+        return keep.clone(), held, None
+
+
+@pytest.fixture
+def made(monkeypatch):
+    m, evict = BoxMemory(8, 2, 3, 2, 32, layers=3, device="cpu", evict="weight"), Evictions()
+    monkeypatch.setattr(relation_head.evict, "box_memory_evict", evict)
+    m.take([60, 10])
+    m.take([30, 0])
+    m.weight[0, :90] = torch.arange(90.0)
+    return m, evict
+
+
+def test_all_layers_in_one_call(made):
+    """No layer is changed before what every layer needs is there."""
+    m, evict = made
+    m.take([40, 5])
+    assert len(evict.calls) == 1
+    memory, pages, lengths, weight, keep = evict.calls[0]
+    assert len(memory) == 3 and all(a is b for a, b in zip(memory, m.layers))
+    assert lengths == [90, 10] and keep == [56, 10] and m.used == [96, 15]
+    assert pages.tolist()[0] == m.table[0]
+
+
+def test_an_eviction_that_fails_takes_nothing(made):
+    m, evict = made
+    before = state(m)
+    evict.fail = True
+    with pytest.raises(MemoryError):
+        m.take([40, 5])
+    assert same(before, state(m))
+    evict.fail = False
+    assert len(m.take([40, 5])) == 45 and m.used == [96, 15]
+
+
+@pytest.mark.parametrize("which", range(6))
+def test_a_tensor_that_cannot_be_made_takes_nothing(made, monkeypatch, which):
+    """The which-th of a call's tensors; after the eviction, which cannot be undone, none is made."""
+    m, evict = made
+    m.forget(1)                                         # (the device's table is made anew)
+    before, count, tensor = state(m), [0], torch.tensor
+
+    def fail(*args, **kw):
+        count[0] += 1
+        if count[0] == which + 1:
+            raise MemoryError("no room")
+        return tensor(*args, **kw)
+    with monkeypatch.context() as p:
+        p.setattr(relation_head.torch, "tensor", fail)
+        try:
+            m.take([40, 5])
+        except MemoryError:
+            assert same(before, state(m)) and not evict.calls
+            return
+    assert count[0] <= which and m.used == [96, 5]
+
+
+def test_a_frame_that_fails_leaves_the_weights(monkeypatch):
+    """A frame that is tried again adds its attention once."""
+    rel = relation_head.relation
+    monkeypatch.setattr(rel, "box_attn_fwd", lambda q, *a, **kw: (q.clone(), torch.zeros(q.shape[0], q.shape[2], q.shape[1]), None))
+    monkeypatch.setattr(rel, "box_memory_attn_fwd", lambda q, *a, **kw: (q.clone(), torch.zeros(q.shape[0], q.shape[2], q.shape[1])))
+    monkeypatch.setattr(rel, "gated_norm_fwd", lambda x, *a, **kw: (x.clone(), x.clone(), None))
+    monkeypatch.setattr(rel, "box_memory_append", lambda *a: None)
+    monkeypatch.setattr(relation_head.evict, "box_memory_weigh", lambda *a, weight, decay, **kw: decay * weight + 1)
+    evict = Evictions()
+    monkeypatch.setattr(relation_head.evict, "box_memory_evict", evict)
+    head = relation_head.RelationHead(16, heads=2)
+    memory = BoxMemory(8, 1, 3, 2, 8, layers=2, device="cpu", evict="weight", decay=0.5)
+    x, boxes = torch.ones(1, 60, 16), torch.rand(1, 60, 4)
+    with torch.no_grad():
+        head(x, boxes, [60], memory)
+        before = state(memory)
+        evict.fail = True
+        with pytest.raises(MemoryError):
+            head(x, boxes, [60], memory)
+        assert same(before, state(memory))
+        evict.fail = False
+        head(x, boxes, [60], memory)
+    # the new weights, once decayed, decide: two layers add 1 each
+    assert torch.equal(evict.calls[0][3], 0.5 * before[3] + 2) and memory.used == [96]
+    assert torch.equal(memory.weight[0, :36], (0.5 * before[3] + 2)[0, :36]) and not memory.weight[0, 36:].any()
+
+
+def test_several_memories_that_do_not_belong_together(monkeypatch):
+    import paper_1906_07155_amd as rex
+    from paper_1906_07155_amd import evict, relation
+    for module in (relation, evict):
+        monkeypatch.setattr(module, "_need_cuda", lambda *a: None)
+    monkeypatch.setattr(evict, "_Call", None)           # (nothing is called)
+    m, i32 = rex.box_memory(4, 2, 32, device="cpu"), lambda *s: torch.zeros(s, dtype=torch.int32)
+    rest = dict(pages=i32(2, 2), lengths=i32(2), weight=torch.zeros(2, 64), keep=i32(2))
+    for bad in ([], [()], [m, m[:4]], [m, rex.box_memory(5, 2, 32, device="cpu")], [m[:4], m]):
+        with pytest.raises(ValueError):
+            rex.box_memory_evict(bad, **rest)
