@@ -54,7 +54,7 @@ typedef struct {
  * few results have long sums; in the backward the gradient of t and partial column sums.  Host-only. */
 re_status_t linear_act_workspace_size(const linear_act_t *a, int32_t backward, size_t *bytes);
 
-/* y: [rows][outs] dense.  slope: the activation's slope at every t, [rows][outs] dense, which the
+/* y: [rows][outs] dense, no part of it in x, weight or bias; it may be the residual, where that is dense.  slope: the activation's slope at every t, [rows][outs] dense, which the
  * backward takes, or NULL: binary32 with binary32 data; with bf16 data 3 * rows * outs bytes, for
  * numbers c of 24 bits that stand for c * 2^-23 - 1/4 (all ones: NaN), the upper 16 bits of all and then
  * the lower 8 of all, 16-byte aligned.  It has to be NULL for RE_ACT_NONE. */

@@ -122,9 +122,9 @@ def linear_act_fwd(x, weight, bias=None, *, act: str = "none", residual=None, sa
                    workspace=None, stream=None):
     """y = act(x weight^T + bias) + residual of x [rows, ins] and weight [outs, ins] (one dtype, rows
     may be strided), bias [outs] of that dtype or float32, act "none", "relu", "gelu" or "silu",
-    residual [rows, outs].  Returns (y, saved): saved, made where `save` is true, is what the
-    backward takes: None without an activation, y itself for relu without a residual, else the
-    activation's slopes."""
+    residual [rows, outs].  `out` may be the residual's memory and none of the others'.  Returns
+    (y, saved): saved, made where `save` is true, is what the backward takes: None without an
+    activation, y itself for relu without a residual, else the activation's slopes."""
     d = _linear_descriptor(x, weight, bias, act, residual)
     shape = (x.shape[0], weight.shape[0])
     if out is not None:

@@ -79,3 +79,13 @@ def test_no_rows(dtype):
     x, w, b, r, gy = T.make(9, 0, 24, 40, dtype, F32, False)
     gx, gw, gb = rex.linear_act_bwd(gy, x, w, None, bias=b)
     assert gx.shape == (0, 40) and bool((gw == 0).all()) and bool((gb == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(5, 72, 136), (16, 40, 8192), (9000, 12, 64), (300, 81, 1024), (1000, 1024, 2048), (513, 77, 250),
+                                   (257, 255, 8199)])
+def test_a_residual_that_is_written_to(dtype, m, n, k):
+    x, w, b, r, _ = T.make(m, m, n, k, dtype, F32, True)
+    want = rex.linear_act_fwd(x, w, b, act="gelu", residual=r)[0]
+    got = rex.linear_act_fwd(x, w, b, act="gelu", residual=r, out=r)[0]
+    assert got is r and torch.equal(got, want)
