@@ -28,8 +28,7 @@ __device__ __forceinline__ float erfc_over_exp(float z) {
     return t * fmaf(r, t, 0.25388532876968384f);
 }
 
-// act(x), and its slope at x where SLOPE, of four.
-template <bool SLOPE>
+// act(x), and its slope at x, of four.
 __device__ __forceinline__ void activate(int act, f32x4 &x, float (&slope)[4]) {
     if (act == kActRelu) {                      // NaN stays, and lets the gradient through
 #pragma unroll
@@ -43,14 +42,14 @@ __device__ __forceinline__ void activate(int act, f32x4 &x, float (&slope)[4]) {
             const float e = __builtin_amdgcn_exp2f(x[i] * x[i] * (-0.5f * kLog2e));
             const float tail = 0.5f * e * erfc_over_exp(fabsf(x[i]) * 0.70710678118654752f);
             const float phi = x[i] < 0.0f ? tail : 1.0f - tail;
-            if (SLOPE) slope[i] = fmaf(x[i] * 0.39894228040143268f, e, phi);
+            slope[i] = fmaf(x[i] * 0.39894228040143268f, e, phi);
             x[i] *= phi;
         }
     } else if (act == kActSilu) {               // x s, s (1 + x (1 - s))
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x[i]));
-            if (SLOPE) slope[i] = s * fmaf(x[i], 1.0f - s, 1.0f);
+            slope[i] = s * fmaf(x[i], 1.0f - s, 1.0f);
             x[i] *= s;
         }
     }
@@ -60,7 +59,9 @@ __device__ __forceinline__ void activate(int act, f32x4 &x, float (&slope)[4]) {
 // steps of 2^-23 from -1/4 on (slopes lie in [-0.13, 1.13]; 0 and 1 are exact), all ones for NaN: the
 // upper 16 of all slopes, then the lower 8 of all.  (16 bits would do for the products, whose operands
 // are bf16, but the bias gradient, a binary32 sum over all rows, would be 1.3e-5 of itself off; binary32
-// would be a quarter more bytes than 24 bits, and there is nothing to evaluate in the backward.)
+// would be a quarter more bytes than 24 bits, and there is nothing to evaluate in the backward.  The step is
+// absolute: below x = -5.92 the slope of gelu, and below x = -19.6 that of silu, is under half of it and counts
+// as 0.)
 template <typename T> struct Slope;
 template <> struct Slope<float> {
     template <int V> static __device__ __forceinline__ void store(void *p, int64_t, int64_t at, const float *x) {
@@ -136,7 +137,7 @@ __device__ __forceinline__ void finish4(const GemmArgs &a, int left, int64_t at,
     float s[4], r[4] = {};
     if (a.vec) {                        // (then N is a multiple of 4)
         if (a.residual) load4<T>(a.residual, rat, r);
-        if (a.act != kActNone) activate<true>(a.act, x, s);
+        if (a.act != kActNone) activate(a.act, x, s);
         if (a.residual) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] += r[i];
@@ -145,7 +146,7 @@ __device__ __forceinline__ void finish4(const GemmArgs &a, int left, int64_t at,
         if (a.slope) Slope<T>::template store<4>(a.slope, static_cast<int64_t>(a.M) * a.N, at, s);
         return;
     }
-    if (a.act != kActNone) activate<true>(a.act, x, s);
+    if (a.act != kActNone) activate(a.act, x, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (i >= left) break;

@@ -51,8 +51,9 @@ struct Product {
 // it is hidden behind the products of other workgroups of the CU, which 256 x 256 has none of).  Tiles
 // that would start another round on the GPU's 256 CUs are cut along k until they fill it, or all are; the
 // parts are written and read again at some 6 TB/s, and joined by a launch more, which costs 6 (1000 x 1024 x 1024
-// in binary32 31 us in two parts, 26 in one; 300 x 256 x 1024 in bf16 15 and 9).  Steps through registers take
-// longer (4096 x 4097 x 4095 in bf16 1.4 times as long, with an operand transposed 2.2 times; in binary32 1.1 times).
+// in binary32 31 us in two parts, 26 in one; 300 x 256 x 1024 in bf16 15 and 9).  Steps through registers count
+// 1.5 times as much in bf16, 2.0 times with an operand transposed and 1.2 times in binary32 (4096 x 4097 x 4095
+// took 1.4, 2.2 and 1.1 times as long as rows of whole chunks).
 struct TileCost {
     int kind, bm, bn;
     double step, alone, around;

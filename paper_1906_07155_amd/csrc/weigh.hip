@@ -6,8 +6,9 @@
 // One to four rows that share a key head's keys (queries times the heads of a group): a lane has a box,
 // half a wave a key head, and products are sums of its lane: of sixteen columns of a matrix product
 // fifteen would be empty, and what is done with its results as well.  64 streams of 8192 boxes in 8 heads
-// of 32: one row 31 us (4.6 TB/s), as columns 91; four 53 and 98; 16 streams in 16 heads of 64: 45 and 56, 62
-// and 62.
+// of 32: one row 43 us with nothing in the caches (143 MB at 3.4 TB/s), 37 with two sets of inputs in turn; and
+// where the same call is repeated, as in all that follows, 28, as columns 91; four 53 and 98; 16 streams in 16
+// heads of 64: 45 and 56, 62 and 62.
 //
 // More: the logits are made as in the recall (attn_fwd.hpp), keys the rows of the products and queries
 // their columns, so a lane has eight keys of one query, and adds their weights up over heads and
@@ -15,8 +16,9 @@
 // a wave takes a page and all of its heads, several heads' codes on their way at once: 16 rows of those 64
 // streams 107 us.  Beyond, a workgroup takes a page, its waves share heads and queries out, and the buckets
 // of 256 queries against the page's boxes are computed once for all heads into LDS: 17 rows 123 us (155 the
-// other way), 128 249 (617); 300 rows against 6000 boxes in 16 heads of 64, 31: vector instructions bound
-// it, half of the time of the 188 CUs that have a page.
+// other way), 128 249 (617); 300 rows against 6000 boxes in 16 heads of 64, 31, of binary32 queries 64, whose
+// products take sixteen times as many matrix cycles: vector instructions bound the former, half of the time of
+// the 188 CUs that have a page.
 #include "attn.hpp"
 #include "evict.hpp"
 
