@@ -187,12 +187,8 @@ class BoxMemory:
     def take(self, counts: Sequence[int]):
         """Places for counts[s] new boxes of each stream: int64 slots of all of them, stream
         after stream.  Raises (and takes nothing) where the pool has too few pages."""
-        return self._take(counts, self.weight)
-
-    def _take(self, counts: Sequence[int], weight):
-        """take, by these weights, which are the memory's where it succeeds."""
         self.check(counts)
-        page = relation.MEMORY_PAGE
+        page, weight = relation.MEMORY_PAGE, self.weight
         free, table, used = list(self.free), [list(p) for p in self.table], list(self.used)
         if weight is not None:                          # the boxes of least weight leave, as many as have to
             used = [min(u, page * self.max_pages - c) for u, c in zip(used, counts)]
@@ -382,7 +378,12 @@ class RelationHead(nn.Module):
             x = torch.where(valid, x, torch.zeros_like(x))
         if memory is not None:                  # nothing is taken or written before all of it is there
             kept = boxes.reshape(B * n, 4)[rows].contiguous()
-            slots = memory._take(host, weight)
+            before, memory.weight = memory.weight, weight       # (the frame's own decide what leaves)
+            try:
+                slots = memory.take(host)
+            except BaseException:
+                memory.weight = before
+                raise
             for held, k, v in fresh:
                 relation.box_memory_append(held, slots, k, v, kept)
         return x

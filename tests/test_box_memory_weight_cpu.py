@@ -123,3 +123,21 @@ def test_several_memories_that_do_not_belong_together(monkeypatch):
     for bad in ([], [()], [m, m[:4]], [m, rex.box_memory(5, 2, 32, device="cpu")], [m[:4], m]):
         with pytest.raises(ValueError):
             rex.box_memory_evict(bad, **rest)
+
+
+def test_a_memory_with_places_of_its_own(monkeypatch):
+    """A frame's places are asked of take, also where a subclass has its own."""
+    rel = relation_head.relation
+    monkeypatch.setattr(rel, "box_attn_fwd", lambda q, *a, **kw: (q.clone(), torch.zeros(q.shape[0], q.shape[2], q.shape[1]), None))
+    monkeypatch.setattr(rel, "box_memory_attn_fwd", lambda q, *a, **kw: (q.clone(), torch.zeros(q.shape[0], q.shape[2], q.shape[1])))
+    monkeypatch.setattr(rel, "gated_norm_fwd", lambda x, *a, **kw: (x.clone(), x.clone(), None))
+    slots = []
+    monkeypatch.setattr(rel, "box_memory_append", lambda held, s, *a: slots.append(s))
+
+    class Memory(BoxMemory):
+        def take(self, counts):
+            return super().take(counts).flip(0)
+    head = relation_head.RelationHead(16, heads=2)
+    with torch.no_grad():
+        head(torch.ones(1, 5, 16), torch.rand(1, 5, 4), [5], Memory(8, 1, 3, 2, 8, layers=2, device="cpu"))
+    assert [s.tolist() for s in slots] == [[4, 3, 2, 1, 0]] * 2
