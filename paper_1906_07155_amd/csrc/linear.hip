@@ -158,7 +158,9 @@ hipError_t launch_skinny_join(const GemmArgs &a, int dtype, hipStream_t s) {
 //
 // g is rounded to bf16, where the data is, for the two products that follow: with an activation other than
 // max(t, 0) their results are then off by two roundings of 2^-9 in the mean, 2.3e-3 of their norm instead
-// of 1.7e-3.  In two parts it would be one, for twice the products (70 and 81 us more at that size).
+// of 1.7e-3 (torch's own bf16 layers, whose activation's gradient is a bf16 tensor: 2.4e-3, and so are their y and
+// bias gradients, which are 1.7e-3 here).  In two parts it would be one, for twice the products (70 and 81 us
+// more at that size).
 
 // 16 bytes of them
 template <typename T, int V> __device__ __forceinline__ void load_run(const T *p, float *x) {
